@@ -134,6 +134,42 @@ typedef struct {
                                            returns HYDRA_E_CAPACITY.                            */
 } hydra_kv;
 
+/* Paged KV cache in 8 bits (HYDRA_BF16 contexts).  Whole pages of verified tokens are "sealed": their K and V are
+ * held as one byte per element with an fp32 scale for each page, layer and head, K and V apart; a row's last, incomplete
+ * page and the tree nodes of a step stay in 16 bits.  Row b's slots below 16 * n_sealed[b] are read from the codes,
+ * page page_table[b * max_pages + s / 16]; all others from `tail`, whose page table is indexed by the same logical
+ * page numbers (tail.page_table[b * tail.max_pages + s / 16]) and has to name pages of the row's own for the slots
+ * 16 * n_sealed[b] .. seq_len[b] + T - 1 only.  So a row needs about T / 16 + 2 of them however long it is, taken in turn.
+ * Every value is rounded once, from the 16 bits that the 16-bit cache would hold, when its page is sealed:
+ *   HYDRA_KV8_INT8  value = code * scale, code in [-127, 127], the nearest one (ties to even); scale = the smallest
+ *                   number of 11 significant bits that is no less than max |x| / 127 over the page's 16 tokens of the head
+ *   HYDRA_KV8_E4M3  value = code * scale, code an 8-bit float (4 exponent and 3 mantissa bits, no infinities), rounded to
+ *                   nearest even; scale = the smallest power of two with max |x| / scale <= 448
+ * A block of zeros has scale 1.  k_codes and v_codes each hold n_layers * n_pages * H * 16 * Dh bytes; page p of layer l, head h
+ * starts at byte ((l * n_pages + p) * H + h) * 16 * Dh, 16-byte aligned; placement inside is private to the library.
+ * scales holds (scale of K, scale of V) of it at [((l * n_pages + p) * H + h) * 2]. */
+enum { HYDRA_KV8_INT8 = 0, HYDRA_KV8_E4M3 = 1 };
+typedef struct {
+    hydra_kv       tail;                /* 16-bit pages of the slots that are not sealed; tail.seq_len_hint bounds seq_len   */
+    void          *k_codes, *v_codes;   /* device                                   */
+    float         *scales;              /* device [n_layers, n_pages, H, 2]         */
+    const int32_t *page_table;          /* device [B, max_pages]                    */
+    int32_t       *n_sealed;            /* device [B]: whole pages held in 8 bits, 16 * n_sealed[b] <= seq_len[b]             */
+    int32_t        n_pages, max_pages;
+    int32_t        format;              /* HYDRA_KV8_INT8 or HYDRA_KV8_E4M3         */
+} hydra_kv8;
+
+/* The pages of a cache as a pool that rows take from, share and give back.  page_table[b, i] is the page of row b's slots
+ * 16 i .. 16 i + 15, or -1 where the row holds none; ref[p] is the number of entries that name page p, 0 = free.  Both are
+ * the caller's; before the first call the tables are all -1 and the counts all 0.  Every cache that goes by the table (the base
+ * cache, a Hydra++ prefix cache, the sealed pages of an 8-bit cache) shares its page numbers: contents are copied by
+ * hydra_kv_copy_pages / hydra_kv8_copy_pages, once for each. */
+typedef struct {
+    int32_t *page_table;                /* device [B, max_pages], in and out        */
+    int32_t *ref;                       /* device [n_pages], in and out             */
+    int32_t  n_pages, max_pages;
+} hydra_pages;
+
 typedef enum {
     HYDRA_W_EMBED = 0,      /* [V, d]                                  index, sub ignored      */
     HYDRA_W_LM_HEAD,        /* [V, d]                                                          */
@@ -185,7 +221,7 @@ size_t hydra_workspace_bytes(const hydra_ctx *ctx, int B);
 
 /* Device-side flags raised by kernels of this context since the last call of
  * this function (or since hydra_bind_weights): bit 0 = a row's seq_len + T
- * exceeded its page table or max_pos (row skipped), bit 1 = a token id outside
+ * exceeded its page table or max_pos (row skipped), or n_sealed or a length was out of range, or a pool had too few pages, bit 1 = a token id outside
  * [0, V) (treated as 0), bit 2 = hydra_prefix_attention met an n_acc outside
  * [1, P] or a path entry outside [0, T_src) (clamped), or kv_compact met a path
  * that is not strictly increasing inside [0, T) (the copies stop there),
@@ -326,6 +362,78 @@ int hydra_prefill_chunk(hydra_ctx *ctx, void *stream, int B, void *ws,
 int hydra_prefix_attention(hydra_ctx *ctx, void *stream, int B, void *ws,
                            const float *hidden, int T_src, const int32_t *path, const int32_t *n_acc,
                            int32_t *seq_len, const hydra_kv *kv, float *h_out);
+
+/* ---- the cache in 8 bits ---------------------------------------------------- */
+
+/* tree_verify_forward and hydra_prefill_chunk behind an 8-bit cache: K and V of the nodes go to kv->tail, attention reads the
+ * sealed pages from the codes.  A row whose n_sealed is negative, beyond seq_len / 16 or beyond max_pages is skipped and flagged
+ * (bit 0).  kv_compact takes &kv->tail.  Errors as there, and UNSUPPORTED for HYDRA_F32 contexts. */
+int tree_verify_forward_kv8(hydra_ctx *ctx, void *stream, int B, void *ws,
+                            const int32_t *tree_tokens, const int32_t *seq_len, const hydra_kv8 *kv,
+                            float *hidden, int32_t *argmax, float *margin, float *logits);
+int hydra_prefill_chunk_kv8(hydra_ctx *ctx, void *stream, int B, void *ws,
+                            const int32_t *tree_tokens, const int32_t *seq_len, const hydra_kv8 *kv);
+
+/* The attention of one layer of tree_verify_forward_kv8 on its own, in the 16-bit format of its interior:
+ *   q   device [B, T, H, Dh] IEEE half, already rotated, 16-byte aligned
+ *   out device [B, T, H, Dh] IEEE half, 16-byte aligned
+ * K/V of the T nodes must already be in slots seq_len[b] .. seq_len[b]+T-1 of kv->tail (see hydra_kv_write). */
+int tree_attention_kv8(hydra_ctx *ctx, void *stream, int B, int layer, void *ws,
+                       const void *q, const int32_t *seq_len, const hydra_kv8 *kv, void *out);
+
+/* Seals every page that has become whole: per row and layer, pages n_sealed[b] .. seq_len[b] / 16 - 1 go from kv->tail into
+ * the codes, then n_sealed[b] = seq_len[b] / 16.  Call it behind kv_compact, once per step or prompt chunk, before the next
+ * tree_verify_forward_kv8 writes to the tail again.  A row whose n_sealed is out of range, or for whose pages a table has no
+ * valid entry, keeps its n_sealed and raises flag bit 0 or 6. */
+int hydra_kv8_seal(hydra_ctx *ctx, void *stream, int B, const int32_t *seq_len, const hydra_kv8 *kv);
+
+/* The values that the cache stands for, in plain layout: kv_plain device [B, n_slots, 2, H, Dh] fp32 of one layer, or
+ * [n_layers, B, n_slots, 2, H, Dh] with layer = -1.  Sealed slots come from the codes, others from kv->tail; slots whose
+ * table entry is out of range are left as they are (flag bit 6).  Slots 0 .. 16 * tail.max_pages - 1 can be read. */
+int hydra_kv8_read(hydra_ctx *ctx, void *stream, int B, int layer, const hydra_kv8 *kv, int first_slot, int n_slots, float *kv_plain);
+
+/* ---- pages: take, give back, share, move -------------------------------------- */
+
+/* Workspace bytes (256-byte aligned device memory) of the hydra_pages_* calls for such a pool. */
+size_t hydra_pages_workspace_bytes(int B, int n_pages, int max_pages);
+
+/* Row b gets a page for every logical page lo[b] / 16 .. ceil((hi[b] + extra) / 16) - 1 that it does not hold (lo == NULL: from 0).
+ * Pages are the lowest-numbered free ones, handed out by row, then by logical page.  Rows are served in order and whole:
+ * the first one that the pool has too few pages left for, and every later one that needs any, gets none (flag bit 0), as does a
+ * row with lo < 0, hi + extra < lo or more pages than max_pages.
+ *   lo, hi device [B] int32 (lo may be NULL)   extra host, >= 0   ok device [B] int32 (out) or NULL: 1 = the row has its pages */
+int hydra_pages_reserve(hydra_ctx *ctx, void *stream, int B, void *ws, const hydra_pages *pages,
+                        const int32_t *lo, const int32_t *hi, int extra, int32_t *ok);
+
+/* Row b gives back every page outside logical pages lo[b] / 16 .. ceil(hi[b] / 16) - 1 (lo == NULL: from 0); hi[b] <= lo[b]
+ * frees the row.  A page whose count reaches 0 is free.  A row with lo < 0 or hi < 0 stays as it is (flag bit 0); an entry
+ * outside the pool, or of a page that is free already, is dropped and flagged (bit 6). */
+int hydra_pages_release(hydra_ctx *ctx, void *stream, int B, const hydra_pages *pages, const int32_t *lo, const int32_t *hi);
+
+/* Every row b with src_row[b] not b or -1 becomes a copy of row src_row[b] as that was before the call (all at once, so rows may
+ * change places): its whole pages, those below seq_len[src] / 16, are shared; in place of its incomplete page row b gets a free
+ * page of its own (the lowest-numbered ones, in row order, of those that are free before the call); what lies behind is not
+ * taken over, and what row b held before is given back.  Rows are served in order: the first one that needs a page when none
+ * is left, and every later one that needs one, stays as it is (flag bit 0), as does a row with seq_len[src] < 0 or beyond the table
+ * (bit 0) or src_row outside [-1, B) (bit 2).  Behind it hydra_kv_copy_pages(n = B, copy_src, copy_dst) copies the contents.
+ *   src_row, seq_len device [B] int32 (lengths before the call; not changed)
+ *   copy_src, copy_dst device [B] int32 (out), -1 where nothing is to be copied
+ *   forked device [B] int32 (out): the row whose sequence row b has now */
+int hydra_pages_fork(hydra_ctx *ctx, void *stream, int B, void *ws, const hydra_pages *pages, const int32_t *src_row,
+                     const int32_t *seq_len, int32_t *copy_src, int32_t *copy_dst, int32_t *forked);
+
+/* Moves the pages in use (U of them) to pages 0 .. U - 1: the k-th lowest page in use at or behind U goes to the k-th lowest free
+ * page below U; page tables and counts follow.  Behind it hydra_kv_copy_pages(n = n_pages, move_src, move_dst, counts).
+ * Entries of the tables outside the pool are left as they are and flagged (bit 6).
+ *   move_src, move_dst device [n_pages] int32 (out), -1 behind the last move
+ *   counts device [2] int32 (out): number of moves, U */
+int hydra_pages_compact(hydra_ctx *ctx, void *stream, int B, void *ws, const hydra_pages *pages, int32_t *move_src, int32_t *move_dst, int32_t *counts);
+
+/* Copies whole pages of every layer, K and V: src[i] -> dst[i] for i < n, or i < *count where that is less (count: device, or NULL).
+ * An entry with a negative page is skipped; one outside the cache is skipped and flagged (bit 6).  No page may be a
+ * destination twice, or a destination and a source.  Of kv only the pages and n_pages are used. */
+int hydra_kv_copy_pages(hydra_ctx *ctx, void *stream, const hydra_kv *kv, int n, const int32_t *src, const int32_t *dst, const int32_t *count);
+int hydra_kv8_copy_pages(hydra_ctx *ctx, void *stream, const hydra_kv8 *kv, int n, const int32_t *src, const int32_t *dst, const int32_t *count);
 
 /* ---- helpers for tests and harnesses -------------------------------------- */
 

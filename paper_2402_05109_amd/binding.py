@@ -16,6 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libhydra.so")
 
 HYDRA_F32, HYDRA_BF16 = 0, 1
+KV8_INT8, KV8_E4M3 = 0, 1
 HYDRA_OK = 0
 E_INVALID_ARG, E_SHAPE, E_CAPACITY, E_UNSUPPORTED, E_HIP, E_STATE = -1, -2, -3, -4, -5, -6
 
@@ -25,7 +26,9 @@ E_INVALID_ARG, E_SHAPE, E_CAPACITY, E_UNSUPPORTED, E_HIP, E_STATE = -1, -2, -3, 
 EXPORTS = ["hydra_create", "hydra_destroy", "hydra_last_error", "hydra_weights_bytes", "hydra_bind_weights",
            "hydra_load_tensor", "hydra_workspace_bytes", "hydra_read_flags", "hydra_draft_tree",
            "tree_verify_forward", "tree_attention", "accept_greedy", "accept_typical", "accept_typical_static", "kv_compact", "hydra_prefill_chunk", "hydra_prefix_attention", "hydra_tree_depth",
-           "hydra_kv_write", "hydra_kv_read", "hydra_profile_begin", "hydra_profile_end", "hydra_layer_kernel_info"]
+           "hydra_kv_write", "hydra_kv_read", "hydra_profile_begin", "hydra_profile_end", "hydra_layer_kernel_info",
+           "tree_verify_forward_kv8", "hydra_prefill_chunk_kv8", "tree_attention_kv8", "hydra_kv8_seal", "hydra_kv8_read", "hydra_pages_workspace_bytes",
+           "hydra_pages_reserve", "hydra_pages_release", "hydra_pages_fork", "hydra_pages_compact", "hydra_kv_copy_pages", "hydra_kv8_copy_pages"]
 
 
 class ModelDesc(C.Structure):
@@ -46,6 +49,15 @@ class TreeDesc(C.Structure):
 class KVDesc(C.Structure):
     _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_table", C.c_void_p),
                 ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("seq_len_hint", C.c_int32)]
+
+
+class KV8Desc(C.Structure):
+    _fields_ = [("tail", KVDesc), ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("scales", C.c_void_p), ("page_table", C.c_void_p),
+                ("n_sealed", C.c_void_p), ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("format", C.c_int32)]
+
+
+class PagesDesc(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("ref", C.c_void_p), ("n_pages", C.c_int32), ("max_pages", C.c_int32)]
 
 
 class HydraError(RuntimeError):
@@ -83,6 +95,19 @@ def _load() -> C.CDLL:
     lib.hydra_profile_begin.argtypes = [vp]
     lib.hydra_layer_kernel_info.argtypes = [vp, i32, C.POINTER(C.c_int64)]
     lib.hydra_profile_end.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_double), C.POINTER(C.c_double)]
+    kv8, pg = C.POINTER(KV8Desc), C.POINTER(PagesDesc)
+    lib.tree_verify_forward_kv8.argtypes = [vp, vp, i32, vp, vp, vp, kv8, vp, vp, vp, vp]
+    lib.hydra_prefill_chunk_kv8.argtypes = [vp, vp, i32, vp, vp, vp, kv8]
+    lib.tree_attention_kv8.argtypes = [vp, vp, i32, i32, vp, vp, vp, kv8, vp]
+    lib.hydra_kv8_seal.argtypes = [vp, vp, i32, vp, kv8]
+    lib.hydra_kv8_read.argtypes = [vp, vp, i32, i32, kv8, i32, i32, vp]
+    lib.hydra_pages_workspace_bytes.argtypes = [i32, i32, i32]; lib.hydra_pages_workspace_bytes.restype = sz
+    lib.hydra_pages_reserve.argtypes = [vp, vp, i32, vp, pg, vp, vp, i32, vp]
+    lib.hydra_pages_release.argtypes = [vp, vp, i32, pg, vp, vp]
+    lib.hydra_pages_fork.argtypes = [vp, vp, i32, vp, pg, vp, vp, vp, vp, vp]
+    lib.hydra_pages_compact.argtypes = [vp, vp, i32, vp, pg, vp, vp, vp]
+    lib.hydra_kv_copy_pages.argtypes = [vp, vp, C.POINTER(KVDesc), i32, vp, vp, vp]
+    lib.hydra_kv8_copy_pages.argtypes = [vp, vp, kv8, i32, vp, vp, vp]
     return lib
 
 
@@ -127,6 +152,36 @@ class KV:
     def desc(self) -> KVDesc:
         return KVDesc(self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.page_table.data_ptr(),
                       self.n_pages, self.max_pages, self.seq_len_hint)
+
+
+class KV8:
+    """Caller-owned paged KV cache in 8 bits with its 16-bit tail (see hydra_kv8 in the header)."""
+
+    def __init__(self, tail: KV, k_codes: torch.Tensor, v_codes: torch.Tensor, scales: torch.Tensor, page_table: torch.Tensor, n_sealed: torch.Tensor,
+                 n_pages: int, fmt: int):
+        _ptr(page_table, torch.int32, "page_table"), _ptr(n_sealed, torch.int32, "n_sealed"), _ptr(scales, torch.float32, "scales")
+        self.tail, self.k_codes, self.v_codes, self.scales = tail, k_codes, v_codes, scales
+        self.page_table, self.n_sealed = page_table, n_sealed
+        self.n_pages, self.max_pages, self.format = int(n_pages), int(page_table.shape[-1]), int(fmt)
+
+    def desc(self) -> KV8Desc:
+        return KV8Desc(self.tail.desc(), self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.scales.data_ptr(), self.page_table.data_ptr(),
+                       self.n_sealed.data_ptr(), self.n_pages, self.max_pages, self.format)
+
+
+class Pages:
+    """Caller-owned page tables [B, max_pages] and counts [n_pages] of a pool of pages (see hydra_pages in the header)."""
+
+    def __init__(self, page_table: torch.Tensor, ref: torch.Tensor):
+        _ptr(page_table, torch.int32, "page_table"), _ptr(ref, torch.int32, "ref")
+        self.page_table, self.ref = page_table, ref
+
+    def desc(self) -> PagesDesc:
+        return PagesDesc(self.page_table.data_ptr(), self.ref.data_ptr(), self.ref.numel(), self.page_table.shape[-1])
+
+
+def pages_workspace_bytes(B: int, n_pages: int, max_pages: int) -> int:
+    return _lib.hydra_pages_workspace_bytes(int(B), int(n_pages), int(max_pages))
 
 
 class Hydra:
@@ -233,6 +288,62 @@ class Hydra:
                                            _ptr(hidden, torch.float32, "hidden"), T_src, _ptr(path, torch.int32, "path"),
                                            _ptr(n_acc, torch.int32, "n_acc"), _ptr(seq_len, torch.int32, "seq_len"),
                                            C.byref(d), _ptr(h_out, torch.float32, "h_out")))
+
+    # ---- the cache in 8 bits
+    def tree_verify_forward_kv8(self, B, ws, tree_tokens, seq_len, kv: KV8, hidden, argmax, margin=None, logits=None) -> None:
+        d = kv.desc()
+        _check(_lib.tree_verify_forward_kv8(self._h, _stream(), B, _ptr(ws, torch.uint8, "ws"), _ptr(tree_tokens, torch.int32, "tree_tokens"),
+                                            _ptr(seq_len, torch.int32, "seq_len"), C.byref(d), _ptr(hidden, torch.float32, "hidden"),
+                                            _ptr(argmax, torch.int32, "argmax"), _ptr(margin, torch.float32, "margin"), _ptr(logits, torch.float32, "logits")))
+
+    def hydra_prefill_chunk_kv8(self, B, ws, tree_tokens, seq_len, kv: KV8) -> None:
+        d = kv.desc()
+        _check(_lib.hydra_prefill_chunk_kv8(self._h, _stream(), B, _ptr(ws, torch.uint8, "ws"), _ptr(tree_tokens, torch.int32, "tree_tokens"),
+                                            _ptr(seq_len, torch.int32, "seq_len"), C.byref(d)))
+
+    def tree_attention_kv8(self, B, layer, ws, q, seq_len, kv: KV8, out) -> None:
+        d = kv.desc()
+        _check(_lib.tree_attention_kv8(self._h, _stream(), B, layer, _ptr(ws, torch.uint8, "ws"), _ptr(q, torch.float16, "q"),
+                                       _ptr(seq_len, torch.int32, "seq_len"), C.byref(d), _ptr(out, torch.float16, "out")))
+
+    def hydra_kv8_seal(self, B, seq_len, kv: KV8) -> None:
+        d = kv.desc()
+        _check(_lib.hydra_kv8_seal(self._h, _stream(), B, _ptr(seq_len, torch.int32, "seq_len"), C.byref(d)))
+
+    def kv8_read(self, B, layer, kv: KV8, first_slot, n_slots, plain) -> None:
+        d = kv.desc()
+        _check(_lib.hydra_kv8_read(self._h, _stream(), B, layer, C.byref(d), first_slot, n_slots, _ptr(plain, torch.float32, "kv_plain")))
+
+    # ---- pages
+    def hydra_pages_reserve(self, B, ws, pages: Pages, lo, hi, extra, ok=None) -> None:
+        d = pages.desc()
+        _check(_lib.hydra_pages_reserve(self._h, _stream(), B, _ptr(ws, torch.uint8, "ws"), C.byref(d), _ptr(lo, torch.int32, "lo"), _ptr(hi, torch.int32, "hi"),
+                                        int(extra), _ptr(ok, torch.int32, "ok")))
+
+    def hydra_pages_release(self, B, pages: Pages, lo, hi) -> None:
+        d = pages.desc()
+        _check(_lib.hydra_pages_release(self._h, _stream(), B, C.byref(d), _ptr(lo, torch.int32, "lo"), _ptr(hi, torch.int32, "hi")))
+
+    def hydra_pages_fork(self, B, ws, pages: Pages, src_row, seq_len, copy_src, copy_dst, forked) -> None:
+        d = pages.desc()
+        _check(_lib.hydra_pages_fork(self._h, _stream(), B, _ptr(ws, torch.uint8, "ws"), C.byref(d), _ptr(src_row, torch.int32, "src_row"),
+                                     _ptr(seq_len, torch.int32, "seq_len"), _ptr(copy_src, torch.int32, "copy_src"),
+                                     _ptr(copy_dst, torch.int32, "copy_dst"), _ptr(forked, torch.int32, "forked")))
+
+    def hydra_pages_compact(self, B, ws, pages: Pages, move_src, move_dst, counts) -> None:
+        d = pages.desc()
+        _check(_lib.hydra_pages_compact(self._h, _stream(), B, _ptr(ws, torch.uint8, "ws"), C.byref(d), _ptr(move_src, torch.int32, "move_src"),
+                                        _ptr(move_dst, torch.int32, "move_dst"), _ptr(counts, torch.int32, "counts")))
+
+    def hydra_kv_copy_pages(self, kv: KV, n, src, dst, count=None) -> None:
+        d = kv.desc()
+        _check(_lib.hydra_kv_copy_pages(self._h, _stream(), C.byref(d), int(n), _ptr(src, torch.int32, "src"), _ptr(dst, torch.int32, "dst"),
+                                        _ptr(count, torch.int32, "count")))
+
+    def hydra_kv8_copy_pages(self, kv: KV8, n, src, dst, count=None) -> None:
+        d = kv.desc()
+        _check(_lib.hydra_kv8_copy_pages(self._h, _stream(), C.byref(d), int(n), _ptr(src, torch.int32, "src"), _ptr(dst, torch.int32, "dst"),
+                                         _ptr(count, torch.int32, "count")))
 
     # ---- harness helpers
     def kv_write(self, B, layer, kv: KV, first_slot, n_slots, plain) -> None:

@@ -150,7 +150,7 @@ WsLayout ws_layout(const hydra_ctx *c, int B) {
     return w;
 }
 
-static int check_common(hydra_ctx *c, int B, const void *ws) {
+int check_common(hydra_ctx *c, int B, const void *ws) {
     if (!c) return fail(HYDRA_E_INVALID_ARG, "ctx is NULL");
     if (B < 1 || B > c->max_batch) return fail(HYDRA_E_CAPACITY, "B outside [1, max_batch]");
     if (!ws) return fail(HYDRA_E_INVALID_ARG, "workspace is NULL");
@@ -159,7 +159,7 @@ static int check_common(hydra_ctx *c, int B, const void *ws) {
     return HYDRA_OK;
 }
 
-static int check_kv(hydra_ctx *c, const hydra_kv *kv) {
+int check_kv(hydra_ctx *c, const hydra_kv *kv) {
     if (!kv || !kv->k_pages || !kv->v_pages || !kv->page_table) return fail(HYDRA_E_INVALID_ARG, "kv or one of its pointers is NULL");
     if (kv->n_pages < 1 || kv->max_pages < 1) return fail(HYDRA_E_INVALID_ARG, "kv: n_pages and max_pages must be positive");
     if (kv->seq_len_hint < 0) return fail(HYDRA_E_INVALID_ARG, "kv: seq_len_hint is negative");
@@ -167,6 +167,20 @@ static int check_kv(hydra_ctx *c, const hydra_kv *kv) {
         return fail(HYDRA_E_CAPACITY, "kv: page table shorter than seq_len_hint + T slots");
     if (kv->seq_len_hint > 0 && kv->seq_len_hint + c->tree.max_depth >= c->m.max_pos)
         return fail(HYDRA_E_CAPACITY, "kv: seq_len_hint + tree depth reaches max_pos");
+    return HYDRA_OK;
+}
+
+static int check_kv8(hydra_ctx *c, const hydra_kv8 *kv) {
+    if (!kv) return fail(HYDRA_E_INVALID_ARG, "kv is NULL");
+    if (!c->bf16) return fail(HYDRA_E_UNSUPPORTED, "the 8-bit cache is for HYDRA_BF16 contexts");
+    int rc = check_kv(c, &kv->tail);
+    if (rc) return rc;
+    if (!kv->k_codes || !kv->v_codes || !kv->scales || !kv->page_table || !kv->n_sealed) return fail(HYDRA_E_INVALID_ARG, "kv8: one of its pointers is NULL");
+    if (kv->n_pages < 1 || kv->max_pages < 1) return fail(HYDRA_E_INVALID_ARG, "kv8: n_pages and max_pages must be positive");
+    if (kv->format != HYDRA_KV8_INT8 && kv->format != HYDRA_KV8_E4M3) return fail(HYDRA_E_INVALID_ARG, "kv8: unknown format");
+    if (((uintptr_t)kv->k_codes | (uintptr_t)kv->v_codes | (uintptr_t)kv->tail.k_pages | (uintptr_t)kv->tail.v_pages) & 15)
+        return fail(HYDRA_E_INVALID_ARG, "kv8: codes and tail pages must be 16-byte aligned");
+    if ((uintptr_t)kv->scales & 7) return fail(HYDRA_E_INVALID_ARG, "kv8: scales must be 8-byte aligned");
     return HYDRA_OK;
 }
 
@@ -274,6 +288,7 @@ int hydra_bind_weights(hydra_ctx *c, void *stream, void *arena, int table_slot) 
         if (rc) return rc;
         if ((rc = attn_max_dynamic_lds(c))) return rc;
         if ((rc = layers_mega_set_attr(c))) return rc;
+        if ((rc = kv8_max_dynamic_lds())) return rc;
     }
     return HYDRA_OK;
 }
@@ -462,8 +477,9 @@ static int lm_head_tail(hydra_ctx *c, hipStream_t s, const float *x, const void 
 // The decoder layers of the context over its B * T tree rows.  lm_tail: final RMSNorm, LM head, argmax (the
 // verify step); otherwise the residual stream after the last layer is left in the workspace's x, unless the rows are tokens: those
 // take the same kernels with and without the tail, also the persistent layer kernel, which has a buffer of its own for it.
+// kv8 (16-bit family): the cache whose tail `kv` is; attention then reads its sealed pages.
 static int forward_layers(hydra_ctx *c, hipStream_t s, int B, void *ws, const RowSource &src, const int32_t *seq_len,
-                          const hydra_kv *kv, bool lm_tail, float *hidden, int32_t *argmax, float *margin, float *logits) {
+                          const hydra_kv *kv, const hydra_kv8 *kv8, bool lm_tail, float *hidden, int32_t *argmax, float *margin, float *logits) {
     int rc;
     const WsLayout w = ws_layout(c, B);
     char *W = (char *)ws, *A = c->arena;
@@ -478,7 +494,7 @@ static int forward_layers(hydra_ctx *c, hipStream_t s, int B, void *ws, const Ro
         const int Mpad = (int)align_up(std::max<size_t>(M, 1), 128);
         RowScale rs = {ss, 1, Mpad, d, c->m.rms_eps};        // rs.nb: rows of ss the last producer filled (1 = a complete sum per row)
         const float *gain0 = (const float *)(A + c->layer[0].attn_norm);
-        if (src.tokens && layers_mega_eligible(c, B, kv)) {
+        if (src.tokens && !kv8 && layers_mega_eligible(c, B, kv)) {
             // up to 64 rows and a bounded context: all layers in one persistent kernel (bf16_layers.hip)
             LayersMegaIO io;
             if ((rc = launch_layers_mega(c, s, B, W + w.mega, seq_len, kv, flags, &io, false))) return rc;
@@ -493,8 +509,9 @@ static int forward_layers(hydra_ctx *c, hipStream_t s, int B, void *ws, const Ro
         for (int l = 0; l < c->m.n_layers; ++l) {
             const LayerOff &o = c->layer[l];
             const float *next_gain = (const float *)(A + (l + 1 < c->m.n_layers ? c->layer[l + 1].attn_norm : c->off_final_norm));
-            if ((rc = launch_gemm_qkv_rope(c, s, xa, A + o.wqkv, M, rs, l, seq_len, kv, qbuf, part, flags))) return rc;
-            if ((rc = launch_attention(c, s, B, l, qbuf, seq_len, kv, apart, w.attn_units, xb, nullptr, flags))) return rc;
+            if ((rc = launch_gemm_qkv_rope(c, s, xa, A + o.wqkv, M, rs, l, seq_len, kv, qbuf, part, flags, !kv8))) return rc;
+            if (kv8) { if ((rc = launch_kv8_attention(c, s, B, l, qbuf, false, seq_len, kv8, apart, w.attn_units, xb, false, flags))) return rc; }
+            else     { if ((rc = launch_attention(c, s, B, l, qbuf, seq_len, kv, apart, w.attn_units, xb, nullptr, flags))) return rc; }
             if ((rc = launch_gemm_resid(c, s, xb, A + o.wo, M, d, d, x, (const float *)(A + o.ffn_norm), xa, ss, Mpad, part, &rs.nb))) return rc;
             if ((rc = launch_gemm_silu(c, s, xa, A + o.wgu, M, F, d, ss, rs.nb, Mpad, xb))) return rc;
             if ((rc = launch_gemm_resid(c, s, xb, A + o.wdown, M, d, F, x, next_gain, xa, ss, Mpad, part, &rs.nb))) return rc;
@@ -534,7 +551,7 @@ int tree_verify_forward(hydra_ctx *c, void *stream, int B, void *ws, const int32
     if (!tree_tokens || !seq_len || !hidden || !argmax) return fail(HYDRA_E_INVALID_ARG, "tree_verify_forward: NULL argument");
     if ((rc = check_kv(c, kv))) return rc;
     const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
-    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, kv, true, hidden, argmax, margin, logits);
+    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, kv, nullptr, true, hidden, argmax, margin, logits);
 }
 
 int hydra_prefill_chunk(hydra_ctx *c, void *stream, int B, void *ws, const int32_t *tree_tokens, const int32_t *seq_len, const hydra_kv *kv) {
@@ -543,7 +560,63 @@ int hydra_prefill_chunk(hydra_ctx *c, void *stream, int B, void *ws, const int32
     if (!tree_tokens || !seq_len) return fail(HYDRA_E_INVALID_ARG, "hydra_prefill_chunk: NULL argument");
     if ((rc = check_kv(c, kv))) return rc;
     const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
-    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, kv, false, nullptr, nullptr, nullptr, nullptr);
+    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, kv, nullptr, false, nullptr, nullptr, nullptr, nullptr);
+}
+
+// ---------------------------------------------------------------------------
+// the cache in 8 bits
+// ---------------------------------------------------------------------------
+int tree_verify_forward_kv8(hydra_ctx *c, void *stream, int B, void *ws, const int32_t *tree_tokens, const int32_t *seq_len, const hydra_kv8 *kv,
+                            float *hidden, int32_t *argmax, float *margin, float *logits) {
+    int rc = check_common(c, B, ws);
+    if (rc) return rc;
+    if (!tree_tokens || !seq_len || !hidden || !argmax) return fail(HYDRA_E_INVALID_ARG, "tree_verify_forward_kv8: NULL argument");
+    if ((rc = check_kv8(c, kv))) return rc;
+    const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
+    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, &kv->tail, kv, true, hidden, argmax, margin, logits);
+}
+
+int hydra_prefill_chunk_kv8(hydra_ctx *c, void *stream, int B, void *ws, const int32_t *tree_tokens, const int32_t *seq_len, const hydra_kv8 *kv) {
+    int rc = check_common(c, B, ws);
+    if (rc) return rc;
+    if (!tree_tokens || !seq_len) return fail(HYDRA_E_INVALID_ARG, "hydra_prefill_chunk_kv8: NULL argument");
+    if ((rc = check_kv8(c, kv))) return rc;
+    const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
+    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, &kv->tail, kv, false, nullptr, nullptr, nullptr, nullptr);
+}
+
+int tree_attention_kv8(hydra_ctx *c, void *stream, int B, int layer, void *ws, const void *q, const int32_t *seq_len, const hydra_kv8 *kv, void *out) {
+    int rc = check_common(c, B, ws);
+    if (rc) return rc;
+    if (!q || !seq_len || !out) return fail(HYDRA_E_INVALID_ARG, "tree_attention_kv8: NULL argument");
+    if (((uintptr_t)q | (uintptr_t)out) & 15) return fail(HYDRA_E_INVALID_ARG, "tree_attention_kv8: q and out must be 16-byte aligned");
+    if (layer < 0 || layer >= c->m.n_layers) return fail(HYDRA_E_INVALID_ARG, "layer out of range");
+    if ((rc = check_kv8(c, kv))) return rc;
+    const WsLayout w = ws_layout(c, B);
+    return launch_kv8_attention(c, (hipStream_t)stream, B, layer, q, true, seq_len, kv, (float *)((char *)ws + w.apart), w.attn_units, out, true, flags_ptr(c));
+}
+
+int hydra_kv8_seal(hydra_ctx *c, void *stream, int B, const int32_t *seq_len, const hydra_kv8 *kv) {
+    if (!c || !seq_len) return fail(HYDRA_E_INVALID_ARG, "hydra_kv8_seal: NULL argument");
+    if (B < 1 || B > c->max_batch) return fail(HYDRA_E_CAPACITY, "B outside [1, max_batch]");
+    if (!c->arena) return fail(HYDRA_E_STATE, "no weight arena bound");
+    int rc = check_kv8(c, kv);
+    if (rc) return rc;
+    return launch_kv8_seal(c, (hipStream_t)stream, B, seq_len, kv);
+}
+
+int hydra_kv8_read(hydra_ctx *c, void *stream, int B, int layer, const hydra_kv8 *kv, int first_slot, int n_slots, float *kv_plain) {
+    if (!c || !kv_plain) return fail(HYDRA_E_INVALID_ARG, "hydra_kv8_read: NULL argument");
+    if (B < 1 || B > c->max_batch) return fail(HYDRA_E_CAPACITY, "B outside [1, max_batch]");
+    if (!c->arena) return fail(HYDRA_E_STATE, "no weight arena bound");
+    if (layer < -1 || layer >= c->m.n_layers) return fail(HYDRA_E_INVALID_ARG, "layer out of range");
+    if ((uintptr_t)kv_plain & 15) return fail(HYDRA_E_INVALID_ARG, "hydra_kv8_read: kv_plain must be 16-byte aligned");
+    int rc = check_kv8(c, kv);
+    if (rc) return rc;
+    if (first_slot < 0 || n_slots < 0 || (int64_t)first_slot + n_slots > (int64_t)kv->tail.max_pages * HYDRA_PAGE)
+        return fail(HYDRA_E_CAPACITY, "slots outside the page table");
+    if (n_slots == 0) return HYDRA_OK;
+    return launch_kv8_read(c, (hipStream_t)stream, B, layer, kv, first_slot, n_slots, kv_plain);
 }
 
 // ---------------------------------------------------------------------------
@@ -561,7 +634,7 @@ int hydra_prefix_attention(hydra_ctx *c, void *stream, int B, void *ws, const fl
     if ((rc = check_kv(c, kv))) return rc;
     hipStream_t s = (hipStream_t)stream;
     const RowSource src = {nullptr, hidden, T_src, path, n_acc};
-    if ((rc = forward_layers(c, s, B, ws, src, seq_len, kv, false, nullptr, nullptr, nullptr, nullptr))) return rc;
+    if ((rc = forward_layers(c, s, B, ws, src, seq_len, kv, nullptr, false, nullptr, nullptr, nullptr, nullptr))) return rc;
     const WsLayout w = ws_layout(c, B);
     return launch_prefix_select(c, s, B, (const float *)((char *)ws + w.x), n_acc, kv, seq_len, h_out);
 }

@@ -365,7 +365,7 @@ int launch_gemm_bias_silu(hydra_ctx *c, hipStream_t s, const void *X, const void
 
 // q|k|v projection, rotary embedding and cache append in one kernel (bf16 family)
 int launch_gemm_qkv_rope(hydra_ctx *c, hipStream_t s, const void *X, const void *W, int M, RowScale rs, int layer,
-                         const int32_t *seq_len, const hydra_kv *kv, void *qbuf, float *part, int32_t *flags) {
+                         const int32_t *seq_len, const hydra_kv *kv, void *qbuf, float *part, int32_t *flags, bool touch) {
     {
         // Beyond 64 rows: plain sums from the tile kernel, then rotary embedding and cache append as a kernel of their own,
         // where the estimates say so (HYDRA_PLAN_QKV_UNFUSED: 0 never, 1 always).  7B shape: 96 rows 39.8 us for the fused
@@ -395,7 +395,7 @@ int launch_gemm_qkv_rope(hydra_ctx *c, hipStream_t s, const void *X, const void 
     // costs more than attention gains, verify 6.35 -> 6.52 ms)
     const int wgs = ceil_div(ceil_div(ceil_div(3 * d, 32), p.nt), p.nw);
     const int idle = std::min(64, 256 - wgs);
-    const int extra = (idle >= 32 && env_or("HYDRA_KV_TOUCH", 1.0) != 0.0) ? idle : 0;
+    const int extra = (touch && idle >= 32 && env_or("HYDRA_KV_TOUCH", 1.0) != 0.0) ? idle : 0;
     return launch_bf16<EpiQkvRope, NT_TWO>(c, s, X, W, M, 3 * d, d, p, epi, extra);
 }
 

@@ -127,8 +127,9 @@ int gemm_tile_max_dynamic_lds();
 int attn_max_dynamic_lds(hydra_ctx *c);
 // per-row 1/rms from the per-band sums of squares ss[band][Mpad] (bf16 family); ss == NULL: no scaling
 struct RowScale { const float *ss; int nb; int Mpad; int d; float eps; };
+// touch: spare workgroups may read the layer's cached pages ahead of attention (not where the cache is held in 8 bits)
 int launch_gemm_qkv_rope(hydra_ctx *c, hipStream_t s, const void *X, const void *W, int M, RowScale rs, int layer,
-                         const int32_t *seq_len, const hydra_kv *kv, void *qbuf, float *part, int32_t *flags);
+                         const int32_t *seq_len, const hydra_kv *kv, void *qbuf, float *part, int32_t *flags, bool touch);
 int launch_embed_prep(hydra_ctx *c, hipStream_t s, const int32_t *tokens, float *x, const float *gain, void *xg,
                       float *ss, int Mpad, int M, int32_t *flags);
 int launch_final_hidden(hydra_ctx *c, hipStream_t s, const float *x, const float *gain, RowScale rs, float *hidden, int M);
@@ -199,6 +200,17 @@ int typical_static_scratch(int32_t **out);       // the current device's copy of
 int launch_compact(hydra_ctx *c, hipStream_t s, int B, const int32_t *n_acc, const int32_t *path,
                    const int32_t *next_root, const int32_t *last_node, const float *hidden, const hydra_kv *kv,
                    int32_t *seq_len, float *h_last, int32_t *root, int32_t *kv_index);
+
+// 8-bit cache (kv8_cache.hip, kv8_attn.hip).  q_plain / out_plain: half [B, T, H, Dh]; otherwise qbuf and the next GEMM's input
+int launch_kv8_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const void *q, bool q_plain, const int32_t *seq_len, const hydra_kv8 *kv,
+                         float *apart, int units_max, void *out, bool out_plain, int32_t *flags);
+int kv8_max_dynamic_lds();
+int launch_kv8_seal(hydra_ctx *c, hipStream_t s, int B, const int32_t *seq_len, const hydra_kv8 *kv);
+int launch_kv8_read(hydra_ctx *c, hipStream_t s, int B, int layer, const hydra_kv8 *kv, int first_slot, int n_slots, float *plain);
+
+// checks of arguments shared by the entry points (api.hip)
+int check_common(hydra_ctx *c, int B, const void *ws);
+int check_kv(hydra_ctx *c, const hydra_kv *kv);
 
 inline const TreeDev *tree_dev(const hydra_ctx *c) {
     return reinterpret_cast<const TreeDev *>(c->arena + c->off_tables + (size_t)c->table_slot * TABLE_SLOT_BYTES);

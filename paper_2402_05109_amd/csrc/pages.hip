@@ -1,0 +1,428 @@
+// The pages of a cache as a pool: rows take pages, give them back, share them and move them; copies of whole pages.
+//
+// The tables and counts are small integers in device memory, so that no call waits for the host and all of them can be captured
+// into a graph.  Every result is a function of the inputs alone: pages are handed out lowest first, by row, and counts are sums.
+#include <algorithm>
+
+#include "device_common.h"
+#include "internal.h"
+
+namespace hydra {
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+
+enum { PG_THREADS = 1024, PG_WAVES = PG_THREADS / 64 };
+
+// Exclusive sum of v over the workgroup's threads, and the total.  `part`: PG_WAVES ints of shared memory; two barriers.
+__device__ __forceinline__ int block_scan(int v, int *part, int &total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    __syncthreads();                                        // `part` may still be read from the call before
+    if (lane == 63) part[wave] = x;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+    for (int w = 0; w < PG_WAVES; ++w) {
+        const int p = part[w];
+        if (w < wave) before += p;
+        total += p;
+    }
+    return before + x - v;
+}
+
+// The `want` lowest free pages into list[]; returns how many there are (at most want).  Uniform over the workgroup.
+__device__ __forceinline__ int lowest_free(const int32_t *ref, int n_pages, int want, int32_t *list, int *part) {
+    int found = 0;
+    for (int p0 = 0; p0 < n_pages && found < want; p0 += PG_THREADS * 4) {
+        const int p = p0 + (int)threadIdx.x * 4;
+        int free_n = 0, is[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { is[e] = p + e < n_pages && ref[p + e] == 0; free_n += is[e]; }
+        int total;
+        int at = found + block_scan(free_n, part, total);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (is[e]) { if (at < want) list[at] = p + e; ++at; }
+        found += total;
+    }
+    return min(found, want);
+}
+
+struct PgRange { int first, last; bool ok; };
+// logical pages [lo / 16, ceil(hi / 16)) of a row that is to hold slots lo .. hi - 1
+__device__ __forceinline__ PgRange page_range(const int32_t *lo, const int32_t *hi, int extra, int b) {
+    const int64_t a = lo ? lo[b] : 0, e = (int64_t)hi[b] + extra;
+    PgRange r;
+    r.ok = a >= 0 && hi[b] >= 0;
+    r.first = (int)(a >> 4);
+    r.last = (int)min((e + 15) >> 4, (int64_t)0x7fffffff);
+    return r;
+}
+
+// ws: need[B], then the pages handed out (at most n_pages)
+__global__ __launch_bounds__(PG_THREADS) void pages_reserve_kernel(int32_t *table, int32_t *ref, int n_pages, int max_pages, int B, const int32_t *lo,
+                                                                    const int32_t *hi, int extra, int32_t *ws, int32_t *ok, int32_t *flags) {
+    __shared__ int part[PG_WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int32_t *start = ws, *list = ws + B;
+    // what each row lacks; -1: its range is not one
+    for (int b = wave; b < B; b += PG_WAVES) {
+        const PgRange r = page_range(lo, hi, extra, b);
+        const bool good = r.ok && (int64_t)(lo ? lo[b] : 0) <= (int64_t)hi[b] + extra && r.last <= max_pages;
+        int need = 0;
+        if (good)
+            for (int i = r.first + lane; i < r.last; i += 64) need += table[(size_t)b * max_pages + i] < 0;
+#pragma unroll
+        for (int d = 32; d; d >>= 1) need += __shfl_xor(need, d);
+        if (lane == 0) start[b] = good ? need : -1;
+    }
+    __syncthreads();
+    // where its pages begin among all that are handed out
+    int all = 0;
+    for (int b0 = 0; b0 < B; b0 += PG_THREADS) {
+        const int b = b0 + (int)threadIdx.x;
+        const int need = b < B ? start[b] : 0;
+        int total;
+        const int at = block_scan(max(need, 0), part, total) + all;
+        if (b < B) start[b] = need < 0 ? -1 : at;
+        all = min(all + total, 0x3fffffff);
+    }
+    const int found = lowest_free(ref, n_pages, min(all, n_pages), list, part);
+    __syncthreads();
+    for (int b = wave; b < B; b += PG_WAVES) {
+        const int at0 = start[b];
+        const PgRange r = page_range(lo, hi, extra, b);
+        bool served = at0 >= 0;
+        if (served) {
+            int need = 0;
+            for (int i = r.first + lane; i < r.last; i += 64) need += table[(size_t)b * max_pages + i] < 0;
+#pragma unroll
+            for (int d = 32; d; d >>= 1) need += __shfl_xor(need, d);
+            served = need == 0 || at0 + need <= found;
+            int at = at0;
+            if (served && need)
+                for (int i0 = r.first; i0 < r.last; i0 += 64) {
+                    const int i = i0 + lane;
+                    const bool lacks = i < r.last && table[(size_t)b * max_pages + i] < 0;
+                    const uint64_t m = __ballot(lacks);
+                    if (lacks) {
+                        const int page = list[at + __popcll(m & ((1ull << lane) - 1ull))];
+                        table[(size_t)b * max_pages + i] = page;
+                        ref[page] = 1;
+                    }
+                    at += __popcll(m);
+                }
+        }
+        if (lane == 0) {
+            if (!served) atomicOr(flags, FLAG_CAPACITY);
+            if (ok) ok[b] = served ? 1 : 0;
+        }
+    }
+}
+
+// an entry gives its page back
+__device__ __forceinline__ void drop_page(int32_t *ref, int n_pages, int page, int32_t *flags) {
+    if ((unsigned)page >= (unsigned)n_pages) { atomicOr(flags, FLAG_BAD_PAGE); return; }
+    if (atomicSub(&ref[page], 1) <= 0) {                    // was free already: stays free
+        atomicAdd(&ref[page], 1);
+        atomicOr(flags, FLAG_BAD_PAGE);
+    }
+}
+
+__global__ __launch_bounds__(256) void pages_release_kernel(int32_t *table, int32_t *ref, int n_pages, int max_pages, const int32_t *lo, const int32_t *hi,
+                                                             int32_t *flags) {
+    const int b = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
+    PgRange r = page_range(lo, hi, 0, b);
+    if (!r.ok) {
+        if (i == 0) atomicOr(flags, FLAG_CAPACITY);
+        return;
+    }
+    if ((lo ? lo[b] : 0) >= hi[b]) r.last = 0;              // the row is freed
+    if (i >= max_pages || (i >= r.first && i < r.last)) return;
+    const int page = table[(size_t)b * max_pages + i];
+    if (page < 0) return;
+    table[(size_t)b * max_pages + i] = -1;
+    drop_page(ref, n_pages, page, flags);
+}
+
+// Which row every row becomes a copy of, and the fresh pages (block 0); meanwhile the others copy the tables into the workspace.
+// ws: fresh page of each row [B] (-1: none), list [B], tables [B, max_pages]
+__global__ __launch_bounds__(PG_THREADS) void pages_fork_plan_kernel(const int32_t *table, const int32_t *ref, int n_pages, int max_pages, int B,
+                                                                      const int32_t *src_row, const int32_t *seq_len, int32_t *ws, int32_t *copy_src,
+                                                                      int32_t *copy_dst, int32_t *forked, int32_t *flags) {
+    if (blockIdx.x > 0) {
+        int32_t *old = ws + 2 * (size_t)B;
+        const size_t n = (size_t)B * max_pages, step = (size_t)(gridDim.x - 1) * PG_THREADS;
+        for (size_t i = (size_t)(blockIdx.x - 1) * PG_THREADS + threadIdx.x; i < n; i += step) old[i] = table[i];
+        return;
+    }
+    __shared__ int part[PG_WAVES];
+    int32_t *fresh = ws, *list = ws + B;
+    int all = 0;
+    for (int b0 = 0; b0 < B; b0 += PG_THREADS) {
+        const int b = b0 + (int)threadIdx.x;
+        int row = b, page = -1;
+        if (b < B) {
+            const int src = src_row[b];
+            if (src < -1 || src >= B) atomicOr(flags, FLAG_BAD_PATH);
+            else if (src >= 0 && src != b) {
+                const int L = seq_len[src];
+                if (L < 0 || (L + 15LL) >> 4 > max_pages) atomicOr(flags, FLAG_CAPACITY);
+                else {
+                    row = src;
+                    if (L & 15) page = table[(size_t)src * max_pages + (L >> 4)];
+                }
+            }
+        }
+        const bool need = page >= 0;
+        int total;
+        const int at = block_scan(need ? 1 : 0, part, total) + all;
+        all += total;
+        if (b < B) {
+            forked[b] = row;
+            copy_src[b] = page;
+            fresh[b] = need ? at : -1;
+        }
+    }
+    const int found = lowest_free(ref, n_pages, min(all, n_pages), list, part);
+    __syncthreads();
+    for (int b = threadIdx.x; b < B; b += PG_THREADS) {
+        const int at = fresh[b];
+        int page = -1;
+        if (at >= 0) {
+            if (at < found) page = list[at];
+            else {                                          // the pool is exhausted: the row stays as it is
+                atomicOr(flags, FLAG_CAPACITY);
+                forked[b] = b;
+                copy_src[b] = -1;
+            }
+        }
+        fresh[b] = page;
+        copy_dst[b] = page;
+    }
+}
+
+__global__ __launch_bounds__(256) void pages_fork_kernel(int32_t *table, int32_t *ref, int n_pages, int max_pages, int B, const int32_t *seq_len,
+                                                          const int32_t *ws, const int32_t *forked, int32_t *flags) {
+    const int b = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
+    const int src = forked[b];
+    if (src == b || i >= max_pages) return;
+    const int32_t *old = ws + 2 * (size_t)B;
+    const int whole = seq_len[src] >> 4;
+    const int was = old[(size_t)b * max_pages + i];
+    int page = -1;
+    if (i < whole) page = old[(size_t)src * max_pages + i];
+    else if (i == whole) page = ws[b];
+    table[(size_t)b * max_pages + i] = page;
+    if (page == was) return;                                // gives up and takes the same page
+    if (page >= 0) {
+        if (page < n_pages) atomicAdd(&ref[page], 1);
+        else atomicOr(flags, FLAG_BAD_PAGE);
+    }
+    if (was >= 0) drop_page(ref, n_pages, was, flags);
+}
+
+// Moves of a compaction.  ws: where page p at or behind U goes [n_pages]
+__global__ __launch_bounds__(PG_THREADS) void pages_compact_plan_kernel(int32_t *ref, int n_pages, int32_t *ws, int32_t *move_src, int32_t *move_dst, int32_t *counts) {
+    __shared__ int part[PG_WAVES];
+    int used = 0;
+    for (int p = threadIdx.x; p < n_pages; p += PG_THREADS) used += ref[p] > 0;
+    int U;
+    block_scan(used, part, U);
+    int holes = 0, moves = 0;
+    for (int p0 = 0; p0 < n_pages; p0 += PG_THREADS) {
+        const int p = p0 + (int)threadIdx.x;
+        const bool in = p < n_pages && ref[p] > 0;
+        const bool hole = p < U && !in, move = p >= U && in;
+        int nh, nm;
+        const int ah = holes + block_scan(hole ? 1 : 0, part, nh), am = moves + block_scan(move ? 1 : 0, part, nm);
+        if (hole) move_dst[ah] = p;
+        if (move) move_src[am] = p;
+        if (p >= U && p < n_pages) ws[p] = p;
+        holes += nh;
+        moves += nm;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n_pages; i += PG_THREADS) {
+        if (i >= moves) { move_src[i] = move_dst[i] = -1; continue; }
+        const int a = move_src[i], d = move_dst[i];
+        ws[a] = d;
+        ref[d] = ref[a];
+        ref[a] = 0;
+    }
+    if (threadIdx.x == 0) { counts[0] = moves; counts[1] = U; }
+}
+
+__global__ __launch_bounds__(256) void pages_remap_kernel(int32_t *table, int n_pages, size_t entries, const int32_t *ws, const int32_t *counts, int32_t *flags) {
+    const int U = counts[1];
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= entries) return;
+    const int page = table[i];
+    if (page >= n_pages) { atomicOr(flags, FLAG_BAD_PAGE); return; }
+    if (page >= U) table[i] = ws[page];
+}
+
+// Whole pages of up to three arrays ([layers][n_pages][bytes] each): a workgroup copies 16 KB pieces, all its loads before its stores.
+struct CopyPlanes { char *base[3]; uint32_t bytes[3], pieces[3]; int n, n_pages, layers; };
+enum { COPY_PIECE = 16384 };
+__global__ __launch_bounds__(256) void copy_pages_kernel(CopyPlanes pl, int n, const int32_t *src, const int32_t *dst, const int32_t *count, int32_t *flags) {
+    if (count) n = min(n, *count);
+    uint32_t per = 0;
+    for (int q = 0; q < pl.n; ++q) per += pl.pieces[q];
+    uint32_t piece = blockIdx.x;
+    int q = 0;
+    while (piece >= pl.pieces[q]) piece -= pl.pieces[q++];
+    const int layer = blockIdx.y;
+    for (int i = blockIdx.z; i < n; i += gridDim.z) {
+        const int a = src[i], d = dst[i];
+        if (a < 0 || d < 0 || a == d) continue;
+        if (a >= pl.n_pages || d >= pl.n_pages) {
+            if (threadIdx.x == 0) atomicOr(flags, FLAG_BAD_PAGE);
+            continue;
+        }
+        const char *from = pl.base[q] + ((size_t)layer * pl.n_pages + a) * pl.bytes[q];
+        char *to = pl.base[q] + ((size_t)layer * pl.n_pages + d) * pl.bytes[q];
+        const uint32_t at = piece * COPY_PIECE, end = min(at + (uint32_t)COPY_PIECE, pl.bytes[q]);
+        typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(4)));     // the caller's pages: no more than 4 bytes' alignment is known
+        u4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t o = at + (j * 256 + threadIdx.x) * 16;
+            if (o + 16 <= end) v[j] = *reinterpret_cast<const u4 *>(from + o);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t o = at + (j * 256 + threadIdx.x) * 16;
+            if (o + 16 <= end) *reinterpret_cast<u4 *>(to + o) = v[j];
+        }
+        const uint32_t rest = end & 15u;                    // scales of an odd number of heads end in half a piece
+        if (rest && threadIdx.x < rest / 4) {
+            const uint32_t o = (end & ~15u) + threadIdx.x * 4;
+            *reinterpret_cast<uint32_t *>(to + o) = *reinterpret_cast<const uint32_t *>(from + o);
+        }
+    }
+}
+
+static int launch_copy(hydra_ctx *c, hipStream_t s, CopyPlanes pl, int n, const int32_t *src, const int32_t *dst, const int32_t *count) {
+    uint32_t per = 0;
+    for (int q = 0; q < pl.n; ++q) { pl.pieces[q] = (pl.bytes[q] + COPY_PIECE - 1) / COPY_PIECE; per += pl.pieces[q]; }
+    const dim3 grid(per, c->m.n_layers, std::min(n, 64)), block(256);
+    hipLaunchKernelGGL(copy_pages_kernel, grid, block, 0, s, pl, n, src, dst, count, flags_dev(c));
+    HYDRA_LAUNCH_CHECK("copy_pages_kernel");
+    return HYDRA_OK;
+}
+
+static int check_pages(hydra_ctx *c, int B, const hydra_pages *p) {
+    if (!c) return fail(HYDRA_E_INVALID_ARG, "ctx is NULL");
+    if (B < 1 || B > c->max_batch) return fail(HYDRA_E_CAPACITY, "B outside [1, max_batch]");
+    if (!c->arena) return fail(HYDRA_E_STATE, "no weight arena bound (hydra_bind_weights)");
+    if (!p || !p->page_table || !p->ref) return fail(HYDRA_E_INVALID_ARG, "pages or one of its pointers is NULL");
+    if (p->n_pages < 1 || p->max_pages < 1) return fail(HYDRA_E_INVALID_ARG, "pages: n_pages and max_pages must be positive");
+    return HYDRA_OK;
+}
+static int check_ws(const void *ws) {
+    if (!ws) return fail(HYDRA_E_INVALID_ARG, "workspace is NULL");
+    if (((uintptr_t)ws) & 255) return fail(HYDRA_E_INVALID_ARG, "workspace must be 256-byte aligned");
+    return HYDRA_OK;
+}
+static int check_copy(hydra_ctx *c, int n, const int32_t *src, const int32_t *dst) {
+    if (!c) return fail(HYDRA_E_INVALID_ARG, "ctx is NULL");
+    if (!c->arena) return fail(HYDRA_E_STATE, "no weight arena bound (hydra_bind_weights)");
+    if (n < 0 || !src || !dst) return fail(HYDRA_E_INVALID_ARG, "copy_pages: n is negative or a list is NULL");
+    return HYDRA_OK;
+}
+
+}  // namespace hydra
+
+using namespace hydra;
+
+extern "C" {
+
+size_t hydra_pages_workspace_bytes(int B, int n_pages, int max_pages) {
+    if (B < 1 || n_pages < 1 || max_pages < 1) return 0;
+    const size_t reserve = (size_t)B + n_pages, fork = 2 * (size_t)B + (size_t)B * max_pages, compact = n_pages;
+    return align_up(std::max(reserve, std::max(fork, compact)) * 4, 256);
+}
+
+int hydra_pages_reserve(hydra_ctx *c, void *stream, int B, void *ws, const hydra_pages *p, const int32_t *lo, const int32_t *hi, int extra, int32_t *ok) {
+    int rc = check_pages(c, B, p);
+    if (rc) return rc;
+    if ((rc = check_ws(ws))) return rc;
+    if (!hi || extra < 0) return fail(HYDRA_E_INVALID_ARG, "hydra_pages_reserve: hi is NULL or extra is negative");
+    hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(PG_THREADS), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages, B, lo, hi, extra,
+                       (int32_t *)ws, ok, flags_dev(c));
+    HYDRA_LAUNCH_CHECK("pages_reserve_kernel");
+    return HYDRA_OK;
+}
+
+int hydra_pages_release(hydra_ctx *c, void *stream, int B, const hydra_pages *p, const int32_t *lo, const int32_t *hi) {
+    int rc = check_pages(c, B, p);
+    if (rc) return rc;
+    if (!hi) return fail(HYDRA_E_INVALID_ARG, "hydra_pages_release: hi is NULL");
+    hipLaunchKernelGGL(pages_release_kernel, dim3(ceil_div(p->max_pages, 256), B), dim3(256), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages,
+                       p->max_pages, lo, hi, flags_dev(c));
+    HYDRA_LAUNCH_CHECK("pages_release_kernel");
+    return HYDRA_OK;
+}
+
+int hydra_pages_fork(hydra_ctx *c, void *stream, int B, void *ws, const hydra_pages *p, const int32_t *src_row, const int32_t *seq_len, int32_t *copy_src,
+                     int32_t *copy_dst, int32_t *forked) {
+    int rc = check_pages(c, B, p);
+    if (rc) return rc;
+    if ((rc = check_ws(ws))) return rc;
+    if (!src_row || !seq_len || !copy_src || !copy_dst || !forked) return fail(HYDRA_E_INVALID_ARG, "hydra_pages_fork: NULL argument");
+    const int copiers = (int)std::min<size_t>(128, ((size_t)B * p->max_pages + PG_THREADS - 1) / PG_THREADS);
+    hipLaunchKernelGGL(pages_fork_plan_kernel, dim3(1 + copiers), dim3(PG_THREADS), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages, B,
+                       src_row, seq_len, (int32_t *)ws, copy_src, copy_dst, forked, flags_dev(c));
+    HYDRA_LAUNCH_CHECK("pages_fork_plan_kernel");
+    hipLaunchKernelGGL(pages_fork_kernel, dim3(ceil_div(p->max_pages, 256), B), dim3(256), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages,
+                       B, seq_len, (const int32_t *)ws, forked, flags_dev(c));
+    HYDRA_LAUNCH_CHECK("pages_fork_kernel");
+    return HYDRA_OK;
+}
+
+int hydra_pages_compact(hydra_ctx *c, void *stream, int B, void *ws, const hydra_pages *p, int32_t *move_src, int32_t *move_dst, int32_t *counts) {
+    int rc = check_pages(c, B, p);
+    if (rc) return rc;
+    if ((rc = check_ws(ws))) return rc;
+    if (!move_src || !move_dst || !counts) return fail(HYDRA_E_INVALID_ARG, "hydra_pages_compact: NULL argument");
+    hipLaunchKernelGGL(pages_compact_plan_kernel, dim3(1), dim3(PG_THREADS), 0, (hipStream_t)stream, p->ref, p->n_pages, (int32_t *)ws, move_src, move_dst, counts);
+    HYDRA_LAUNCH_CHECK("pages_compact_plan_kernel");
+    const size_t entries = (size_t)B * p->max_pages;
+    hipLaunchKernelGGL(pages_remap_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, (hipStream_t)stream, p->page_table, p->n_pages, entries,
+                       (const int32_t *)ws, counts, flags_dev(c));
+    HYDRA_LAUNCH_CHECK("pages_remap_kernel");
+    return HYDRA_OK;
+}
+
+int hydra_kv_copy_pages(hydra_ctx *c, void *stream, const hydra_kv *kv, int n, const int32_t *src, const int32_t *dst, const int32_t *count) {
+    int rc = check_copy(c, n, src, dst);
+    if (rc) return rc;
+    if (!kv || !kv->k_pages || !kv->v_pages || kv->n_pages < 1) return fail(HYDRA_E_INVALID_ARG, "kv or one of its page arrays is NULL, or n_pages is not positive");
+    if (n == 0) return HYDRA_OK;
+    CopyPlanes pl = {};
+    pl.n = 2; pl.n_pages = kv->n_pages; pl.layers = c->m.n_layers;
+    pl.base[0] = (char *)kv->k_pages; pl.base[1] = (char *)kv->v_pages;
+    pl.bytes[0] = pl.bytes[1] = (uint32_t)(c->m.d * HYDRA_PAGE * c->esz);
+    return launch_copy(c, (hipStream_t)stream, pl, n, src, dst, count);
+}
+
+int hydra_kv8_copy_pages(hydra_ctx *c, void *stream, const hydra_kv8 *kv, int n, const int32_t *src, const int32_t *dst, const int32_t *count) {
+    int rc = check_copy(c, n, src, dst);
+    if (rc) return rc;
+    if (!c->bf16) return fail(HYDRA_E_UNSUPPORTED, "the 8-bit cache is for HYDRA_BF16 contexts");
+    if (!kv || !kv->k_codes || !kv->v_codes || !kv->scales || kv->n_pages < 1) return fail(HYDRA_E_INVALID_ARG, "kv8 or one of its arrays is NULL, or n_pages is not positive");
+    if (n == 0) return HYDRA_OK;
+    CopyPlanes pl = {};
+    pl.n = 3; pl.n_pages = kv->n_pages; pl.layers = c->m.n_layers;
+    pl.base[0] = (char *)kv->k_codes; pl.base[1] = (char *)kv->v_codes; pl.base[2] = (char *)kv->scales;
+    pl.bytes[0] = pl.bytes[1] = (uint32_t)(c->m.d * HYDRA_PAGE); pl.bytes[2] = (uint32_t)(c->m.n_heads * 8);
+    return launch_copy(c, (hipStream_t)stream, pl, n, src, dst, count);
+}
+
+}  // extern "C"
