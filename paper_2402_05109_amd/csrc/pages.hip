@@ -272,8 +272,6 @@ struct CopyPlanes { char *base[3]; uint32_t bytes[3], pieces[3]; int n, n_pages,
 enum { COPY_PIECE = 16384 };
 __global__ __launch_bounds__(256) void copy_pages_kernel(CopyPlanes pl, int n, const int32_t *src, const int32_t *dst, const int32_t *count, int32_t *flags) {
     if (count) n = min(n, *count);
-    uint32_t per = 0;
-    for (int q = 0; q < pl.n; ++q) per += pl.pieces[q];
     uint32_t piece = blockIdx.x;
     int q = 0;
     while (piece >= pl.pieces[q]) piece -= pl.pieces[q++];
@@ -404,6 +402,7 @@ int hydra_kv_copy_pages(hydra_ctx *c, void *stream, const hydra_kv *kv, int n, c
     int rc = check_copy(c, n, src, dst);
     if (rc) return rc;
     if (!kv || !kv->k_pages || !kv->v_pages || kv->n_pages < 1) return fail(HYDRA_E_INVALID_ARG, "kv or one of its page arrays is NULL, or n_pages is not positive");
+    if (((uintptr_t)kv->k_pages | (uintptr_t)kv->v_pages) & 15) return fail(HYDRA_E_INVALID_ARG, "copy_pages: pages must be 16-byte aligned");
     if (n == 0) return HYDRA_OK;
     CopyPlanes pl = {};
     pl.n = 2; pl.n_pages = kv->n_pages; pl.layers = c->m.n_layers;
@@ -417,6 +416,8 @@ int hydra_kv8_copy_pages(hydra_ctx *c, void *stream, const hydra_kv8 *kv, int n,
     if (rc) return rc;
     if (!c->bf16) return fail(HYDRA_E_UNSUPPORTED, "the 8-bit cache is for HYDRA_BF16 contexts");
     if (!kv || !kv->k_codes || !kv->v_codes || !kv->scales || kv->n_pages < 1) return fail(HYDRA_E_INVALID_ARG, "kv8 or one of its arrays is NULL, or n_pages is not positive");
+    if (((uintptr_t)kv->k_codes | (uintptr_t)kv->v_codes) & 15 || (uintptr_t)kv->scales & 7)
+        return fail(HYDRA_E_INVALID_ARG, "copy_pages: codes must be 16-byte aligned, scales 8-byte");
     if (n == 0) return HYDRA_OK;
     CopyPlanes pl = {};
     pl.n = 3; pl.n_pages = kv->n_pages; pl.layers = c->m.n_layers;

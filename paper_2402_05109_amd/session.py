@@ -37,11 +37,21 @@ class _Outputs:
 class Session:
     """`shape` needs attributes d, NL, H, Dh, F, V, dtype ('f32'|'bf16'), K, mlp_layers, rms_eps,
     rope_theta, include_root_embedding.  `get_tensor(name)` returns the named weight as a
-    device tensor in the model dtype (names as in the weight generator)."""
+    device tensor in the model dtype (names as in the weight generator).
+
+    cache_format 'int8' or 'e4m3' (bf16 models): whole pages of the base cache are held in 8 bits; a row keeps the
+    few 16-bit pages of its last, incomplete page and of a step's tree nodes.
+    pool_pages: the cache has that many pages for all rows together (B * max_len tokens have not to fit), which rows take
+    as they grow, share after fork() and give back with free_rows(); defragment() moves the pages in use to the front."""
 
     def __init__(self, shape, parent: Sequence[int], B: int, max_len: int,
                  get_tensor: Callable[[str], torch.Tensor], device="cuda:0", prefill_chunk: int = 64,
-                 page_perm_seed: Optional[int] = None, want_logits: bool = False, max_pos: Optional[int] = None):
+                 page_perm_seed: Optional[int] = None, want_logits: bool = False, max_pos: Optional[int] = None,
+                 cache_format: Optional[str] = None, pool_pages: Optional[int] = None):
+        if cache_format not in (None, "int8", "e4m3"):
+            raise ValueError(f"cache_format {cache_format!r}: None (16 bits), 'int8' or 'e4m3'")
+        if cache_format and shape.dtype != "bf16":
+            raise ValueError("an 8-bit cache needs a bf16 model")
         self.shape, self.B, self.dev = shape, B, torch.device(device)
         self.parent = list(parent)
         self.dtype_code = hb.HYDRA_BF16 if shape.dtype == "bf16" else hb.HYDRA_F32
@@ -59,20 +69,49 @@ class Session:
         self._bind(self.main)
         self._load_weights(get_tensor)
         # KV cache
-        T_max = max(len(self.parent), self.prefill_chunk)
+        self._T_max = T_max = max(len(self.parent), self.prefill_chunk)
         self.max_pages = (max_len + T_max + 15) // 16
-        self.n_pages = B * self.max_pages
-        n_el = shape.NL * self.n_pages * shape.H * 16 * shape.Dh
+        self.pool = pool_pages is not None
+        self.n_pages = int(pool_pages) if self.pool else B * self.max_pages
         cache_dtype = torch.float16 if shape.dtype == "bf16" else torch.float32     # 2 or 4 bytes per element; content is private
-        self.k_pages = torch.zeros(n_el, dtype=cache_dtype, device=self.dev)
-        self.v_pages = torch.zeros(n_el, dtype=cache_dtype, device=self.dev)
-        if page_perm_seed is None:
-            perm = torch.arange(self.n_pages, dtype=torch.int32)
+        block = shape.H * 16 * shape.Dh
+        i32 = dict(dtype=torch.int32, device=self.dev)
+        if self.pool:
+            self.page_table = torch.full((B, self.max_pages), -1, **i32)
+            self.pages = hb.Pages(self.page_table, torch.zeros(self.n_pages, **i32))
+            self._lists = torch.zeros(5, max(B, self.n_pages), **i32)              # copies or moves, their counts, forked rows, rows served
         else:
-            g = torch.Generator().manual_seed(page_perm_seed)
-            perm = torch.randperm(self.n_pages, generator=g).to(torch.int32)
-        self.page_table = perm.reshape(B, self.max_pages).contiguous().to(self.dev)
-        self.kv = hb.KV(self.k_pages, self.v_pages, self.page_table, self.n_pages, seq_len_hint=0)
+            if page_perm_seed is None:
+                perm = torch.arange(self.n_pages, dtype=torch.int32)
+            else:
+                g = torch.Generator().manual_seed(page_perm_seed)
+                perm = torch.randperm(self.n_pages, generator=g).to(torch.int32)
+            self.page_table = perm.reshape(B, self.max_pages).contiguous().to(self.dev)
+        self.kv8: Optional[hb.KV8] = None
+        if cache_format is None:
+            self.k_pages = torch.zeros(shape.NL * self.n_pages * block, dtype=cache_dtype, device=self.dev)
+            self.v_pages = torch.zeros(shape.NL * self.n_pages * block, dtype=cache_dtype, device=self.dev)
+            self.kv = hb.KV(self.k_pages, self.v_pages, self.page_table, self.n_pages, seq_len_hint=0)
+        else:
+            # 16-bit pages that a row can need at once: those of the slots 16 n .. 16 n + 14 + T, taken in turn; from a small pool of their
+            # own (with one more per row for copies) where rows can be forked
+            ring = (T_max + 14) // 16 + 1
+            self.n_tail = B * (ring + (1 if self.pool else 0))
+            self.k_pages = torch.zeros(shape.NL * self.n_tail * block, dtype=cache_dtype, device=self.dev)
+            self.v_pages = torch.zeros(shape.NL * self.n_tail * block, dtype=cache_dtype, device=self.dev)
+            if self.pool:
+                tail_table = torch.full((B, self.max_pages), -1, **i32)
+                self.tail_pages = hb.Pages(tail_table, torch.zeros(self.n_tail, **i32))
+            else:
+                tail_table = (torch.arange(B, **i32)[:, None] * ring + torch.arange(self.max_pages, **i32)[None, :] % ring).contiguous()
+            self.kv = hb.KV(self.k_pages, self.v_pages, tail_table, self.n_tail, seq_len_hint=0)
+            self.k_codes = torch.zeros(shape.NL * self.n_pages * block, dtype=torch.uint8, device=self.dev)
+            self.v_codes = torch.zeros(shape.NL * self.n_pages * block, dtype=torch.uint8, device=self.dev)
+            self.kv8 = hb.KV8(self.kv, self.k_codes, self.v_codes, torch.ones(shape.NL, self.n_pages, shape.H, 2, device=self.dev), self.page_table,
+                              torch.zeros(B, **i32), self.n_pages, hb.KV8_INT8 if cache_format == "int8" else hb.KV8_E4M3)
+        if self.pool:
+            most = max(self.n_pages, self.kv.n_pages)
+            self._pages_ws = torch.empty(hb.pages_workspace_bytes(B, most, self.max_pages), dtype=torch.uint8, device=self.dev)
         # state
         self.seq_len = torch.zeros(B, dtype=torch.int32, device=self.dev)
         self.h_last = torch.zeros(B, shape.d, dtype=torch.float32, device=self.dev)
@@ -99,7 +138,7 @@ class Session:
                 first.load_tensor(kind, 0, 0, get_tensor(f"prefix.{nm}"))
             first.load_tensor(hb.W_FINAL_NORM, 0, 0, torch.ones(shape.d, dtype=self.tdtype, device=self.dev))   # never used; kept defined
             torch.cuda.synchronize()
-            n_el1 = self.n_pages * shape.H * 16 * shape.Dh
+            n_el1 = self.n_pages * block
             self.pk_pages = torch.zeros(n_el1, dtype=cache_dtype, device=self.dev)
             self.pv_pages = torch.zeros(n_el1, dtype=cache_dtype, device=self.dev)
             self.pkv = hb.KV(self.pk_pages, self.pv_pages, self.page_table, self.n_pages, seq_len_hint=0)
@@ -137,6 +176,8 @@ class Session:
         room for 16 contexts in all)."""
         if name in self._ctx:
             raise ValueError(f"context {name!r} exists")
+        if self.kv8 is not None and len(parent) > self._T_max:
+            raise ValueError(f"an 8-bit cache of this session has 16-bit pages for trees of up to {self._T_max} nodes")
         c = self._make_ctx(name, list(parent))
         self._bind(c)
         need = c.workspace_bytes(self.B)
@@ -167,12 +208,12 @@ class Session:
             self._prefix_bind(self._prefix_ctx_new(P))
         return self._pctx[P]
 
-    def prefix_attention(self, name: str = "main") -> None:
-        """Feeds the accepted tokens' hidden states of context `name` to the prefix layer; h_last becomes its output."""
+    def prefix_attention(self, name: str = "main", rows: Optional[int] = None) -> None:
+        """Feeds the accepted tokens' hidden states of context `name` to the prefix layer; h_last becomes its output (the first `rows` rows)."""
         c, o = self._ctx[name], self._out[name]
         P = o.path.shape[1]
         self.pkv.seq_len_hint = self.host_len
-        self.prefix_ctx(P).hydra_prefix_attention(self.B, self.ws, o.hidden, c.T, o.path, o.n_acc, self.pseq_len, self.pkv, self.h_last)
+        self.prefix_ctx(P).hydra_prefix_attention(rows or self.B, self.ws, o.hidden, c.T, o.path, o.n_acc, self.pseq_len, self.pkv, self.h_last)
 
     def out(self, name: str = "main") -> _Outputs:
         return self._out[name]
@@ -205,22 +246,121 @@ class Session:
         self.seq_len.zero_(); self.h_last.zero_(); self.root.zero_()
         if self.prefix:
             self.pseq_len.zero_()
+        if self.kv8 is not None:
+            self.kv8.n_sealed.zero_()
+        if self.pool:
+            for p in self._pools():
+                p.page_table.fill_(-1)
+                p.ref.zero_()
         self.host_len = 0
         self._len_event = None
 
+    # ---- the cache behind a forward pass, in 16 or 8 bits ------------------------
+    def _forward(self, c: hb.Hydra, o: _Outputs, B: int) -> None:
+        args = (o.tree_tokens, self.seq_len[:B])
+        out = (o.hidden, o.argmax, o.margin, o.logits)
+        if self.kv8 is None:
+            c.tree_verify_forward(B, self.ws, *args, self.kv, *out)
+        else:
+            c.tree_verify_forward_kv8(B, self.ws, *args, self.kv8, *out)
+
+    def _keep_accepted(self, c: hb.Hydra, o: _Outputs, B: int, h_last: torch.Tensor, root: torch.Tensor) -> None:
+        c.kv_compact(B, o.n_acc, o.path, o.next_root, o.last_node, o.hidden, self.kv, self.seq_len, h_last, root, o.kv_index)
+        if self.kv8 is not None:
+            c.hydra_kv8_seal(B, self.seq_len, self.kv8)
+
+    # ---- pages ------------------------------------------------------------------
+    def _pools(self) -> List[hb.Pages]:
+        return [self.pages] if self.kv8 is None else [self.pages, self.tail_pages]
+
+    def _need_pool(self) -> None:
+        if not self.pool:
+            raise ValueError("rows of this session have pages of their own: create the Session with pool_pages")
+
+    def _reserve(self, T: int, B: int) -> None:
+        """Pages for T more slots of the first B rows.  Waits for the device only where the pool might be too small."""
+        if not self.pool:
+            return
+        ok = self._lists[4]
+        self.main.hydra_pages_reserve(B, self._pages_ws, self.pages, None, self.seq_len, T, ok)
+        if self.kv8 is not None:
+            lo = self.kv8.n_sealed * 16
+            self.main.hydra_pages_release(B, self.tail_pages, lo, self.seq_len)
+            self.main.hydra_pages_reserve(B, self._pages_ws, self.tail_pages, lo, self.seq_len, T)
+        if self.B * ((self.host_len + T + 15) // 16) > self.n_pages and not bool(ok[:B].all()):
+            raise RuntimeError(f"the pool of {self.n_pages} pages is exhausted")
+
+    def fork(self, src_rows: Sequence[int]) -> None:
+        """Row b becomes a copy of row src_rows[b] as it is now (b or -1: stays).  Whole pages are shared; only the last, incomplete page
+        is copied.  For samples of one prompt, or beams that change places."""
+        self._need_pool()
+        if len(src_rows) != self.B or any(r < -1 or r >= self.B for r in src_rows):
+            raise ValueError(f"fork: {self.B} rows of [-1, {self.B})")
+        B, m = self.B, self.main
+        want = torch.tensor([b if r < 0 else r for b, r in enumerate(src_rows)], dtype=torch.int32, device=self.dev)
+        src, dst, forked = self._lists[0], self._lists[1], self._lists[3]
+        for p in self._pools():                       # what lies behind the text (scratch of the last step) goes back first
+            m.hydra_pages_release(B, p, None, self.seq_len)
+        m.hydra_pages_fork(B, self._pages_ws, self.pages, want, self.seq_len, src, dst, forked)
+        if not torch.equal(forked[:B], want):
+            got = forked[:B].clone()
+            self._take_rows(got, src, dst)
+            raise RuntimeError(f"the pool of {self.n_pages} pages is exhausted: rows {(got != want).nonzero()[:, 0].tolist()} stay as they were")
+        self._take_rows(forked[:B].clone(), src, dst)
+
+    def _take_rows(self, rows: torch.Tensor, src: torch.Tensor, dst: torch.Tensor) -> None:
+        """Contents and state of rows that the tables say are copies now."""
+        B, m = self.B, self.main
+        if self.kv8 is None:
+            m.hydra_kv_copy_pages(self.kv, B, src, dst)
+        if self.prefix:
+            self.prefix_ctx(self.main.depth + 1).hydra_kv_copy_pages(self.pkv, B, src, dst)
+        if self.kv8 is not None:
+            m.hydra_pages_fork(B, self._pages_ws, self.tail_pages, rows, self.seq_len, src, dst, self._lists[3])
+            m.hydra_kv_copy_pages(self.kv, B, src, dst)
+        state = [self.seq_len, self.h_last, self.root] + ([self.pseq_len] if self.prefix else []) + ([self.kv8.n_sealed] if self.kv8 is not None else [])
+        for t in state:
+            t.copy_(t[rows.long()])
+        self._len_event = None                        # a length on its way to the host may be another row's
+
+    def free_rows(self, rows: Sequence[int]) -> None:
+        """The rows' text ends: they start again from nothing, and their pages (where no other row shares them) are free."""
+        self._need_pool()
+        at = torch.tensor(list(rows), dtype=torch.int64, device=self.dev)
+        for t in [self.seq_len, self.h_last, self.root] + ([self.pseq_len] if self.prefix else []) + ([self.kv8.n_sealed] if self.kv8 is not None else []):
+            t.index_fill_(0, at, 0)
+        for p in self._pools():
+            self.main.hydra_pages_release(self.B, p, None, self.seq_len)
+
+    def defragment(self) -> int:
+        """Gives back what no text needs, moves the pages in use to the front of the pool and returns how many they are (waits for the device)."""
+        self._need_pool()
+        m, (src, dst, counts) = self.main, self._lists[:3]
+        for p in self._pools():
+            m.hydra_pages_release(self.B, p, None, self.seq_len)
+        m.hydra_pages_compact(self.B, self._pages_ws, self.pages, src, dst, counts)
+        if self.kv8 is None:
+            m.hydra_kv_copy_pages(self.kv, self.n_pages, src, dst, counts)
+        else:
+            m.hydra_kv8_copy_pages(self.kv8, self.n_pages, src, dst, counts)
+        if self.prefix:
+            self.prefix_ctx(m.depth + 1).hydra_kv_copy_pages(self.pkv, self.n_pages, src, dst, counts)
+        return int(counts[1])
+
     def prefill(self, prompts: torch.Tensor) -> None:
-        """prompts: int32 [B, L] (same length for every row).  Causal chunks through
+        """prompts: int32 [B, L] (same length for every row; with pool_pages also fewer rows, the first ones).  Causal chunks through
         tree_verify_forward with a chain tree; the state update is kv_compact with the
         identity path.  Where an exception breaks the prompt off, seq_len, h_last and root are those behind the last chunk that was
         computed whole (behind the text in front of the prompt if there is none)."""
         B, L = prompts.shape
-        assert B == self.B
+        assert B == self.B or (self.pool and B < self.B)
         prompts = prompts.to(self.dev, torch.int32)
         chunks = [min(self.prefill_chunk, L - pos) for pos in range(0, L, self.prefill_chunk)]
         # A chunk whose outputs a later chunk of the same length writes again ends behind the decoder layers: no final norm, LM head and
         # argmax, whose results nobody can read once the call is over.  Not where the prefix layer reads every chunk's hidden states, and not where the prompt
-        # does not fit (the chunks in front of the one that is refused then keep their outputs and the state behind them).
-        layers_only = not self.prefix and self.host_len + L <= min(self.max_pages * 16, self._max_pos)
+        # does not fit (the chunks in front of the one that is refused then keep their outputs and the state behind them).  Not behind an 8-bit
+        # cache either: the 16-bit pages of the text in front are taken again two chunks later, so there would be no way back to it.
+        layers_only = not self.prefix and self.kv8 is None and self.host_len + L <= min(self.max_pages * 16, self._max_pos)
         last = {n: i for i, n in enumerate(chunks)}
         pos = 0
         behind = None                                 # seq_len and its bound behind the last chunk that h_last and root know of, if others followed
@@ -229,11 +369,12 @@ class Session:
                 name = f"chain{n}"
                 c = self.ctx(name)
                 o = self._out[name]
-                o.tree_tokens.copy_(prompts[:, pos:pos + n])
+                o.tree_tokens[:B].copy_(prompts[:, pos:pos + n])
                 self._hint(n)
+                self._reserve(n, B)
                 if i == chunks.index(n):              # the same for every chunk of this length
                     o.n_acc.fill_(n)
-                    o.path.copy_(torch.arange(n, dtype=torch.int32, device=self.dev).expand(B, n))
+                    o.path.copy_(torch.arange(n, dtype=torch.int32, device=self.dev).expand(self.B, n))
                     o.last_node.fill_(n - 1)
                 h_last, root = self.h_last, self.root
                 if layers_only and i < last[n]:
@@ -242,13 +383,13 @@ class Session:
                     h_last, root = torch.empty_like(h_last), torch.empty_like(root)       # of outputs that are not written
                     c.hydra_prefill_chunk(B, self.ws, o.tree_tokens, self.seq_len, self.kv)
                 else:
-                    c.tree_verify_forward(B, self.ws, o.tree_tokens, self.seq_len, self.kv, o.hidden, o.argmax, o.margin, o.logits)
+                    self._forward(c, o, B)
                     o.next_root.copy_(o.argmax[:, n - 1])
-                c.kv_compact(B, o.n_acc, o.path, o.next_root, o.last_node, o.hidden, self.kv, self.seq_len, h_last, root, o.kv_index)
+                self._keep_accepted(c, o, B, h_last, root)
                 if h_last is self.h_last:
                     behind = None
                 if self.prefix:
-                    self.prefix_attention(name)       # hint: still the length before this chunk
+                    self.prefix_attention(name, B)    # hint: still the length before this chunk
                 pos += n
                 self.host_len += n
         except BaseException:
@@ -264,7 +405,8 @@ class Session:
     def verify(self, name: str = "main") -> None:
         c, o = self.ctx(name), self._out[name]
         self._hint(c.T)
-        c.tree_verify_forward(self.B, self.ws, o.tree_tokens, self.seq_len, self.kv, o.hidden, o.argmax, o.margin, o.logits)
+        self._reserve(c.T, self.B)
+        self._forward(c, o, self.B)
 
     def accept(self, name: str = "main") -> None:
         c, o = self.ctx(name), self._out[name]
@@ -280,8 +422,7 @@ class Session:
     def compact(self, name: str = "main") -> None:
         c, o = self.ctx(name), self._out[name]
         self._hint(c.T)
-        c.kv_compact(self.B, o.n_acc, o.path, o.next_root, o.last_node, o.hidden, self.kv, self.seq_len, self.h_last,
-                     self.root, o.kv_index)
+        self._keep_accepted(c, o, self.B, self.h_last, self.root)
         self.host_len += c.depth + 1          # upper bound; the device holds the exact value
         self._growth_since_copy += c.depth + 1
 
