@@ -510,7 +510,7 @@ static int forward_layers(hydra_ctx *c, hipStream_t s, int B, void *ws, const Ro
             const LayerOff &o = c->layer[l];
             const float *next_gain = (const float *)(A + (l + 1 < c->m.n_layers ? c->layer[l + 1].attn_norm : c->off_final_norm));
             if ((rc = launch_gemm_qkv_rope(c, s, xa, A + o.wqkv, M, rs, l, seq_len, kv, qbuf, part, flags, !kv8))) return rc;
-            if (kv8) { if ((rc = launch_kv8_attention(c, s, B, l, qbuf, false, seq_len, kv8, apart, w.attn_units, xb, false, flags))) return rc; }
+            if (kv8) { if ((rc = launch_kv8_attention(c, s, B, l, qbuf, false, seq_len, kv8, apart, w.attn_units, xb, flags))) return rc; }
             else     { if ((rc = launch_attention(c, s, B, l, qbuf, seq_len, kv, apart, w.attn_units, xb, nullptr, flags))) return rc; }
             if ((rc = launch_gemm_resid(c, s, xb, A + o.wo, M, d, d, x, (const float *)(A + o.ffn_norm), xa, ss, Mpad, part, &rs.nb))) return rc;
             if ((rc = launch_gemm_silu(c, s, xa, A + o.wgu, M, F, d, ss, rs.nb, Mpad, xb))) return rc;
@@ -593,7 +593,7 @@ int tree_attention_kv8(hydra_ctx *c, void *stream, int B, int layer, void *ws, c
     if (layer < 0 || layer >= c->m.n_layers) return fail(HYDRA_E_INVALID_ARG, "layer out of range");
     if ((rc = check_kv8(c, kv))) return rc;
     const WsLayout w = ws_layout(c, B);
-    return launch_kv8_attention(c, (hipStream_t)stream, B, layer, q, true, seq_len, kv, (float *)((char *)ws + w.apart), w.attn_units, out, true, flags_ptr(c));
+    return launch_kv8_attention(c, (hipStream_t)stream, B, layer, q, true, seq_len, kv, (float *)((char *)ws + w.apart), w.attn_units, out, flags_ptr(c));
 }
 
 int hydra_kv8_seal(hydra_ctx *c, void *stream, int B, const int32_t *seq_len, const hydra_kv8 *kv) {

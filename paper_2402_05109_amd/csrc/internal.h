@@ -201,9 +201,9 @@ int launch_compact(hydra_ctx *c, hipStream_t s, int B, const int32_t *n_acc, con
                    const int32_t *next_root, const int32_t *last_node, const float *hidden, const hydra_kv *kv,
                    int32_t *seq_len, float *h_last, int32_t *root, int32_t *kv_index);
 
-// 8-bit cache (kv8_cache.hip, kv8_attn.hip).  q_plain / out_plain: half [B, T, H, Dh]; otherwise qbuf and the next GEMM's input
-int launch_kv8_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const void *q, bool q_plain, const int32_t *seq_len, const hydra_kv8 *kv,
-                         float *apart, int units_max, void *out, bool out_plain, int32_t *flags);
+// 8-bit cache (kv8_cache.hip, kv8_attn.hip).  plain: queries and result are half [B, T, H, Dh]; otherwise qbuf and the next GEMM's input
+int launch_kv8_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const void *q, bool plain, const int32_t *seq_len, const hydra_kv8 *kv,
+                         float *apart, int units_max, void *out, int32_t *flags);
 int kv8_max_dynamic_lds();
 int launch_kv8_seal(hydra_ctx *c, hipStream_t s, int B, const int32_t *seq_len, const hydra_kv8 *kv);
 int launch_kv8_read(hydra_ctx *c, hipStream_t s, int B, int layer, const hydra_kv8 *kv, int first_slot, int n_slots, float *plain);

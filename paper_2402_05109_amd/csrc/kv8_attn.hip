@@ -20,17 +20,24 @@ namespace hydra {
 
 static constexpr float LOG2E = 1.44269504f;
 
-// Exponents of one 32-key tile -> weights, in place, the running maximum and the lane's share of the sum (its two pages apart).
-struct TileScale { float k0, k1, v0, v1, r0, r1; };      // of its two pages: c s_K, log2 s_V, 1 / s_V
+// How far (in powers of two) a query's maximum may trail its exponents before what was accumulated is rescaled.  Weights are then at most
+// 2^LAZY; being floating, they keep their 11 bits, and the sum is taken over the rounded ones, so that a row that one key
+// dominates still gets that key's value exactly.  16 rows x 64 nodes x 2048 tokens 69.6 -> 66.0 us, 4 rows 29.8 -> 27.7 against LAZY = 0 (the
+// maximum of 32 queries moves in nearly every one of a wave's tiles).
+static constexpr float LAZY = 8.f;
+
+struct TileScale { float k0, k1, v0, v1, r0, r1; };      // of a tile's two pages: c s_K, log2 s_V, 1 / s_V
+
+// Products of one 32-key tile -> weights as the P^T operands of the two pages, the running maximum, and this half-wave's share of the sum.
 template <int DT>
-__device__ __forceinline__ void kv8_softmax(f32x16_t &z, const TileScale &ts, float &m_run, float &l_run, f32x16_t (&o)[DT]) {
+__device__ __forceinline__ void kv8_softmax(const f32x16_t &z, const TileScale &ts, float &m_run, float &l_run, f32x16_t (&o)[DT], u32x4_t (&pb)[2]) {
     float a = z[0], b = z[8];
 #pragma unroll
     for (int v = 1; v < 8; ++v) { a = fmaxf(a, z[v]); b = fmaxf(b, z[8 + v]); }
     float top = fmaxf(fmaf(a, ts.k0, ts.v0), fmaf(b, ts.k1, ts.v1));
     const HalfWaves h = half_waves(top);
     top = fmaxf(h.lo, h.hi);
-    if (__any(top > m_run)) {
+    if (__any(top > m_run + LAZY)) {
         const float m_new = fmaxf(m_run, top);
         const float alpha = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
@@ -44,13 +51,18 @@ __device__ __forceinline__ void kv8_softmax(f32x16_t &z, const TileScale &ts, fl
     const float c0 = ts.v0 - ref, c1 = ts.v1 - ref;
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-    for (int v = 0; v < 8; ++v) {
-        z[v] = __builtin_amdgcn_exp2f(fmaf(z[v], ts.k0, c0));
-        z[8 + v] = __builtin_amdgcn_exp2f(fmaf(z[8 + v], ts.k1, c1));
-        s0 += z[v];
-        s1 += z[8 + v];
+    for (int w = 0; w < 4; ++w) {
+        pb[0][w] = half_pack(__builtin_amdgcn_exp2f(fmaf(z[2 * w], ts.k0, c0)), __builtin_amdgcn_exp2f(fmaf(z[2 * w + 1], ts.k0, c0)));
+        pb[1][w] = half_pack(__builtin_amdgcn_exp2f(fmaf(z[8 + 2 * w], ts.k1, c1)), __builtin_amdgcn_exp2f(fmaf(z[8 + 2 * w + 1], ts.k1, c1)));
     }
-    l_run += s0 * ts.r0 + s1 * ts.r1;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t p0 = pb[0][w], p1 = pb[1][w];
+        const h16x2_t h0 = __builtin_bit_cast(h16x2_t, p0), h1 = __builtin_bit_cast(h16x2_t, p1);
+        s0 = fmaf((float)h0[0], ts.r0, s0); s0 = fmaf((float)h0[1], ts.r0, s0);
+        s1 = fmaf((float)h1[0], ts.r1, s1); s1 = fmaf((float)h1[1], ts.r1, s1);
+    }
+    l_run += s0 + s1;
 }
 
 struct Kv8Args {
@@ -65,16 +77,34 @@ struct Kv8Args {
     void *out;
     int32_t *flags;
     int max_pages8, n_pages8, max_pages, n_pages, layer, T, H, groups, key_wgs;
+    int plain;                                               // queries and result are half [B, T, H, Dh]; otherwise the packed query buffer and the next GEMM's input
     float c;
 };
 
-enum { KV8_WAVES = 8 };
-static size_t kv8_lds_bytes(int Dh, int qt) { return (size_t)qt * Dh * 64 + (size_t)KV8_WAVES * Dh * 128 + KV8_WAVES * 64 * 4 * qt; }
+// 16 bytes of a query: dims d0 .. d0 + 7 of column `col` of a query tile (queries past the last one: zeros, or whatever the packed buffer holds; nobody
+// stores their result)
+template <int DH>
+__device__ __forceinline__ u32x4_t query_piece(const Kv8Args &p, int b, int h, int qtile, int QTtot, int col, int d0) {
+    if (!p.plain) return p.q[((((size_t)b * p.H + h) * QTtot + qtile) * (DH / 16) + (d0 >> 4)) * 64 + ((d0 >> 3) & 1) * 32 + col];
+    const int query = qtile * 32 + col;
+    u32x4_t v = {0u, 0u, 0u, 0u};
+    if (query < p.T) v = *reinterpret_cast<const u32x4_t *>(reinterpret_cast<const a16_t *>(p.q) + ((size_t)(b * p.T + query) * p.H + h) * DH + d0);
+    return v;
+}
+// four dims of a result
+template <int DH>
+__device__ __forceinline__ void store_result(const Kv8Args &p, int m, int h, int dim, float a, float b, float c, float d) {
+    a16_t *to = reinterpret_cast<a16_t *>(p.out) + (p.plain ? ((size_t)m * p.H + h) * DH + dim : x_index<true>(m, h * DH + dim, p.H * DH));
+    *reinterpret_cast<u32x2_t *>(to) = u32x2_t{f2a_pack(a, b), f2a_pack(c, d)};
+}
 
-// PLAIN: queries and result are half [B, T, H, Dh]; otherwise the packed query buffer and the next GEMM's input.
-template <int DH, int QT, int FMT, bool PLAIN>
-__global__ __launch_bounds__(KV8_WAVES * 64, 2) void kv8_attn_kernel(Kv8Args p) {
-    constexpr int KS = DH / 16, DT = DH / 32, NW = KV8_WAVES, KB = DH / 32, VB = DH / 32, TILE = KB + VB;     // KB, VB: KiB of a tile's K and V codes
+// queries and tiles, or maxima, sums and O of one query tile
+static size_t kv8_lds_bytes(int Dh, int qt, int nw) { return std::max((size_t)qt * Dh * 64 + (size_t)nw * Dh * 128, (size_t)nw * 256 * qt + (size_t)nw * Dh * 128); }
+
+// AUX: cache policy of the K/V requests, 2 = nontemporal
+template <int DH, int QT, int NW, int FMT, int AUX>
+__global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8Args p) {
+    constexpr int KS = DH / 16, DT = DH / 32, KB = DH / 32, VB = DH / 32, TILE = KB + VB;     // KB, VB: KiB of a tile's K and V codes
     extern __shared__ float lds[];                          // queries [QT][KS], two tiles per wave [NW][2][TILE], of 1 KiB each; later sums
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hl = lane >> 5, col = lane & 31;
@@ -85,27 +115,12 @@ __global__ __launch_bounds__(KV8_WAVES * 64, 2) void kv8_attn_kernel(Kv8Args p) 
     if (group >= p.groups) return;
     const int b = group / H, h = group - b * H, qg = j % QG, key_wg = j / QG;
     const int units = p.key_wgs * NW, unit = key_wg * NW + wave;
-    const int L = p.seq_len[b], ns = p.n_sealed[b];
     const int32_t *t8 = p.table8 + (size_t)b * p.max_pages8, *t16 = p.table16 + (size_t)b * p.max_pages;
-    if (L < 0 || L + T > p.max_pages * 16 || ns < 0 || ns > (L >> 4) || ns > p.max_pages8) {     // uniform over the workgroup
-        if (tid == 0 && j == 0 && h == 0) atomicOr(p.flags, FLAG_CAPACITY);
-        return;
-    }
-    // ---- queries to LDS, in the order of the codes: block (i, e) holds, for half-wave hl, dims 32 i + 16 hl + 8 e .. + 7
-    u32x4_t *qs = reinterpret_cast<u32x4_t *>(lds);
-    for (int i = wave; i < QT * KS; i += NW) {
-        const int q = i / KS, blk = i % KS, i2 = blk >> 1, e = blk & 1;
-        int qtile = qg * QT + q;
-        if (qtile >= QTtot) qtile = QTtot - 1;               // a second tile behind the last query: the first one again, which nobody stores
-        u32x4_t v = {0u, 0u, 0u, 0u};
-        if (PLAIN) {
-            const int query = qtile * 32 + col;
-            if (query < T) v = *reinterpret_cast<const u32x4_t *>(reinterpret_cast<const a16_t *>(p.q) + ((size_t)(b * T + query) * H + h) * DH + 32 * i2 + 16 * hl + 8 * e);
-        } else {
-            v = p.q[((((size_t)b * H + h) * QTtot + qtile) * KS + 2 * i2 + hl) * 64 + e * 32 + col];
-        }
-        qs[i * 64 + lane] = v;
-    }
+    // ---- trip 1: whatever does not depend on the row's length.  Page ids of this wave's first 32 tiles, a page per lane (the table has max_pages8
+    // entries for every row; those past the sealed pages are not used), ancestor masks, queries
+    auto page_of = [&](int first) { return 2 * (unit + (first + (lane >> 1)) * units) + (lane & 1); };
+    auto page_id = [&](int lp) { return t8[min(lp, p.max_pages8 - 1)]; };
+    int ids = page_id(page_of(0));
     uint64_t anc[QT][2];
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
@@ -113,56 +128,112 @@ __global__ __launch_bounds__(KV8_WAVES * 64, 2) void kv8_attn_kernel(Kv8Args p) 
         anc[q][0] = anc[q][1] = 0ull;
         if (query < T) { anc[q][0] = p.tree->anc[query][0]; anc[q][1] = p.tree->anc[query][1]; }
     }
+    const int L = p.seq_len[b], ns = p.n_sealed[b];
+    // queries to LDS, in the order of the codes: block (i, e) holds, for half-wave hl, dims 32 i + 16 hl + 8 e .. + 7
+    u32x4_t *qs = reinterpret_cast<u32x4_t *>(lds);
+    constexpr int NQ = (QT * KS + NW - 1) / NW;
+    u32x4_t qreg[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        const int q = min(i * NW + wave, QT * KS - 1) / KS, blk = (i * NW + wave) % KS;
+        const int qtile = min(qg * QT + q, QTtot - 1);       // a second tile behind the last query: the first one again, which nobody stores
+        qreg[i] = query_piece<DH>(p, b, h, qtile, QTtot, col, 32 * (blk >> 1) + 16 * hl + 8 * (blk & 1));
+    }
+    if (L < 0 || L + T > p.max_pages * 16 || ns < 0 || ns > (L >> 4) || ns > p.max_pages8) {     // uniform over the workgroup
+        if (tid == 0 && j == 0 && h == 0) atomicOr(p.flags, FLAG_CAPACITY);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < NQ; ++i)
+        if (i * NW + wave < QT * KS) qs[(i * NW + wave) * 64 + lane] = qreg[i];
     const int total = L + T, n8 = (ns + 1) >> 1, first16 = ns * 16, n16 = (total - first16 + 31) >> 5, row_pages = (total + 15) >> 4;
     const int mine8 = unit < n8 ? (n8 - unit + units - 1) / units : 0;           // this wave's tiles of codes: unit, unit + units, ...
+    const int t0 = (unit - n8 % units + units) % units;      // and of the tail, which go on in the same turn: t0, t0 + units, ...
+    const bool tail = t0 < n16;
+    // pages outside the cache are replaced by page 0 and reported at the end: no branch between a page's number and the loads that it is for
+    bool bad = false;
+    auto page_in = [&](int page, int n_pages, bool used) {
+        const bool good = (unsigned)page < (unsigned)n_pages;
+        bad |= used && !good;
+        return good ? page : 0;
+    };
+    int a0, a1;
+    auto tail_pages = [&](int t) {                           // the second page may be missing: the first one is then read twice
+        const int lp = ns + 2 * t, r0 = t16[min(lp, p.max_pages - 1)], r1 = t16[min(lp + 1, p.max_pages - 1)];
+        const bool both = lp + 1 < row_pages;
+        a0 = page_in(r0, p.n_pages, t < n16);
+        a1 = both ? page_in(r1, p.n_pages, t < n16) : a0;
+    };
+    tail_pages(t0);
 
-    // ---- pages and scales of the wave's next 32 tiles, a page per lane
-    int pgs = 0;
-    float pk = 0.f, pv = 0.f, pr = 0.f;
-    auto page_ids = [&](int first) {
-        const int lp = 2 * (unit + (first + (lane >> 1)) * units) + (lane & 1);
+    // ---- trip 2: scales of the 32 tiles, and the first two tiles
+    int pgs;
+    float pk, pv, pr;
+    auto scales_of = [&](int lp) {
         const bool there = lp < ns;
-        pgs = there ? checked_page(t8[lp], p.n_pages8, p.flags) : -1;
-        const float2 s = reinterpret_cast<const float2 *>(p.scales)[((size_t)p.layer * p.n_pages8 + max(pgs, 0)) * H + h];
-        pk = there ? s.x * p.c : 0.f;                        // a page that is not there: exponent -infinity, weight 0
-        pv = there ? __builtin_amdgcn_logf(s.y) : -INFINITY;
-        pr = there ? 1.0f / s.y : 0.f;
+        const int page = page_in(ids, p.n_pages8, there);
+        pgs = there ? page : -1;
+        const float2 s = reinterpret_cast<const float2 *>(p.scales)[((size_t)p.layer * p.n_pages8 + page) * H + h];
+        pk = there ? s.x : 0.f;
+        pv = there ? s.y : 0.f;
+    };
+    auto scales_done = [&] {                                 // a page that is not there: exponent -infinity, weight 0
+        pk *= p.c;
+        pr = pv > 0.f ? __builtin_amdgcn_rcpf(pv) : 0.f;
+        pv = __builtin_amdgcn_logf(pv);
         asm volatile("" : "+v"(pgs), "+v"(pk), "+v"(pv), "+v"(pr));               // awaited here: nothing in the loop waits for an ordinary load
     };
-    page_ids(0);
+    scales_of(page_of(0));
 #pragma unroll
     for (int q = 0; q < QT; ++q) asm volatile("" : "+v"(anc[q][0]), "+v"(anc[q][1]));
 
     u32x4_t *mine = qs + (QT * KS + wave * 2 * TILE) * 64;
     const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)mine;
-    auto dma = [&](const void *src, int block) {
+    auto dma = [&](const char *src, int block) {
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
-                                         (__attribute__((address_space(3))) void *)(uintptr_t)(mine_at + (uint32_t)block * 1024u), 16, 0, 0);
-    };
-    // pages of tile `it`: the second one may be missing (then the first one is read twice), a tile behind the last one reads page 0
-    auto tile_pages = [&](int it, int &p0, int &p1) {
-        p0 = max(__builtin_amdgcn_readlane(pgs, 2 * (it & 31)), 0);
-        p1 = __builtin_amdgcn_readlane(pgs, 2 * (it & 31) + 1);
-        if (p1 < 0) p1 = p0;
+                                         (__attribute__((address_space(3))) void *)(uintptr_t)(mine_at + (uint32_t)block * 1024u), 16, 0, AUX);
     };
     auto lane_of = [](float v, int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)); };
     auto tile_scale = [&](int it) {
         const int l = 2 * (it & 31);
         return TileScale{lane_of(pk, l), lane_of(pk, l + 1), lane_of(pv, l), lane_of(pv, l + 1), lane_of(pr, l), lane_of(pr, l + 1)};
     };
-    auto request_k = [&](int p0, int p1, int slot) {
-        const uint8_t *kp = p.kcodes + kv8_block_base(p.layer, p.n_pages8, (col >> 4) ? p1 : p0, H, h, DH) + (hl * 16 + (col & 15)) * 16;
-#pragma unroll
-        for (int i = 0; i < KB; ++i) dma(kp + i * 512, slot * TILE + i);
+    auto tail_k = [&](int p0, int p1) {
+        return reinterpret_cast<const char *>(p.kpages + kv_block_base(p.layer, p.n_pages, (col >> 4) ? p1 : p0, H, h, DH)) + (hl * 16 + (col & 15)) * 16;
     };
-    auto request_v = [&](int p0, int p1, int slot) {
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const uint8_t *vp = p.vcodes + kv8_block_base(p.layer, p.n_pages8, g ? p1 : p0, H, h, DH) + lane * 16;
-#pragma unroll
-            for (int i = 0; i < VB / 2; ++i) dma(vp + i * 1024, slot * TILE + KB + g * (VB / 2) + i);
+    auto tail_v = [&](int page) { return reinterpret_cast<const char *>(p.vpages + kv_block_base(p.layer, p.n_pages, page, H, h, DH)) + (col * 2 + hl) * 16; };
+    // Half of what goes to a slot: K (part 0) or V (part 1) of tile `it` of codes; behind the last of those the first tile of the tail, its K as
+    // the next, its V as the one after it (K: 16 DH bytes in each half; V: a page in each half); then one and the same 16 bytes in every lane, so
+    // that the number of requests in flight is always the same.
+    auto request = [&](int it, int part) {
+        const char *a, *c;                                   // first and second half of the KB blocks
+        int step = 1024;
+        if (it < mine8) {
+            const int l = 2 * (it & 31), p0 = max(__builtin_amdgcn_readlane(pgs, l), 0), q1 = __builtin_amdgcn_readlane(pgs, l + 1), p1 = q1 < 0 ? p0 : q1;
+            if (part == 0) {
+                step = 512;
+                a = reinterpret_cast<const char *>(p.kcodes) + kv8_block_base(p.layer, p.n_pages8, (col >> 4) ? p1 : p0, H, h, DH) + (hl * 16 + (col & 15)) * 16;
+                c = a + KB / 2 * 512;
+            } else {
+                a = reinterpret_cast<const char *>(p.vcodes) + kv8_block_base(p.layer, p.n_pages8, p0, H, h, DH) + lane * 16;
+                c = reinterpret_cast<const char *>(p.vcodes) + kv8_block_base(p.layer, p.n_pages8, p1, H, h, DH) + lane * 16;
+            }
+        } else if (tail && it == mine8) {
+            step = 512;
+            a = tail_k(a0, a1) + part * KB * 512;
+            c = a + KB / 2 * 512;
+        } else if (tail && it == mine8 + 1) {
+            a = tail_v(part ? a1 : a0);
+            c = a + KB / 2 * 1024;
+        } else {
+            step = 0;
+            a = c = reinterpret_cast<const char *>(p.kcodes) + kv8_block_base(p.layer, p.n_pages8, 0, H, h, DH);
         }
+        const int to = (it & 1) * TILE + part * KB;
+#pragma unroll
+        for (int i = 0; i < KB; ++i) dma((i < KB / 2 ? a : c) + (i < KB / 2 ? i : i - KB / 2) * step, to + i);
     };
+    request(0, 0); request(0, 1); request(1, 0); request(1, 1);
     f32x16_t o[QT][DT];
 #pragma unroll
     for (int q = 0; q < QT; ++q)
@@ -173,19 +244,11 @@ __global__ __launch_bounds__(KV8_WAVES * 64, 2) void kv8_attn_kernel(Kv8Args p) 
     float m_run[QT], l_run[QT];
 #pragma unroll
     for (int q = 0; q < QT; ++q) { m_run[q] = -INFINITY; l_run[q] = 0.f; }
-    __syncthreads();                                         // the queries are in LDS
+    scales_done();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");              // the queries are in LDS; the tiles need not be
 
-    if (mine8 > 0) {
-        int p0, p1;
-        tile_pages(0, p0, p1); request_k(p0, p1, 0); request_v(p0, p1, 0);
-        tile_pages(min(1, mine8 - 1), p0, p1); request_k(p0, p1, 1); request_v(p0, p1, 1);
-    }
-    TileScale ts = tile_scale(0), next = tile_scale(1);
-    for (int it = 0; it < mine8; ++it) {
-        const int slot = it & 1;
-        const u32x4_t *tile = mine + slot * TILE * 64 + lane;
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(VB + TILE) : "memory");          // K has landed: younger are its V and the next tile
-        f32x16_t z[QT];
+    auto scores = [&](int it, f32x16_t (&z)[QT]) {          // S^T of tile `it`, whose K has landed
+        const u32x4_t *tile = mine + (it & 1) * TILE * 64 + lane;
 #pragma unroll
         for (int q = 0; q < QT; ++q)
 #pragma unroll
@@ -205,29 +268,14 @@ __global__ __launch_bounds__(KV8_WAVES * 64, 2) void kv8_attn_kernel(Kv8Args p) 
                 z[q] = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, kb), __builtin_bit_cast(a16x8_t, qs[at + (q * KS + 2 * i + 1) * 64]), z[q]);
             }
         }
-        // the tile after the next one; where it is the first of another 32, the loads of their pages end every wait
-        const int nx = it + 2;
-        int p0 = 0, p1 = 0;
-        if ((nx & 31) == 0 && nx < mine8) page_ids(nx);
-        if (nx < mine8) tile_pages(nx, p0, p1);
-        const TileScale after = tile_scale(nx);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K is read
-        request_k(p0, p1, slot);
-        u32x4_t pb[QT][2];
-#pragma unroll
-        for (int q = 0; q < QT; ++q) {
-            kv8_softmax<DT>(z[q], ts, m_run[q], l_run[q], o[q]);
-#pragma unroll
-            for (int g = 0; g < 2; ++g)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) pb[q][g][w] = half_pack(z[q][8 * g + 2 * w], z[q][8 * g + 2 * w + 1]);
-        }
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TILE + KB) : "memory");          // V has landed: younger are the next tile and another K
+    };
+    auto values = [&](int it, const u32x4_t (&pb)[QT][2]) { // O^T += V^T P^T of tile `it`, whose V has landed
+        const u32x4_t *tile = mine + ((it & 1) * TILE + KB) * 64 + lane;
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int i = 0; i < VB / 2; ++i) {
-                const u32x4_t w = tile[(KB + g * (VB / 2) + i) * 64];
+                const u32x4_t w = tile[(g * (VB / 2) + i) * 64];
                 uint32_t v[8];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) kv8_halves<FMT>(w[e], v[2 * e], v[2 * e + 1]);
@@ -238,70 +286,91 @@ __global__ __launch_bounds__(KV8_WAVES * 64, 2) void kv8_attn_kernel(Kv8Args p) 
                     o[q][2 * i + 1] = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, vb), __builtin_bit_cast(a16x8_t, pb[q][g]), o[q][2 * i + 1]);
                 }
             }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V is read
-        request_v(p0, p1, slot);
+    };
+    auto new_pages = [&](int it) {                           // tile `it` is the first of another 32: the loads of their pages end every wait
+        if ((it & 31) == 0 && it < mine8) {
+            ids = page_id(page_of(it));
+            scales_of(page_of(it));
+            scales_done();
+        }
+    };
+    TileScale ts = tile_scale(0), next = tile_scale(1);
+    for (int it = 0; it < mine8; ++it) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(VB + TILE) : "memory");      // K has landed: younger are its V and the next tile
+        f32x16_t z[QT];
+        u32x4_t pb[QT][2];
+        scores(it, z);
+        new_pages(it + 2);
+        const TileScale after = tile_scale(it + 2);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                    // K is read
+        request(it + 2, 0);
+#pragma unroll
+        for (int q = 0; q < QT; ++q) kv8_softmax<DT>(z[q], ts, m_run[q], l_run[q], o[q], pb[q]);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TILE + KB) : "memory");      // V has landed: younger are the next tile and another K
+        values(it, pb);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                    // V is read
+        request(it + 2, 1);
         ts = next;
         next = after;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // what was requested past the last tile has landed
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // the tail's first tile, or what was requested past the last one, has landed
 
-    // ---- the 16-bit tail: tiles n8, n8 + 1, ... in the same turn
+    // ---- the 16-bit tail: K in one slot, V in the other
     const TileScale one = {p.c, p.c, 0.f, 0.f, 1.f, 1.f};
-    for (int t = (unit - n8 % units + units) % units; t < n16; t += units) {
-        const int slot0 = first16 + t * 32, lp = ns + 2 * t;
-        const int p0 = checked_page(t16[lp], p.n_pages, p.flags);
-        const int p1 = lp + 1 < row_pages ? checked_page(t16[lp + 1], p.n_pages, p.flags) : p0;
-        u32x4_t w[KS];
-        const u32x4_t *kp = reinterpret_cast<const u32x4_t *>(p.kpages + kv_block_base(p.layer, p.n_pages, (col >> 4) ? p1 : p0, H, h, DH)) + hl * 16 + (col & 15);
+    for (int t = t0, sk = mine8 & 1; t < n16; t += units) {
+        if (t != t0) {                                       // a row with many pages that are not sealed
+            tail_pages(t);
+            const char *kp = tail_k(a0, a1), *v0 = tail_v(a0), *v1 = tail_v(a1);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                    // the tile before this one is read
 #pragma unroll
-        for (int s = 0; s < KS; ++s) w[s] = kp[s * 32];
+            for (int s = 0; s < KS; ++s) dma(kp + s * 512, sk * TILE + s);
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {                        // V to LDS, each lane its own pieces
-            const u32x4_t *vp = reinterpret_cast<const u32x4_t *>(p.vpages + kv_block_base(p.layer, p.n_pages, g ? p1 : p0, H, h, DH)) + col * 2 + hl;
+            for (int i = 0; i < DT; ++i) { dma(v0 + i * 1024, (sk ^ 1) * TILE + i); dma(v1 + i * 1024, (sk ^ 1) * TILE + DT + i); }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        const int slot0 = first16 + t * 32;
+        const u32x4_t *kt = mine + sk * TILE * 64 + lane, *vt = mine + (sk ^ 1) * TILE * 64 + lane;
+        f32x16_t z[QT];
+        u32x4_t pb[QT][2];
+#pragma unroll
+        for (int q = 0; q < QT; ++q)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) z[q][v] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {                       // 16-bit K has dims 16 s + 8 hl in step s: block (s / 2, e = hl), its half-wave s % 2
+            const a16x8_t k = __builtin_bit_cast(a16x8_t, kt[s * 64]);
+#pragma unroll
+            for (int q = 0; q < QT; ++q)
+                z[q] = HYDRA_MFMA16(k, __builtin_bit_cast(a16x8_t, qs[(q * KS + (s & ~1) + hl) * 64 + (s & 1) * 32 + col]), z[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+            const uint32_t seen = keys_seen(slot0, L, anc[q][0], anc[q][1]) >> (4 * hl);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) z[q][v] = (seen >> (8 * (v >> 2) + (v & 3))) & 1u ? z[q][v] : -INFINITY;
+            kv8_softmax<DT>(z[q], one, m_run[q], l_run[q], o[q], pb[q]);
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
             u32x4_t keep;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                // dword e holds keys i = 2e, 2e+1 of this half-wave: token = 8*(i/4) + 4*hl + i%4.  Slots past the last node become 0: stale contents
+                // dword e holds keys i = 2e, 2e+1 of this half-wave: token = 8*(i/4) + 4*hl + i%4.  V of slots past the last node becomes 0: stale contents
                 const int i0 = 2 * e, i1 = 2 * e + 1;
                 const int s0 = slot0 + 16 * g + 8 * (i0 >> 2) + 4 * hl + (i0 & 3);
                 const int s1 = slot0 + 16 * g + 8 * (i1 >> 2) + 4 * hl + (i1 & 3);
                 keep[e] = (s0 < total ? 0x0000ffffu : 0u) | (s1 < total ? 0xffff0000u : 0u);
             }
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) mine[(g * DT + dt) * 64 + lane] = vp[dt * 64] & keep;
-        }
-        f32x16_t z[QT];
-#pragma unroll
-        for (int q = 0; q < QT; ++q)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) z[q][v] = 0.f;
-#pragma unroll
-        for (int s = 0; s < KS; ++s)                         // 16-bit K has dims 16 s + 8 hl in step s: block (s / 2, e = hl), its half-wave s % 2
-#pragma unroll
-            for (int q = 0; q < QT; ++q)
-                z[q] = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, w[s]), __builtin_bit_cast(a16x8_t, qs[(q * KS + (s & ~1) + hl) * 64 + (s & 1) * 32 + col]), z[q]);
-#pragma unroll
-        for (int q = 0; q < QT; ++q) {
-            const uint32_t seen = keys_seen(slot0, L, anc[q][0], anc[q][1]) >> (4 * hl);
-#pragma unroll
-            for (int v = 0; v < 16; ++v) z[q][v] = (seen >> (8 * (v >> 2) + (v & 3))) & 1u ? z[q][v] : -INFINITY;
-            kv8_softmax<DT>(z[q], one, m_run[q], l_run[q], o[q]);
-        }
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            u32x4_t pb[QT];
-#pragma unroll
-            for (int q = 0; q < QT; ++q)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) pb[q][e] = half_pack(z[q][8 * g + 2 * e], z[q][8 * g + 2 * e + 1]);
-#pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
-                const a16x8_t v = __builtin_bit_cast(a16x8_t, mine[(g * DT + dt) * 64 + lane]);
+                const a16x8_t v = __builtin_bit_cast(a16x8_t, vt[(g * DT + dt) * 64] & keep);
 #pragma unroll
-                for (int q = 0; q < QT; ++q) o[q][dt] = HYDRA_MFMA16(v, __builtin_bit_cast(a16x8_t, pb[q]), o[q][dt]);
+                for (int q = 0; q < QT; ++q) o[q][dt] = HYDRA_MFMA16(v, __builtin_bit_cast(a16x8_t, pb[q][g]), o[q][dt]);
             }
         }
     }
+
+    if (__any(bad) && lane == 0) atomicOr(p.flags, FLAG_BAD_PAGE);
 
     // ---- merge the waves through LDS, one query tile after the other: maxima and sums [QT][NW][2][32], then O[NW][DT * 16][64]
     __syncthreads();                                         // every wave is done with queries and tiles
@@ -351,9 +420,7 @@ __global__ __launch_bounds__(KV8_WAVES * 64, 2) void kv8_attn_kernel(Kv8Args p) 
             if (p.key_wgs > 1) {
                 *reinterpret_cast<f32x4_t *>(rec + (size_t)query * DH + dim) = f32x4_t{acc[0], acc[1], acc[2], acc[3]};
             } else if (query < T) {
-                const u32x2_t pk2 = {f2a_pack(acc[0] * inv, acc[1] * inv), f2a_pack(acc[2] * inv, acc[3] * inv)};
-                a16_t *to = reinterpret_cast<a16_t *>(p.out) + (PLAIN ? ((size_t)m * H + h) * DH + dim : x_index<true>(m, h * DH + dim, H * DH));
-                *reinterpret_cast<u32x2_t *>(to) = pk2;
+                store_result<DH>(p, m, h, dim, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
             }
         }
         if (p.key_wgs > 1 && wave == 0 && hl == 0) {
@@ -364,11 +431,239 @@ __global__ __launch_bounds__(KV8_WAVES * 64, 2) void kv8_attn_kernel(Kv8Args p) 
     }
 }
 
+// Short contexts: a workgroup takes one 32-query tile of one (row, head) and 1 / DS of the head's dims, its eight waves split the keys and meet in LDS,
+// and the result goes straight out.  A chain of round trips, so everything that can be is requested at once: the page ids before the length
+// is known, then all tiles of a wave (20 registers each with DS = 4) and the first tile of its tail.
+enum { KV8_SHORT_WAVES = 8, KV8_SHORT_TILES = 5 };
+template <int DH, int DS>
+struct Short8 { u32x4_t k[DH / 32]; uint32_t v[2][DH / DS / 16]; };       // V: 8 bytes for each 32 dims of a page
+
+template <int DH, int DS>
+struct ShortTail { u32x4_t k[DH / 16]; u32x4_t v[2][DH / 32 / DS]; };
+
+static size_t kv8_short_lds_bytes(int Dh, int ds) {
+    return ((size_t)KV8_SHORT_WAVES * 64 + std::max((size_t)KV8_SHORT_WAVES * (Dh / 32 / ds) * 16 * 64, (size_t)Dh * 16)) * 4;       // O, or the query tile
+}
+
+template <int DH, int DS, int FMT>
+__global__ __launch_bounds__(KV8_SHORT_WAVES * 64, 2) void kv8_short_kernel(Kv8Args p) {
+    constexpr int KS = DH / 16, KB = DH / 32, DT = DH / 32 / DS, NW = KV8_SHORT_WAVES, RING = DT == 4 ? 2 : 4;
+    extern __shared__ float lds[];                          // [NW][2][32] maxima and sums, then the query tile and later O[NW][DT * 16][64]
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hl = lane >> 5, col = lane & 31;
+    const int T = p.T, H = p.H;
+    const int QTtot = (T + 31) >> 5, per = QTtot * DS;
+    const int seq = (int)blockIdx.x >> 3;
+    const int group = seq / per * 8 + ((int)blockIdx.x & 7), j = seq % per;
+    if (group >= p.groups) return;
+    const int b = group / H, h = group - b * H, qtile = j / DS, ds = j % DS;
+    const int32_t *t8 = p.table8 + (size_t)b * p.max_pages8, *t16 = p.table16 + (size_t)b * p.max_pages;
+    u32x4_t *qs = reinterpret_cast<u32x4_t *>(lds + NW * 64);
+    const int query = qtile * 32 + col;
+    uint64_t anc0 = 0ull, anc1 = 0ull;
+    if (query < T) { anc0 = p.tree->anc[query][0]; anc1 = p.tree->anc[query][1]; }
+    int pg[RING][2];                                        // the table has max_pages8 entries for every row; those past the sealed pages are not used
+#pragma unroll
+    for (int i = 0; i < RING; ++i) {
+        const int t = wave + i * NW;
+        pg[i][0] = t8[min(2 * t, p.max_pages8 - 1)];
+        pg[i][1] = t8[min(2 * t + 1, p.max_pages8 - 1)];
+    }
+    const int L = p.seq_len[b], ns = p.n_sealed[b];
+    if (wave < KS) qs[wave * 64 + lane] = query_piece<DH>(p, b, h, qtile, QTtot, col, 32 * (wave >> 1) + 16 * hl + 8 * (wave & 1));
+    if (L < 0 || L + T > p.max_pages * 16 || ns < 0 || ns > (L >> 4) || ns > p.max_pages8) {     // uniform over the workgroup
+        if (tid == 0 && j == 0 && h == 0) atomicOr(p.flags, FLAG_CAPACITY);
+        return;
+    }
+    const int total = L + T, n8 = (ns + 1) >> 1, first16 = ns * 16, n16 = (total - first16 + 31) >> 5, row_pages = (total + 15) >> 4;
+    const int mine8 = wave < n8 ? (n8 - wave + NW - 1) / NW : 0;               // tiles of codes wave, wave + NW, ...; the tail's go on in the same turn
+    const int t0 = (wave - n8 % NW + NW) % NW;
+    const bool tail = t0 < n16;
+
+    // Loads are never behind a condition: a tile past the last one reads one and the same piece of page 0 in every lane.
+    auto load8 = [&](Short8<DH, DS> &kv, TileScale &ts, int it, int p0, int p1) {
+        const int t = wave + it * NW;
+        const bool live = t < n8, both = 2 * t + 1 < ns;
+        p0 = live ? checked_page(p0, p.n_pages8, p.flags) : 0;
+        p1 = both ? checked_page(p1, p.n_pages8, p.flags) : p0;
+        const int ln = live ? lane : 0, lh = ln >> 5, lc = ln & 31;
+        const float2 *sc = reinterpret_cast<const float2 *>(p.scales);
+        const float2 s0 = sc[((size_t)p.layer * p.n_pages8 + p0) * H + h], s1 = sc[((size_t)p.layer * p.n_pages8 + p1) * H + h];
+        ts.k0 = s0.x; ts.k1 = s1.x; ts.v0 = s0.y; ts.v1 = s1.y;                // raw; see scale8
+        const uint8_t *kp = p.kcodes + kv8_block_base(p.layer, p.n_pages8, (lc >> 4) ? p1 : p0, H, h, DH) + (lh * 16 + (lc & 15)) * 16;
+#pragma unroll
+        for (int i = 0; i < KB; ++i) kv.k[i] = *reinterpret_cast<const u32x4_t *>(kp + i * 512);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const uint8_t *vp = p.vcodes + kv8_block_base(p.layer, p.n_pages8, g ? p1 : p0, H, h, DH) + ln * 16;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const int d = ds * DT + dt;                  // (the 32 dims' place in the head)
+                const u32x2_t w = *reinterpret_cast<const u32x2_t *>(vp + (d >> 1) * 1024 + (d & 1) * 8);
+                kv.v[g][2 * dt] = w[0]; kv.v[g][2 * dt + 1] = w[1];
+            }
+        }
+    };
+    auto scale8 = [&](TileScale &ts, int it) {
+        const bool both = 2 * (wave + it * NW) + 1 < ns;     // a page that is not there: exponent -infinity, weight 0
+        const float v0 = ts.v0, v1 = ts.v1;
+        ts.k0 *= p.c;
+        ts.v0 = __builtin_amdgcn_logf(v0);
+        ts.r0 = __builtin_amdgcn_rcpf(v0);
+        ts.k1 = both ? ts.k1 * p.c : 0.f;
+        ts.v1 = both ? __builtin_amdgcn_logf(v1) : -INFINITY;
+        ts.r1 = both ? __builtin_amdgcn_rcpf(v1) : 0.f;
+    };
+    f32x16_t o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[dt][v] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    auto step8 = [&](const Short8<DH, DS> &kv, TileScale ts, int it) {
+        f32x16_t z;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) z[v] = 0.f;
+        int at = lane;
+        asm volatile("" : "+v"(at));                         // keeps the reads of the queries here (hoisted, they are registers)
+#pragma unroll
+        for (int i = 0; i < KB; ++i) {
+            uint32_t k[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kv8_halves<FMT>(kv.k[i][e], k[2 * e], k[2 * e + 1]);
+            const u32x4_t ka = {k[0], k[1], k[2], k[3]}, kb = {k[4], k[5], k[6], k[7]};
+            z = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, ka), __builtin_bit_cast(a16x8_t, qs[at + 2 * i * 64]), z);
+            z = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, kb), __builtin_bit_cast(a16x8_t, qs[at + (2 * i + 1) * 64]), z);
+        }
+        scale8(ts, it);
+        u32x4_t pb[2];
+        kv8_softmax<DT>(z, ts, m_run, l_run, o, pb);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                uint32_t v[4];
+                kv8_halves<FMT>(kv.v[g][2 * dt], v[0], v[1]);
+                kv8_halves<FMT>(kv.v[g][2 * dt + 1], v[2], v[3]);
+                const u32x4_t va = {v[0], v[1], v[2], v[3]};
+                o[dt] = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, va), __builtin_bit_cast(a16x8_t, pb[g]), o[dt]);
+            }
+        }
+    };
+    // the 16-bit tail
+    auto load16 = [&](ShortTail<DH, DS> &kv, int t, int p0, int p1, bool live) {
+        p0 = live ? checked_page(p0, p.n_pages, p.flags) : 0;
+        p1 = live && ns + 2 * t + 1 < row_pages ? checked_page(p1, p.n_pages, p.flags) : p0;
+        const int ln = live ? lane : 0, lh = ln >> 5, lc = ln & 31;
+        const u32x4_t *kp = reinterpret_cast<const u32x4_t *>(p.kpages + kv_block_base(p.layer, p.n_pages, (lc >> 4) ? p1 : p0, H, h, DH)) + lh * 16 + (lc & 15);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) kv.k[s] = kp[s * 32];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const u32x4_t *vp = reinterpret_cast<const u32x4_t *>(p.vpages + kv_block_base(p.layer, p.n_pages, g ? p1 : p0, H, h, DH)) + lc * 2 + lh;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) kv.v[g][dt] = vp[(ds * DT + dt) * 64];
+        }
+    };
+    auto step16 = [&](ShortTail<DH, DS> &kv, int t) {
+        const TileScale one = {p.c, p.c, 0.f, 0.f, 1.f, 1.f};
+        const int slot0 = first16 + t * 32;
+        f32x16_t z;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) z[v] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)                         // 16-bit K has dims 16 s + 8 hl in step s: block (s / 2, e = hl), its half-wave s % 2
+            z = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, kv.k[s]), __builtin_bit_cast(a16x8_t, qs[((s & ~1) + hl) * 64 + (s & 1) * 32 + col]), z);
+        const uint32_t seen = keys_seen(slot0, L, anc0, anc1) >> (4 * hl);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) z[v] = (seen >> (8 * (v >> 2) + (v & 3))) & 1u ? z[v] : -INFINITY;
+        u32x4_t pb[2];
+        kv8_softmax<DT>(z, one, m_run, l_run, o, pb);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            u32x4_t keep;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                // dword e holds keys i = 2e, 2e+1 of this half-wave: token = 8*(i/4) + 4*hl + i%4.  V of slots past the last node becomes 0: stale contents
+                const int i0 = 2 * e, i1 = 2 * e + 1;
+                const int s0 = slot0 + 16 * g + 8 * (i0 >> 2) + 4 * hl + (i0 & 3);
+                const int s1 = slot0 + 16 * g + 8 * (i1 >> 2) + 4 * hl + (i1 & 3);
+                keep[e] = (s0 < total ? 0x0000ffffu : 0u) | (s1 < total ? 0xffff0000u : 0u);
+            }
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+                o[dt] = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, kv.v[g][dt] & keep), __builtin_bit_cast(a16x8_t, pb[g]), o[dt]);
+        }
+    };
+    const int lp0 = ns + 2 * t0;
+    const int a0 = t16[min(lp0, p.max_pages - 1)], a1 = t16[min(lp0 + 1, p.max_pages - 1)];
+    Short8<DH, DS> ring[RING];
+    TileScale rs[RING];
+#pragma unroll
+    for (int i = 0; i < RING; ++i) load8(ring[i], rs[i], i, pg[i][0], pg[i][1]);
+    ShortTail<DH, DS> last;
+    load16(last, t0, a0, a1, tail);
+    __syncthreads();                                         // the query tile is in LDS
+    int it = 0;
+    for (; it + RING < mine8; it += RING)                    // all of the ring's tiles exist
+#pragma unroll
+        for (int i = 0; i < RING; ++i) {
+            const int next = it + i + RING, t = wave + next * NW;
+            const int p0 = t8[min(2 * t, p.max_pages8 - 1)], p1 = t8[min(2 * t + 1, p.max_pages8 - 1)];
+            step8(ring[i], rs[i], it + i);
+            load8(ring[i], rs[i], next, p0, p1);
+        }
+#pragma unroll
+    for (int i = 0; i < RING; ++i)
+        if (it + i < mine8) step8(ring[i], rs[i], it + i);
+    if (tail) step16(last, t0);
+    for (int t = t0 + NW; t < n16; t += NW) {                // a row with many pages that are not sealed
+        const int lp = ns + 2 * t;
+        load16(last, t, t16[lp], t16[min(lp + 1, p.max_pages - 1)], true);
+        step16(last, t);
+    }
+
+    // ---- merge the waves through LDS: ml[NW][2][32], then O[NW][DT * 16][64] where the queries were
+    float *ml = lds, *ob = lds + NW * 64;
+    const HalfWaves lh2 = half_waves(l_run);                 // each half-wave has summed its own keys
+    if (hl == 0) {
+        ml[(wave * 2 + 0) * 32 + col] = m_run;
+        ml[(wave * 2 + 1) * 32 + col] = lh2.lo + lh2.hi;
+    }
+    __syncthreads();
+    float m_tot = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m_tot = fmaxf(m_tot, ml[(w * 2 + 0) * 32 + col]);
+    const float m_safe = m_tot == -INFINITY ? 0.f : m_tot;
+    float l_tot = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) l_tot += __builtin_amdgcn_exp2f(ml[(w * 2 + 0) * 32 + col] - m_safe) * ml[(w * 2 + 1) * 32 + col];
+    const float f = __builtin_amdgcn_exp2f(m_run - m_safe);
+    float *dst = ob + (size_t)wave * DT * 16 * 64 + lane;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) dst[(dt * 16 + v) * 64] = o[dt][v] * f;
+    __syncthreads();
+    // the (band, group of 4 registers = 4 consecutive dims) items are shared out over the waves
+    const float inv = 1.0f / l_tot;
+    for (int id = wave; id < DT * 4; id += NW) {
+        const int dt = id >> 2, g4 = id & 3;
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float *src = ob + (size_t)w * DT * 16 * 64 + lane;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[q] += src[(dt * 16 + 4 * g4 + q) * 64];
+        }
+        if (query < T) store_result<DH>(p, b * T + query, h, 32 * (ds * DT + dt) + 8 * g4 + 4 * hl, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    }
+}
+
 // out = sum_u 2^(M_u - M) O_u / sum_u 2^(M_u - M) l_u over the records of a head: one thread per (query, 4 dims), all its loads in one round trip.
 enum { KV8_MERGE_MAX = 16 };
-template <bool PLAIN>
 __global__ __launch_bounds__(256) void kv8_merge_kernel(const float *__restrict__ apart, const int32_t *__restrict__ seq_len, const int32_t *__restrict__ n_sealed,
-                                                         int T, int H, int Dh, int units, int max_pages, int max_pages8, void *out) {
+                                                         int T, int H, int Dh, int units, int max_pages, int max_pages8, int plain, void *out) {
     const int h = blockIdx.y, b = blockIdx.z;
     const int per_q = Dh >> 2;
     const int n = blockIdx.x * (256 / per_q) + threadIdx.x / per_q;
@@ -405,51 +700,83 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(const float *__restrict_
     const float inv = 1.0f / den;
     const int m = b * T + n;
     const u32x2_t pk = {f2a_pack(acc[0] * inv, acc[1] * inv), f2a_pack(acc[2] * inv, acc[3] * inv)};
-    a16_t *to = reinterpret_cast<a16_t *>(out) + (PLAIN ? ((size_t)m * H + h) * Dh + dim : x_index<true>(m, h * Dh + dim, H * Dh));
+    a16_t *to = reinterpret_cast<a16_t *>(out) + (plain ? ((size_t)m * H + h) * Dh + dim : x_index<true>(m, h * Dh + dim, H * Dh));
     *reinterpret_cast<u32x2_t *>(to) = pk;
 }
 
-#define KV8_EACH(X) X(128, 1, KV8_INT8) X(128, 2, KV8_INT8) X(128, 1, KV8_E4M3) X(128, 2, KV8_E4M3) X(64, 1, KV8_INT8) X(64, 2, KV8_INT8) X(64, 1, KV8_E4M3) X(64, 2, KV8_E4M3)
+// (query tiles of a wave, waves, request policy) that the rules below choose from
+#define KV8_EACH_OF(X, DHv, Fv) X(DHv, 1, 8, Fv, 0) X(DHv, 1, 4, Fv, 2) X(DHv, 2, 8, Fv, 0) X(DHv, 2, 8, Fv, 2) X(DHv, 2, 4, Fv, 0) X(DHv, 2, 4, Fv, 2)
+#define KV8_EACH(X)                                                                                                                     \
+    KV8_EACH_OF(X, 128, KV8_INT8) KV8_EACH_OF(X, 128, KV8_E4M3) KV8_EACH_OF(X, 64, KV8_INT8) KV8_EACH_OF(X, 64, KV8_E4M3)               \
+    X(64, 1, 8, KV8_INT8, 2) X(64, 1, 8, KV8_E4M3, 2)
+#define KV8_SHORT_EACH(X)                                                                                                               \
+    X(128, 1, KV8_INT8) X(128, 2, KV8_INT8) X(128, 4, KV8_INT8) X(128, 1, KV8_E4M3) X(128, 2, KV8_E4M3) X(128, 4, KV8_E4M3)             \
+    X(64, 1, KV8_INT8) X(64, 2, KV8_INT8) X(64, 1, KV8_E4M3) X(64, 2, KV8_E4M3)
 
 int kv8_max_dynamic_lds() {
     hipError_t e = hipSuccess;
-#define ATTR(DHv, QTv, Fv)                                                                                                                                      \
-    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)kv8_attn_kernel<DHv, QTv, Fv, true>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);     \
-    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)kv8_attn_kernel<DHv, QTv, Fv, false>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+#define ATTR(DHv, QTv, NWv, Fv, AUXv) \
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)kv8_attn_kernel<DHv, QTv, NWv, Fv, AUXv>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     KV8_EACH(ATTR)
+#undef ATTR
+#define ATTR(DHv, DSv, Fv) \
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)kv8_short_kernel<DHv, DSv, Fv>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    KV8_SHORT_EACH(ATTR)
 #undef ATTR
     if (e != hipSuccess) return hip_fail(e, "hipFuncSetAttribute(8-bit attention kernels)");
     return HYDRA_OK;
 }
 
-int launch_kv8_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const void *q, bool q_plain, const int32_t *seq_len, const hydra_kv8 *kv,
-                         float *apart, int units_max, void *out, bool out_plain, int32_t *flags) {
-    (void)out_plain;                                         // queries and result are plain together or packed together
+int launch_kv8_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const void *q, bool plain, const int32_t *seq_len, const hydra_kv8 *kv,
+                         float *apart, int units_max, void *out, int32_t *flags) {
     const int T = c->tree.T, H = c->m.n_heads, Dh = c->m.head_dim;
-    const int QTtot = ceil_div(T, 32), qt = QTtot > 1 ? 2 : 1, qgroups = ceil_div(QTtot, qt);
+    const int QTtot = ceil_div(T, 32);
     const int len = kv->tail.seq_len_hint > 0 ? kv->tail.seq_len_hint : c->m.max_pos;
-    const int tiles = ceil_div(len + T, 32) + 1, hb = H * B * qgroups;
-    const int wgs = std::max(1, std::min({ceil_div(tiles, KV8_WAVES * 2), std::max(1, 256 / hb), units_max, (int)KV8_MERGE_MAX}));
+    const int tiles = ceil_div(len + T, 32) + 1;
     Kv8Args a;
     a.q = (const u32x4_t *)q; a.kcodes = (const uint8_t *)kv->k_codes; a.vcodes = (const uint8_t *)kv->v_codes; a.scales = kv->scales;
     a.table8 = kv->page_table; a.n_sealed = kv->n_sealed; a.kpages = (const a16_t *)kv->tail.k_pages; a.vpages = (const a16_t *)kv->tail.v_pages;
     a.table16 = kv->tail.page_table; a.seq_len = seq_len; a.tree = tree_dev(c); a.apart = apart; a.out = out; a.flags = flags;
     a.max_pages8 = kv->max_pages; a.n_pages8 = kv->n_pages; a.max_pages = kv->tail.max_pages; a.n_pages = kv->tail.n_pages; a.layer = layer;
-    a.T = T; a.H = H; a.groups = H * B; a.key_wgs = wgs; a.c = LOG2E / sqrtf((float)Dh);
-    const dim3 grid(ceil_div(H * B, 8) * 8 * qgroups * wgs), block(KV8_WAVES * 64);
-    const size_t lds = kv8_lds_bytes(Dh, qt);
-#define LAUNCH(DHv, QTv, Fv)                                                                                                     \
-    if (Dh == DHv && qt == QTv && kv->format == Fv) {                                                                            \
-        if (q_plain) hipLaunchKernelGGL((kv8_attn_kernel<DHv, QTv, Fv, true>), grid, block, lds, s, a);                          \
-        else         hipLaunchKernelGGL((kv8_attn_kernel<DHv, QTv, Fv, false>), grid, block, lds, s, a);                         \
+    a.T = T; a.H = H; a.groups = H * B; a.plain = plain ? 1 : 0; a.c = LOG2E / sqrtf((float)Dh);
+    // Up to 40 key tiles, while a workgroup per (row, head, 32-query tile) fits one round of the chip: no records and no merge, and the head's
+    // dims shared out over more workgroups while those fit the round too (us: 64 nodes behind 777 tokens, 32 heads 10.0 / 10.7 / 13.8 with 4 / 2 / 1
+    // shares, 16.7 with records and merge; 4 rows of it 19.1 against 24.0; beyond one round 16 rows of 400 tokens 40 against 26).
+    if (tiles <= KV8_SHORT_WAVES * KV8_SHORT_TILES && QTtot * H * B <= 256) {
+        int ds = Dh / 32;
+        while (ds > 1 && QTtot * H * B * ds > 256) ds >>= 1;
+        a.key_wgs = 1;
+        const dim3 grid(ceil_div(H * B, 8) * 8 * QTtot * ds), block(KV8_SHORT_WAVES * 64);
+#define LAUNCH(DHv, DSv, Fv) \
+        if (Dh == DHv && ds == DSv && kv->format == Fv) hipLaunchKernelGGL((kv8_short_kernel<DHv, DSv, Fv>), grid, block, kv8_short_lds_bytes(DHv, DSv), s, a);
+        KV8_SHORT_EACH(LAUNCH)
+#undef LAUNCH
+        HYDRA_LAUNCH_CHECK("kv8_short_kernel");
+        return HYDRA_OK;
     }
+    // Beyond that the keys of a head are split over waves and, while the chip has room, over workgroups.
+    //   query tiles of a wave: one while a workgroup for each fits one round (a tile then takes half as long and K/V come from L2 the second time: 64
+    //     nodes, 32 heads, 2000 / 8000 tokens 14.6 / 27.4 us against 18.9 / 27.3, 4 rows of 2048 25.8 against 30.2), two beyond (16 rows of 2048 61.2
+    //     against 73.8)
+    //   waves of a workgroup: eight; four with more (row, head, query group)s than CUs, two or more workgroups to a CU, so that one's first
+    //     round trips and merge lie under another's stream (16 rows of 2048 61.2 against 70.4; 8 rows of 128 nodes 30.3 against 39.7), and for up to 32 nodes with
+    //     128 dims (32003 tokens, 40 heads 57.8 against 63.2; 8000 tokens 19.4 against 21.2; with 64 dims 17.2 against 16.2)
+    const int qt = QTtot > 1 && H * B * QTtot > 256 ? 2 : 1, qgroups = ceil_div(QTtot, qt), hb = H * B * qgroups;
+    const int nw = hb > 256 || (Dh == 128 && QTtot == 1) ? 4 : 8;
+    const int wgs = std::max(1, std::min({ceil_div(tiles, nw * 2), std::max(1, 256 / hb), units_max, (int)KV8_MERGE_MAX}));
+    a.key_wgs = wgs;
+    // K and V that one workgroup alone reads are requested nontemporal (32003 tokens 63.8 -> 57.8 us, 16 rows of 2048 and 32 nodes 60.3 -> 56.8)
+    const int aux = qgroups == 1 ? 2 : 0;
+    const dim3 grid(ceil_div(H * B, 8) * 8 * qgroups * wgs), block(nw * 64);
+    const size_t lds = kv8_lds_bytes(Dh, qt, nw);
+#define LAUNCH(DHv, QTv, NWv, Fv, AUXv) \
+    if (Dh == DHv && qt == QTv && nw == NWv && kv->format == Fv && aux == AUXv) hipLaunchKernelGGL((kv8_attn_kernel<DHv, QTv, NWv, Fv, AUXv>), grid, block, lds, s, a);
     KV8_EACH(LAUNCH)
 #undef LAUNCH
     HYDRA_LAUNCH_CHECK("kv8_attn_kernel");
     if (wgs > 1) {
         const dim3 mgrid(ceil_div(T, 256 / (Dh / 4)), H, B), mblock(256);
-        if (q_plain) hipLaunchKernelGGL(kv8_merge_kernel<true>, mgrid, mblock, 0, s, apart, seq_len, kv->n_sealed, T, H, Dh, wgs, kv->tail.max_pages, kv->max_pages, out);
-        else         hipLaunchKernelGGL(kv8_merge_kernel<false>, mgrid, mblock, 0, s, apart, seq_len, kv->n_sealed, T, H, Dh, wgs, kv->tail.max_pages, kv->max_pages, out);
+        hipLaunchKernelGGL(kv8_merge_kernel, mgrid, mblock, 0, s, apart, seq_len, kv->n_sealed, T, H, Dh, wgs, kv->tail.max_pages, kv->max_pages, a.plain, out);
         HYDRA_LAUNCH_CHECK("kv8_merge_kernel");
     }
     return HYDRA_OK;
