@@ -117,7 +117,9 @@ __global__ __launch_bounds__(256) void kv8_sealed_kernel(const int32_t *__restri
 
 int launch_kv8_seal(hydra_ctx *c, hipStream_t s, int B, const int32_t *seq_len, const hydra_kv8 *kv) {
     const int H = c->m.n_heads, Dh = c->m.head_dim;
-    const dim3 grid(std::max(1, ceil_div((c->tree.T / 16 + 1) * H * 2, 4)), c->m.n_layers, B), block(256);
+    // as many waves as a step of the context's tree can complete pages (a row with more of them goes round); with twice as many, half of them without
+    // work, 16 rows x 8 layers of a page each took 19 us instead of 15
+    const dim3 grid(ceil_div(ceil_div(c->tree.T, 16) * H * 2, 4), c->m.n_layers, B), block(256);
 #define SEAL(DHv, Fv)                                                                                                                              \
     hipLaunchKernelGGL((kv8_seal_kernel<DHv, Fv>), grid, block, 0, s, (const a16_t *)kv->tail.k_pages, (const a16_t *)kv->tail.v_pages,            \
                        kv->tail.page_table, kv->tail.max_pages, kv->tail.n_pages, (uint8_t *)kv->k_codes, (uint8_t *)kv->v_codes, kv->scales,      \
@@ -132,49 +134,82 @@ int launch_kv8_seal(hydra_ctx *c, hipStream_t s, int B, const int32_t *seq_len, 
     return HYDRA_OK;
 }
 
-// Plain values of the slots first .. first + n - 1: one workgroup per logical page, head and (layer, row).
-template <int FMT>
+// Plain values of the slots first .. first + n - 1: one wave per logical page, head and K or V.  Bound by the stores (four bytes for each code read),
+// so a lane always holds four consecutive dims of a token and 32 (16) lanes write a token's whole 512 (256) bytes.
+template <int DH, int FMT>
 __global__ __launch_bounds__(256) void kv8_read_kernel(const a16_t *__restrict__ kpages, const a16_t *__restrict__ vpages,
                                                         const int32_t *__restrict__ table16, int max_pages, int n_pages,
                                                         const uint8_t *__restrict__ kcodes, const uint8_t *__restrict__ vcodes, const float *__restrict__ scales,
                                                         const int32_t *__restrict__ table8, int max_pages8, int n_pages8, const int32_t *__restrict__ n_sealed,
-                                                        int layer0, int B, int first, int n, int H, int Dh, float *__restrict__ plain, int32_t *flags) {
-    const int i = (first >> 4) + (int)blockIdx.x, h = blockIdx.y, b = (int)blockIdx.z % B, l = (int)blockIdx.z / B, layer = layer0 + l;
+                                                        int layer0, int B, int first, int n, int H, float *__restrict__ plain, int32_t *flags) {
+    constexpr int QUADS = DH / 4, TOKS = 64 / QUADS;         // lanes of a token, tokens of a wave's store
+    const int lane = threadIdx.x & 63, task = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kv = task & 1, h = (task >> 1) % H, i = (first >> 4) + (task >> 1) / H, b = (int)blockIdx.y, l = (int)blockIdx.z, layer = layer0 + l;
+    if (i > (first + n - 1) >> 4) return;
     const bool sealed = i < min(n_sealed[b], max_pages8);
     const int page = sealed ? table8[(size_t)b * max_pages8 + i] : table16[(size_t)b * max_pages + i];
     if ((unsigned)page >= (unsigned)(sealed ? n_pages8 : n_pages)) {
-        if (threadIdx.x == 0) atomicOr(flags, FLAG_BAD_PAGE);
+        if (lane == 0) atomicOr(flags, FLAG_BAD_PAGE);
         return;
     }
-    const size_t base = sealed ? kv8_block_base(layer, n_pages8, page, H, h, Dh) : kv_block_base(layer, n_pages, page, H, h, Dh);
-    const int quads = Dh >> 2;
-    for (int it = threadIdx.x; it < 32 * quads; it += 256) {
-        const int dim = it % quads * 4, kv = it / quads & 1, tok = it / quads >> 1;
+    const int dim = lane % QUADS * 4, t0 = lane / QUADS;
+    float *const out = plain + (((((size_t)l * B + b) * n) * 2 + kv) * H + h) * DH + dim;          // of slot `first`
+    const size_t stride = (size_t)2 * H * DH;
+    auto put = [&](int tok, f32x4_t v) {
         const int slot = i * 16 + tok - first;
-        if (slot < 0 || slot >= n) continue;
-        f32x4_t v;
-        if (sealed) {
-            const float s = scales[(((size_t)layer * n_pages8 + page) * H + h) * 2 + kv];
+        if (slot >= 0 && slot < n) __builtin_nontemporal_store(v, reinterpret_cast<f32x4_t *>(out + slot * stride));
+    };
+    if (sealed) {
+        const uint8_t *src = (kv ? vcodes : kcodes) + kv8_block_base(layer, n_pages8, page, H, h, DH);
+        const float s = scales[(((size_t)layer * n_pages8 + page) * H + h) * 2 + kv];
+        if (kv == 0) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = s * kv8_value<FMT>(kv ? vcodes[base + v8_in_block(tok, dim + e)] : kcodes[base + k8_in_block(tok, dim + e)]);
+            for (int r = 0; r < 16 / TOKS; ++r) {
+                const int tok = r * TOKS + t0;
+                const uint32_t w = *reinterpret_cast<const uint32_t *>(src + k8_in_block(tok, dim));
+                put(tok, f32x4_t{s * kv8_value<FMT>(w & 255u), s * kv8_value<FMT>((w >> 8) & 255u), s * kv8_value<FMT>((w >> 16) & 255u), s * kv8_value<FMT>(w >> 24)});
+            }
         } else {
+            typedef __attribute__((ext_vector_type(2))) uint32_t u2;
+            // a lane's share of the 16 tokens: 16 / TOKS of them that lie together, tokens v_perm^-1 of TOKS-th parts of 0 .. 15
+            constexpr int RUN = 16 / TOKS;                   // 8 with 128 dims, 4 with 64: bytes of one dim
+            u2 w[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = a2f(kv ? vpages[base + v_in_block<true>(tok, dim + e, Dh)] : kpages[base + k_in_block<true>(tok, dim + e, Dh)]);
+            for (int e = 0; e < 4; ++e) {
+                const int d = dim + e, p0 = t0 * RUN, at = (((d >> 6) * 2 + (p0 >> 3)) * 32 + (d & 31)) * 16 + ((d >> 5) & 1) * 8 + (p0 & 7);
+                w[e][0] = *reinterpret_cast<const uint32_t *>(src + at);
+                w[e][1] = RUN == 8 ? *reinterpret_cast<const uint32_t *>(src + at + 4) : 0u;
+            }
+#pragma unroll
+            for (int r = 0; r < RUN; ++r) {
+                const int q = t0 * RUN + r, tok = ((q & 7) >> 2) * 8 + (q >> 3) * 4 + (q & 3);        // v_perm(tok) == q
+                f32x4_t v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = s * kv8_value<FMT>((w[e][r >> 2] >> (8 * (r & 3))) & 255u);
+                put(tok, v);
+            }
         }
-        *reinterpret_cast<f32x4_t *>(plain + (((((size_t)l * B + b) * n + slot) * 2 + kv) * H + h) * Dh + dim) = v;
+    } else {
+        const a16_t *src = (kv ? vpages : kpages) + kv_block_base(layer, n_pages, page, H, h, DH);
+        for (int tok = t0; tok < 16; tok += TOKS) {
+            f32x4_t v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = a2f(src[kv ? v_in_block<true>(tok, dim + e, DH) : k_in_block<true>(tok, dim + e, DH)]);
+            put(tok, v);
+        }
     }
 }
 
 int launch_kv8_read(hydra_ctx *c, hipStream_t s, int B, int layer, const hydra_kv8 *kv, int first_slot, int n_slots, float *plain) {
     const int H = c->m.n_heads, Dh = c->m.head_dim, NL = layer < 0 ? c->m.n_layers : 1;
-    const dim3 grid((first_slot + n_slots - 1) / 16 - first_slot / 16 + 1, H, B * NL), block(256);
-#define READ(Fv)                                                                                                                                    \
-    hipLaunchKernelGGL((kv8_read_kernel<Fv>), grid, block, 0, s, (const a16_t *)kv->tail.k_pages, (const a16_t *)kv->tail.v_pages, kv->tail.page_table, \
+    const int pages = (first_slot + n_slots - 1) / 16 - first_slot / 16 + 1;
+    const dim3 grid(ceil_div(pages * H * 2, 4), B, NL), block(256);
+#define READ(DHv, Fv)                                                                                                                               \
+    hipLaunchKernelGGL((kv8_read_kernel<DHv, Fv>), grid, block, 0, s, (const a16_t *)kv->tail.k_pages, (const a16_t *)kv->tail.v_pages, kv->tail.page_table, \
                        kv->tail.max_pages, kv->tail.n_pages, (const uint8_t *)kv->k_codes, (const uint8_t *)kv->v_codes, kv->scales, kv->page_table,     \
-                       kv->max_pages, kv->n_pages, kv->n_sealed, layer < 0 ? 0 : layer, B, first_slot, n_slots, H, Dh, plain, flags_dev(c))
-    if (kv->format == KV8_INT8) READ(KV8_INT8); else READ(KV8_E4M3);
+                       kv->max_pages, kv->n_pages, kv->n_sealed, layer < 0 ? 0 : layer, B, first_slot, n_slots, H, plain, flags_dev(c))
+    if (Dh == 128) { if (kv->format == KV8_INT8) READ(128, KV8_INT8); else READ(128, KV8_E4M3); }
+    else           { if (kv->format == KV8_INT8) READ(64, KV8_INT8); else READ(64, KV8_E4M3); }
 #undef READ
     HYDRA_LAUNCH_CHECK("kv8_read_kernel");
     return HYDRA_OK;

@@ -35,19 +35,27 @@ __device__ __forceinline__ int block_scan(int v, int *part, int &total) {
     return before + x - v;
 }
 
-// The `want` lowest free pages into list[]; returns how many there are (at most want).  Uniform over the workgroup.
+// The `want` lowest free pages into list[]; returns how many there are (at most want).  Uniform over the workgroup.  A thread looks at 16 counts at a
+// time, all of them in one round trip.
 __device__ __forceinline__ int lowest_free(const int32_t *ref, int n_pages, int want, int32_t *list, int *part) {
+    typedef int32_t i4 __attribute__((ext_vector_type(4), aligned(4)));
+    enum { PER = 16 };
     int found = 0;
-    for (int p0 = 0; p0 < n_pages && found < want; p0 += PG_THREADS * 4) {
-        const int p = p0 + (int)threadIdx.x * 4;
-        int free_n = 0, is[4];
+    for (int p0 = 0; p0 < n_pages && found < want; p0 += PG_THREADS * PER) {
+        const int p = p0 + (int)threadIdx.x * PER;
+        uint32_t free_mask = 0;
+        if (p + PER <= n_pages) {
+            i4 v[PER / 4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { is[e] = p + e < n_pages && ref[p + e] == 0; free_n += is[e]; }
+            for (int e = 0; e < PER / 4; ++e) v[e] = *reinterpret_cast<const i4 *>(ref + p + 4 * e);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) free_mask |= (v[e >> 2][e & 3] == 0 ? 1u : 0u) << e;
+        } else {
+            for (int e = 0; p + e < n_pages; ++e) free_mask |= (ref[p + e] == 0 ? 1u : 0u) << e;
+        }
         int total;
-        int at = found + block_scan(free_n, part, total);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (is[e]) { if (at < want) list[at] = p + e; ++at; }
+        int at = found + block_scan(__popc(free_mask), part, total);
+        for (; free_mask && at < want; free_mask &= free_mask - 1) list[at++] = p + __ffs(free_mask) - 1;
         found += total;
     }
     return min(found, want);
@@ -64,63 +72,116 @@ __device__ __forceinline__ PgRange page_range(const int32_t *lo, const int32_t *
     return r;
 }
 
-// ws: need[B], then the pages handed out (at most n_pages)
+struct PgRow { int first, last, lacks, start; };             // its logical pages; how many have none (-1: no such range); where its pages begin among all
+enum { PG_ROWS = 1024, PG_GROUP = 4 };
+
+// How many entries each row lacks, and the first of them: a wave takes G rows and requests A pieces of 64 entries of each at a time.
+template <int G, int A>
+__device__ __forceinline__ void count_lacking(const int32_t *table, int max_pages, int B, PgRow *rows, int lane, int wave) {
+    for (int b0 = wave; b0 < B; b0 += PG_WAVES * G) {
+        int first[G], last[G], need[G], found[G], most = 0;
+#pragma unroll
+        for (int r = 0; r < G; ++r) {
+            const int b = b0 + r * PG_WAVES;
+            first[r] = last[r] = need[r] = 0;
+            if (b < B) { first[r] = rows[b].first; last[r] = rows[b].last; }
+            found[r] = last[r];
+            most = max(most, last[r] - first[r]);
+        }
+        for (int i0 = 0; i0 < most; i0 += 64 * A) {
+            int v[G][A];
+#pragma unroll
+            for (int r = 0; r < G; ++r)
+#pragma unroll
+                for (int u = 0; u < A; ++u) {
+                    const int i = first[r] + i0 + u * 64 + lane, b = min(b0 + r * PG_WAVES, B - 1);      // no load behind a condition
+                    v[r][u] = table[(size_t)b * max_pages + min(i, max_pages - 1)];
+                    v[r][u] = i < last[r] ? v[r][u] : 0;
+                }
+#pragma unroll
+            for (int r = 0; r < G; ++r)
+#pragma unroll
+                for (int u = 0; u < A; ++u) {
+                    const uint64_t m = __ballot(v[r][u] < 0);
+                    if (m && !need[r]) found[r] = first[r] + i0 + u * 64 + __builtin_ctzll(m);
+                    need[r] += __popcll(m);
+                }
+        }
+        if (lane == 0)
+#pragma unroll
+            for (int r = 0; r < G; ++r) {
+                const int b = b0 + r * PG_WAVES;
+                if (b < B && rows[b].lacks == 0) { rows[b].first = found[r]; rows[b].lacks = need[r]; }
+            }
+    }
+}
+
+// Four rows of a wave go together, their loads in flight at once, and what is known of a row (PgRow) lies in shared memory for up to PG_ROWS rows: a call
+// is a chain of a dozen round trips whatever it hands out (64 rows of 2048 entries 39 us with a row after the other, 16 now).
+// ws: PgRow [B], then the pages handed out (at most n_pages).
 __global__ __launch_bounds__(PG_THREADS) void pages_reserve_kernel(int32_t *table, int32_t *ref, int n_pages, int max_pages, int B, const int32_t *lo,
                                                                     const int32_t *hi, int extra, int32_t *ws, int32_t *ok, int32_t *flags) {
     __shared__ int part[PG_WAVES];
+    __shared__ PgRow in_lds[PG_ROWS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int32_t *start = ws, *list = ws + B;
-    // what each row lacks; -1: its range is not one
-    for (int b = wave; b < B; b += PG_WAVES) {
+    PgRow *rows = B <= PG_ROWS ? in_lds : reinterpret_cast<PgRow *>(ws);
+    int32_t *list = ws + 4 * (size_t)B;
+    for (int b = threadIdx.x; b < B; b += PG_THREADS) {
         const PgRange r = page_range(lo, hi, extra, b);
         const bool good = r.ok && (int64_t)(lo ? lo[b] : 0) <= (int64_t)hi[b] + extra && r.last <= max_pages;
-        int need = 0;
-        if (good)
-            for (int i = r.first + lane; i < r.last; i += 64) need += table[(size_t)b * max_pages + i] < 0;
-#pragma unroll
-        for (int d = 32; d; d >>= 1) need += __shfl_xor(need, d);
-        if (lane == 0) start[b] = good ? need : -1;
+        rows[b] = PgRow{good ? r.first : 0, good ? r.last : 0, good ? 0 : -1, 0};
     }
     __syncthreads();
-    // where its pages begin among all that are handed out
+    if (B <= PG_WAVES) count_lacking<1, 16>(table, max_pages, B, rows, lane, wave);
+    else               count_lacking<PG_GROUP, 4>(table, max_pages, B, rows, lane, wave);
+    __syncthreads();
     int all = 0;
     for (int b0 = 0; b0 < B; b0 += PG_THREADS) {
         const int b = b0 + (int)threadIdx.x;
-        const int need = b < B ? start[b] : 0;
         int total;
-        const int at = block_scan(max(need, 0), part, total) + all;
-        if (b < B) start[b] = need < 0 ? -1 : at;
+        const int at = block_scan(b < B ? max(rows[b].lacks, 0) : 0, part, total) + all;
+        if (b < B) rows[b].start = at;
         all = min(all + total, 0x3fffffff);
     }
     const int found = lowest_free(ref, n_pages, min(all, n_pages), list, part);
     __syncthreads();
-    for (int b = wave; b < B; b += PG_WAVES) {
-        const int at0 = start[b];
-        const PgRange r = page_range(lo, hi, extra, b);
-        bool served = at0 >= 0;
-        if (served) {
-            int need = 0;
-            for (int i = r.first + lane; i < r.last; i += 64) need += table[(size_t)b * max_pages + i] < 0;
+    for (int b = threadIdx.x; b < B; b += PG_THREADS) {
+        const PgRow r = rows[b];
+        const bool served = r.lacks == 0 || (r.lacks > 0 && r.start + r.lacks <= found);
+        if (!served) { atomicOr(flags, FLAG_CAPACITY); rows[b].lacks = 0; }
+        if (ok) ok[b] = served ? 1 : 0;
+    }
+    __syncthreads();
+    for (int b0 = wave; b0 < B; b0 += PG_WAVES * PG_GROUP) {
+        PgRow r[PG_GROUP];
+        int most = 0;                                        // the longest way from a row's first entry without a page to its end
 #pragma unroll
-            for (int d = 32; d; d >>= 1) need += __shfl_xor(need, d);
-            served = need == 0 || at0 + need <= found;
-            int at = at0;
-            if (served && need)
-                for (int i0 = r.first; i0 < r.last; i0 += 64) {
-                    const int i = i0 + lane;
-                    const bool lacks = i < r.last && table[(size_t)b * max_pages + i] < 0;
-                    const uint64_t m = __ballot(lacks);
-                    if (lacks) {
-                        const int page = list[at + __popcll(m & ((1ull << lane) - 1ull))];
-                        table[(size_t)b * max_pages + i] = page;
-                        ref[page] = 1;
-                    }
-                    at += __popcll(m);
-                }
+        for (int k = 0; k < PG_GROUP; ++k) {
+            const int b = b0 + k * PG_WAVES;
+            r[k] = b < B ? rows[b] : PgRow{0, 0, 0, 0};
+            if (r[k].lacks > 0) most = max(most, r[k].last - r[k].first);
         }
-        if (lane == 0) {
-            if (!served) atomicOr(flags, FLAG_CAPACITY);
-            if (ok) ok[b] = served ? 1 : 0;
+        for (int i0 = 0; i0 < most; i0 += 64) {
+            int page[PG_GROUP];
+            bool lack[PG_GROUP];
+#pragma unroll
+            for (int k = 0; k < PG_GROUP; ++k) {
+                const int i = r[k].first + i0 + lane;
+                const int v = table[(size_t)min(b0 + k * PG_WAVES, B - 1) * max_pages + min(i, max_pages - 1)];
+                lack[k] = r[k].lacks > 0 && i < r[k].last && v < 0;
+            }
+#pragma unroll
+            for (int k = 0; k < PG_GROUP; ++k) {
+                const uint64_t m = __ballot(lack[k]);
+                page[k] = list[lack[k] ? r[k].start + __popcll(m & ((1ull << lane) - 1ull)) : 0];
+                r[k].start += __popcll(m);
+            }
+#pragma unroll
+            for (int k = 0; k < PG_GROUP; ++k)
+                if (lack[k]) {
+                    table[(size_t)(b0 + k * PG_WAVES) * max_pages + r[k].first + i0 + lane] = page[k];
+                    ref[page[k]] = 1;
+                }
         }
     }
 }
@@ -150,19 +211,45 @@ __global__ __launch_bounds__(256) void pages_release_kernel(int32_t *table, int3
     drop_page(ref, n_pages, page, flags);
 }
 
-// Which row every row becomes a copy of, and the fresh pages (block 0); meanwhile the others copy the tables into the workspace.
-// ws: fresh page of each row [B] (-1: none), list [B], tables [B, max_pages]
-__global__ __launch_bounds__(PG_THREADS) void pages_fork_plan_kernel(const int32_t *table, const int32_t *ref, int n_pages, int max_pages, int B,
-                                                                      const int32_t *src_row, const int32_t *seq_len, int32_t *ws, int32_t *copy_src,
-                                                                      int32_t *copy_dst, int32_t *forked, int32_t *flags) {
-    if (blockIdx.x > 0) {
-        int32_t *old = ws + 2 * (size_t)B;
+// Entry i of row b in a fork: the page is named once more by each of the row's `copies`; a row that becomes a copy itself takes its new entry and gives
+// its old page back.
+__device__ __forceinline__ void fork_entry(int32_t *table, int32_t *ref, int n_pages, int max_pages, int b, int i, int src, int copies, const int32_t *seq_len,
+                                           int fresh, const int32_t *old, int32_t *flags) {
+    if (src == b && copies == 0) return;
+    const int was = old[(size_t)b * max_pages + i];
+    if (copies > 0 && was >= 0 && i < seq_len[b] >> 4) {
+        if (was < n_pages) atomicAdd(&ref[was], copies);
+        else atomicOr(flags, FLAG_BAD_PAGE);
+    }
+    if (src == b) return;
+    const int whole = seq_len[src] >> 4;
+    int page = -1;
+    if (i < whole) page = old[(size_t)src * max_pages + i];
+    else if (i == whole && fresh >= 0) { page = fresh; atomicAdd(&ref[page], 1); }
+    table[(size_t)b * max_pages + i] = page;
+    if (was >= 0) drop_page(ref, n_pages, was, flags);
+}
+
+// Which row every row becomes a copy of, and the fresh pages.  ws: fresh page of each row [B] (-1: none), list [B], copies of each row [B].  SMALL (one workgroup; the tables fit
+// its shared memory): the new tables as well; otherwise block 0 plans while the others copy the tables behind the list, for pages_fork_kernel.
+enum { PG_SMALL = 8192 };
+template <bool SMALL>
+__global__ __launch_bounds__(PG_THREADS) void pages_fork_plan_kernel(int32_t *table, int32_t *ref, int n_pages, int max_pages, int B, const int32_t *src_row,
+                                                                      const int32_t *seq_len, int32_t *ws, int32_t *copy_src, int32_t *copy_dst, int32_t *forked,
+                                                                      int32_t *flags) {
+    __shared__ int part[PG_WAVES];
+    __shared__ int32_t tables[SMALL ? PG_SMALL : 1];
+    if (SMALL) {
+        for (int i = threadIdx.x; i < B * max_pages; i += PG_THREADS) tables[i] = table[i];
+        __syncthreads();
+    } else if (blockIdx.x > 0) {
+        int32_t *old = ws + 3 * (size_t)B;
         const size_t n = (size_t)B * max_pages, step = (size_t)(gridDim.x - 1) * PG_THREADS;
         for (size_t i = (size_t)(blockIdx.x - 1) * PG_THREADS + threadIdx.x; i < n; i += step) old[i] = table[i];
         return;
     }
-    __shared__ int part[PG_WAVES];
-    int32_t *fresh = ws, *list = ws + B;
+    const int32_t *old = SMALL ? tables : table;
+    int32_t *fresh = ws, *list = ws + B, *copies = ws + 2 * (size_t)B;
     int all = 0;
     for (int b0 = 0; b0 < B; b0 += PG_THREADS) {
         const int b = b0 + (int)threadIdx.x;
@@ -175,7 +262,7 @@ __global__ __launch_bounds__(PG_THREADS) void pages_fork_plan_kernel(const int32
                 if (L < 0 || (L + 15LL) >> 4 > max_pages) atomicOr(flags, FLAG_CAPACITY);
                 else {
                     row = src;
-                    if (L & 15) page = table[(size_t)src * max_pages + (L >> 4)];
+                    if (L & 15) page = old[(size_t)src * max_pages + (L >> 4)];
                 }
             }
         }
@@ -187,6 +274,7 @@ __global__ __launch_bounds__(PG_THREADS) void pages_fork_plan_kernel(const int32
             forked[b] = row;
             copy_src[b] = page;
             fresh[b] = need ? at : -1;
+            copies[b] = 0;
         }
     }
     const int found = lowest_free(ref, n_pages, min(all, n_pages), list, part);
@@ -204,46 +292,66 @@ __global__ __launch_bounds__(PG_THREADS) void pages_fork_plan_kernel(const int32
         }
         fresh[b] = page;
         copy_dst[b] = page;
+        if (forked[b] != b) atomicAdd(&copies[forked[b]], 1);
+    }
+    if (!SMALL) return;
+    __syncthreads();
+    for (int e = threadIdx.x; e < B * max_pages; e += PG_THREADS) {
+        const int b = e / max_pages;
+        fork_entry(table, ref, n_pages, max_pages, b, e - b * max_pages, forked[b], copies[b], seq_len, fresh[b], tables, flags);
     }
 }
 
 __global__ __launch_bounds__(256) void pages_fork_kernel(int32_t *table, int32_t *ref, int n_pages, int max_pages, int B, const int32_t *seq_len,
                                                           const int32_t *ws, const int32_t *forked, int32_t *flags) {
     const int b = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
-    const int src = forked[b];
-    if (src == b || i >= max_pages) return;
-    const int32_t *old = ws + 2 * (size_t)B;
-    const int whole = seq_len[src] >> 4;
-    const int was = old[(size_t)b * max_pages + i];
-    int page = -1;
-    if (i < whole) page = old[(size_t)src * max_pages + i];
-    else if (i == whole) page = ws[b];
-    table[(size_t)b * max_pages + i] = page;
-    if (page == was) return;                                // gives up and takes the same page
-    if (page >= 0) {
-        if (page < n_pages) atomicAdd(&ref[page], 1);
-        else atomicOr(flags, FLAG_BAD_PAGE);
-    }
-    if (was >= 0) drop_page(ref, n_pages, was, flags);
+    if (i < max_pages) fork_entry(table, ref, n_pages, max_pages, b, i, forked[b], ws[2 * (size_t)B + b], seq_len, ws[b], ws + 3 * (size_t)B, flags);
 }
 
-// Moves of a compaction.  ws: where page p at or behind U goes [n_pages]
-__global__ __launch_bounds__(PG_THREADS) void pages_compact_plan_kernel(int32_t *ref, int n_pages, int32_t *ws, int32_t *move_src, int32_t *move_dst, int32_t *counts) {
+__device__ __forceinline__ void remap_entry(int32_t *entry, int n_pages, int U, const int32_t *to, int32_t *flags) {
+    const int page = *entry;
+    if (page >= n_pages) atomicOr(flags, FLAG_BAD_PAGE);
+    else if (page >= U) *entry = to[page];
+}
+
+// Moves of a compaction.  ws: where page p at or behind U goes [n_pages].  entries > 0: the tables (so many entries) follow at once.
+__global__ __launch_bounds__(PG_THREADS) void pages_compact_plan_kernel(int32_t *table, int entries, int32_t *ref, int n_pages, int32_t *ws, int32_t *move_src,
+                                                                         int32_t *move_dst, int32_t *counts, int32_t *flags) {
     __shared__ int part[PG_WAVES];
+    enum { PER = 8 };
     int used = 0;
-    for (int p = threadIdx.x; p < n_pages; p += PG_THREADS) used += ref[p] > 0;
+    for (int p0 = threadIdx.x; p0 < n_pages; p0 += PG_THREADS * PER) {
+        int v[PER];
+#pragma unroll
+        for (int e = 0; e < PER; ++e) { const int p = p0 + e * PG_THREADS; v[e] = p < n_pages ? ref[p] : 0; }
+#pragma unroll
+        for (int e = 0; e < PER; ++e) used += v[e] > 0;
+    }
     int U;
     block_scan(used, part, U);
     int holes = 0, moves = 0;
-    for (int p0 = 0; p0 < n_pages; p0 += PG_THREADS) {
-        const int p = p0 + (int)threadIdx.x;
-        const bool in = p < n_pages && ref[p] > 0;
-        const bool hole = p < U && !in, move = p >= U && in;
+    for (int p0 = 0; p0 < n_pages; p0 += PG_THREADS * PER) {            // a thread looks at PER pages in a row
+        const int p = p0 + (int)threadIdx.x * PER;
+        int v[PER], hole = 0, move = 0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) v[e] = p + e < n_pages ? ref[p + e] : 0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            if (p + e >= n_pages) continue;
+            hole += p + e < U && v[e] <= 0;
+            move += p + e >= U && v[e] > 0;
+        }
         int nh, nm;
-        const int ah = holes + block_scan(hole ? 1 : 0, part, nh), am = moves + block_scan(move ? 1 : 0, part, nm);
-        if (hole) move_dst[ah] = p;
-        if (move) move_src[am] = p;
-        if (p >= U && p < n_pages) ws[p] = p;
+        int ah = holes + block_scan(hole, part, nh), am = moves + block_scan(move, part, nm);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            if (p + e >= n_pages) continue;
+            if (p + e < U) { if (v[e] <= 0) move_dst[ah++] = p + e; }
+            else {
+                ws[p + e] = p + e;
+                if (v[e] > 0) move_src[am++] = p + e;
+            }
+        }
         holes += nh;
         moves += nm;
     }
@@ -256,15 +364,13 @@ __global__ __launch_bounds__(PG_THREADS) void pages_compact_plan_kernel(int32_t 
         ref[a] = 0;
     }
     if (threadIdx.x == 0) { counts[0] = moves; counts[1] = U; }
+    __syncthreads();
+    for (int i = threadIdx.x; i < entries; i += PG_THREADS) remap_entry(table + i, n_pages, U, ws, flags);
 }
 
 __global__ __launch_bounds__(256) void pages_remap_kernel(int32_t *table, int n_pages, size_t entries, const int32_t *ws, const int32_t *counts, int32_t *flags) {
-    const int U = counts[1];
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= entries) return;
-    const int page = table[i];
-    if (page >= n_pages) { atomicOr(flags, FLAG_BAD_PAGE); return; }
-    if (page >= U) table[i] = ws[page];
+    if (i < entries) remap_entry(table + i, n_pages, counts[1], ws, flags);
 }
 
 // Whole pages of up to three arrays ([layers][n_pages][bytes] each): a workgroup copies 16 KB pieces, all its loads before its stores.
@@ -343,7 +449,7 @@ extern "C" {
 
 size_t hydra_pages_workspace_bytes(int B, int n_pages, int max_pages) {
     if (B < 1 || n_pages < 1 || max_pages < 1) return 0;
-    const size_t reserve = (size_t)B + n_pages, fork = 2 * (size_t)B + (size_t)B * max_pages, compact = n_pages;
+    const size_t reserve = 4 * (size_t)B + n_pages, fork = 3 * (size_t)B + (size_t)B * max_pages, compact = n_pages;
     return align_up(std::max(reserve, std::max(fork, compact)) * 4, 256);
 }
 
@@ -374,8 +480,15 @@ int hydra_pages_fork(hydra_ctx *c, void *stream, int B, void *ws, const hydra_pa
     if (rc) return rc;
     if ((rc = check_ws(ws))) return rc;
     if (!src_row || !seq_len || !copy_src || !copy_dst || !forked) return fail(HYDRA_E_INVALID_ARG, "hydra_pages_fork: NULL argument");
-    const int copiers = (int)std::min<size_t>(128, ((size_t)B * p->max_pages + PG_THREADS - 1) / PG_THREADS);
-    hipLaunchKernelGGL(pages_fork_plan_kernel, dim3(1 + copiers), dim3(PG_THREADS), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages, B,
+    const size_t entries = (size_t)B * p->max_pages;
+    if (entries <= PG_SMALL) {
+        hipLaunchKernelGGL(pages_fork_plan_kernel<true>, dim3(1), dim3(PG_THREADS), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages, B,
+                           src_row, seq_len, (int32_t *)ws, copy_src, copy_dst, forked, flags_dev(c));
+        HYDRA_LAUNCH_CHECK("pages_fork_plan_kernel");
+        return HYDRA_OK;
+    }
+    const int copiers = (int)std::min<size_t>(128, (entries + PG_THREADS - 1) / PG_THREADS);
+    hipLaunchKernelGGL(pages_fork_plan_kernel<false>, dim3(1 + copiers), dim3(PG_THREADS), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages, B,
                        src_row, seq_len, (int32_t *)ws, copy_src, copy_dst, forked, flags_dev(c));
     HYDRA_LAUNCH_CHECK("pages_fork_plan_kernel");
     hipLaunchKernelGGL(pages_fork_kernel, dim3(ceil_div(p->max_pages, 256), B), dim3(256), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages,
@@ -389,9 +502,12 @@ int hydra_pages_compact(hydra_ctx *c, void *stream, int B, void *ws, const hydra
     if (rc) return rc;
     if ((rc = check_ws(ws))) return rc;
     if (!move_src || !move_dst || !counts) return fail(HYDRA_E_INVALID_ARG, "hydra_pages_compact: NULL argument");
-    hipLaunchKernelGGL(pages_compact_plan_kernel, dim3(1), dim3(PG_THREADS), 0, (hipStream_t)stream, p->ref, p->n_pages, (int32_t *)ws, move_src, move_dst, counts);
-    HYDRA_LAUNCH_CHECK("pages_compact_plan_kernel");
     const size_t entries = (size_t)B * p->max_pages;
+    const bool small = entries <= PG_SMALL;                 // one kernel; beyond, the tables are spread over the chip
+    hipLaunchKernelGGL(pages_compact_plan_kernel, dim3(1), dim3(PG_THREADS), 0, (hipStream_t)stream, p->page_table, small ? (int)entries : 0, p->ref, p->n_pages,
+                       (int32_t *)ws, move_src, move_dst, counts, flags_dev(c));
+    HYDRA_LAUNCH_CHECK("pages_compact_plan_kernel");
+    if (small) return HYDRA_OK;
     hipLaunchKernelGGL(pages_remap_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, (hipStream_t)stream, p->page_table, p->n_pages, entries,
                        (const int32_t *)ws, counts, flags_dev(c));
     HYDRA_LAUNCH_CHECK("pages_remap_kernel");
