@@ -21,9 +21,10 @@ namespace hydra {
 static constexpr float LOG2E = 1.44269504f;
 
 // How far (in powers of two) a query's maximum may trail its exponents before what was accumulated is rescaled.  Weights are then at most
-// 2^LAZY; being floating, they keep their 11 bits, and the sum is taken over the rounded ones, so that a row that one key
-// dominates still gets that key's value exactly.  16 rows x 64 nodes x 2048 tokens 69.6 -> 66.0 us, 4 rows 29.8 -> 27.7 against LAZY = 0 (the
-// maximum of 32 queries moves in nearly every one of a wave's tiles).
+// 2^LAZY; being floating, they keep their 11 bits.  16 rows x 64 nodes x 2048 tokens 69.6 -> 66.0 us, 4 rows 29.8 -> 27.7 against LAZY = 0 (the maximum of
+// 32 queries moves in nearly every one of a wave's tiles); the error against 64 bits 2.2e-4 -> 2.6e-4, of which 2.1e-4 is the rounding of the result.
+// The sum takes the weights in 32 bits, as they are before they are rounded: where V is small its page's weights are, and after the rounding
+// nothing might be left of them, while the sum divides them by that scale again.
 static constexpr float LAZY = 8.f;
 
 struct TileScale { float k0, k1, v0, v1, r0, r1; };      // of a tile's two pages: c s_K, log2 s_V, 1 / s_V
@@ -52,17 +53,14 @@ __device__ __forceinline__ void kv8_softmax(const f32x16_t &z, const TileScale &
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        pb[0][w] = half_pack(__builtin_amdgcn_exp2f(fmaf(z[2 * w], ts.k0, c0)), __builtin_amdgcn_exp2f(fmaf(z[2 * w + 1], ts.k0, c0)));
-        pb[1][w] = half_pack(__builtin_amdgcn_exp2f(fmaf(z[8 + 2 * w], ts.k1, c1)), __builtin_amdgcn_exp2f(fmaf(z[8 + 2 * w + 1], ts.k1, c1)));
+        const float a0 = __builtin_amdgcn_exp2f(fmaf(z[2 * w], ts.k0, c0)), a1 = __builtin_amdgcn_exp2f(fmaf(z[2 * w + 1], ts.k0, c0));
+        const float b0 = __builtin_amdgcn_exp2f(fmaf(z[8 + 2 * w], ts.k1, c1)), b1 = __builtin_amdgcn_exp2f(fmaf(z[8 + 2 * w + 1], ts.k1, c1));
+        s0 += a0; s0 += a1;
+        s1 += b0; s1 += b1;
+        pb[0][w] = half_pack(a0, a1);
+        pb[1][w] = half_pack(b0, b1);
     }
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const uint32_t p0 = pb[0][w], p1 = pb[1][w];
-        const h16x2_t h0 = __builtin_bit_cast(h16x2_t, p0), h1 = __builtin_bit_cast(h16x2_t, p1);
-        s0 = fmaf((float)h0[0], ts.r0, s0); s0 = fmaf((float)h0[1], ts.r0, s0);
-        s1 = fmaf((float)h1[0], ts.r1, s1); s1 = fmaf((float)h1[1], ts.r1, s1);
-    }
-    l_run += s0 + s1;
+    l_run += s0 * ts.r0 + s1 * ts.r1;
 }
 
 struct Kv8Args {

@@ -240,3 +240,44 @@ def test_other_streams_and_graphs():
         got = out.clone()
         check = check_attention(c, kv8, kv, q, L, [x // 16 for x in L], "int8", parent)
         assert torch.equal(got, check)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("H,Dh,B", [(2, 128, 1), (32, 64, 9)])             # few rows; more (row, head)s than compute units
+@pytest.mark.parametrize("small,large", [(160, 416), (416, 160)])
+@pytest.mark.parametrize("down", [10, 16, 20])
+def test_weight_shared_by_pages_of_large_and_small_values(fmt, H, Dh, B, small, large, down):
+    """Two pages of one wave's tiles take equal shares of the weight, and the values of one are 2^-down of the other's: the small ones do not show in
+    the result, but their weight does, in the sum that it is divided by."""
+    T, L = 8, [700] * B
+    parent = tree_parent(T)
+    kv = random_kv(21, B, 720, H, Dh).float()
+    kv[:, :, 0] *= 0.05
+    direction = torch.randn(H, Dh, generator=torch.Generator(device=DEV).manual_seed(7), device=DEV)
+    kv[:, small:small + 16, 0] = direction
+    kv[:, large:large + 16, 0] = direction
+    kv[:, :, 1] *= 100.0
+    kv[:, small:small + 16, 1] *= 2.0 ** -down
+    kv = kv.half()
+    q = direction.expand(B, T, H, Dh).half().contiguous()
+    c = context(H, Dh, B, T, 1, 1024)
+    kv8 = caches(H, Dh, B, 1, 720, fmt, seed=22)
+    fill(c, kv8, kv, L)
+    check_attention(c, kv8, kv, q, L, [n // 16 for n in L], fmt, parent)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("T", [1, 33, 128])
+def test_nothing_sealed(fmt, T):
+    H, Dh, L = 2, 64, [1500, 3]
+    parent = tree_parent(T)
+    c = context(H, Dh, 2, T, 1, 1700)
+    kv8 = caches(H, Dh, 2, 1, 1500 + T, fmt, seed=T)
+    kv = random_kv(T, 2, 1500 + T, H, Dh)
+    fill(c, kv8, kv, L, sealed_at=[0, 0])
+    q = torch.randn(2, T, H, Dh, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).half()
+    check_attention(c, kv8, kv, q, L, [0, 0], fmt, parent)
+    kv8.tail.seq_len_hint = 1500
+    check_attention(c, kv8, kv, q, L, [0, 0], fmt, parent)
+    kv8.tail.seq_len_hint = 1                                # a hint that is too short: never a matter of results
+    check_attention(c, kv8, kv, q, L, [0, 0], fmt, parent)
