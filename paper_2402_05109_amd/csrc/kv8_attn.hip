@@ -432,7 +432,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8Args p) {
 // Short contexts: a workgroup takes one 32-query tile of one (row, head) and 1 / DS of the head's dims, its eight waves split the keys and meet in LDS,
 // and the result goes straight out.  A chain of round trips, so everything that can be is requested at once: the page ids before the length
 // is known, then all tiles of a wave (20 registers each with DS = 4) and the first tile of its tail.
-enum { KV8_SHORT_WAVES = 8, KV8_SHORT_TILES = 5 };
+enum { KV8_SHORT_WAVES = 8 };
 template <int DH, int DS>
 struct Short8 { u32x4_t k[DH / 32]; uint32_t v[2][DH / DS / 16]; };       // V: 8 bytes for each 32 dims of a page
 
@@ -737,10 +737,12 @@ int launch_kv8_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const vo
     a.table16 = kv->tail.page_table; a.seq_len = seq_len; a.tree = tree_dev(c); a.apart = apart; a.out = out; a.flags = flags;
     a.max_pages8 = kv->max_pages; a.n_pages8 = kv->n_pages; a.max_pages = kv->tail.max_pages; a.n_pages = kv->tail.n_pages; a.layer = layer;
     a.T = T; a.H = H; a.groups = H * B; a.plain = plain ? 1 : 0; a.c = LOG2E / sqrtf((float)Dh);
-    // Up to 40 key tiles, while a workgroup per (row, head, 32-query tile) fits one round of the chip: no records and no merge, and the head's
-    // dims shared out over more workgroups while those fit the round too (us: 64 nodes behind 777 tokens, 32 heads 10.0 / 10.7 / 13.8 with 4 / 2 / 1
-    // shares, 16.7 with records and merge; 4 rows of it 19.1 against 24.0; beyond one round 16 rows of 400 tokens 40 against 26).
-    if (tiles <= KV8_SHORT_WAVES * KV8_SHORT_TILES && QTtot * H * B <= 256) {
+    // Short contexts, while a workgroup per (row, head, 32-query tile) fits one round of the chip: no records and no merge, and the head's dims shared out over
+    // more workgroups while those fit the round too (us: 64 nodes behind 777 tokens, 32 heads 10.0 / 10.7 / 13.8 with 4 / 2 / 1 shares, 16.7 with records
+    // and merge; 4 rows of it 19.1 against 24.0; beyond one round 16 rows of 400 tokens 40 against 26).  Up to 36 key tiles (one node, 32 heads,
+    // 701 / 1250 / 2000 tokens 9.8 / 12.4 / 14.8 against 12.3 / 11.7 / 13.0), 56 with more than one query tile (64 nodes, 1300 / 1650 / 2000 tokens 13.0 / 14.6 / 15.8
+    // against 13.7 / 14.5 / 15.1; 2 rows of 1500 15.8 against 18.4; 128 nodes, 1650 tokens 15.7 against 17.5).
+    if (tiles <= (QTtot > 1 ? 56 : 36) && QTtot * H * B <= 256) {
         int ds = Dh / 32;
         while (ds > 1 && QTtot * H * B * ds > 256) ds >>= 1;
         a.key_wgs = 1;
