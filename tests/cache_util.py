@@ -33,19 +33,15 @@ def context(H, Dh, B, T=1, NL=1, max_pos=256, arity=3, dtype=hb.HYDRA_BF16, pare
     return c
 
 
-def caches(H, Dh, B, NL, slots, fmt, seed=0, ring=0):
+def caches(H, Dh, B, NL, slots, fmt, seed=0, more=0):
     """An 8-bit cache with a full-length 16-bit tail, pages in random places; everything not written is NaN (codes that are NaN
-    in e4m3).  ring > 0: a row's tail pages are taken in turn from `ring` of its own."""
+    in e4m3).  more: so many unused pages in front of all others."""
     g = torch.Generator().manual_seed(seed)
     pages = (slots + 15) // 16
-    n16 = B * (ring or pages) + 2
-    if ring:
-        own = torch.randperm(n16, generator=g)[:B * ring].reshape(B, ring)
-        table16 = own[:, torch.arange(pages) % ring]
-    else:
-        table16 = torch.randperm(n16, generator=g)[:B * pages].reshape(B, pages)
-    n8 = B * pages + 3
-    table8 = torch.randperm(n8, generator=g)[:B * pages].reshape(B, pages)
+    n16 = more + B * pages + 2
+    table16 = more + torch.randperm(B * pages + 2, generator=g)[:B * pages].reshape(B, pages)
+    n8 = more + B * pages + 3
+    table8 = more + torch.randperm(B * pages + 3, generator=g)[:B * pages].reshape(B, pages)
     block = H * 16 * Dh
     k, v = (torch.full((NL * n16 * block,), math.nan, dtype=torch.float16, device=DEV) for _ in range(2))
     tail = hb.KV(k, v, table16.to(torch.int32).to(DEV).contiguous(), n16)

@@ -281,3 +281,32 @@ def test_nothing_sealed(fmt, T):
     check_attention(c, kv8, kv, q, L, [0, 0], fmt, parent)
     kv8.tail.seq_len_hint = 1                                # a hint that is too short: never a matter of results
     check_attention(c, kv8, kv, q, L, [0, 0], fmt, parent)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_caches_beyond_4_gib(fmt):
+    """Pages whose codes, and whose 16-bit values, lie more than 2^32 bytes behind the first ones."""
+    H, Dh, T, B, L = 8, 128, 9, 2, [150, 97]
+    more = 2 ** 32 // (H * 16 * Dh) + 5
+    parent = tree_parent(T)
+    c = context(H, Dh, B, T, 1, 256)
+    kv8 = caches(H, Dh, B, 1, 176, fmt, seed=30, more=more)
+    kv = random_kv(30, B, 176, H, Dh)
+    fill(c, kv8, kv, L)
+    spoil(kv8, 1, H, Dh, [n // 16 for n in L], kv8.tail.page_table)
+    q = torch.randn(B, T, H, Dh, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).half()
+    check_attention(c, kv8, kv, q, L, [n // 16 for n in L], fmt, parent)
+    # the sealed pages of row 0 moved to the front
+    was = kv8.page_table[0, :9].clone()
+    to = torch.arange(9, dtype=torch.int32, device=DEV)
+    c.hydra_kv8_copy_pages(kv8, 9, was, to)
+    kv8.page_table[0, :9] = to
+    check_attention(c, kv8, kv, q, L, [n // 16 for n in L], fmt, parent)
+    out = torch.full((B, 64, 2, H, Dh), math.nan, device=DEV)
+    c.kv8_read(B, 0, kv8, 20, 64, out)
+    want, _ = cache_values(kv, [n // 16 for n in L], fmt)
+    assert_equal(out.double(), want[:, 20:84])
+    tail = kv8.tail.page_table[1, 6:7].clone()
+    c.hydra_kv_copy_pages(kv8.tail, 1, tail, to[:1])
+    block = H * 16 * Dh
+    assert torch.equal(kv8.tail.k_pages[:block], kv8.tail.k_pages[int(tail) * block:(int(tail) + 1) * block]) and c.read_flags() == 0

@@ -172,6 +172,28 @@ def test_a_life_of_pages(B, rows, pool, seed):
             both.compact()
 
 
+@pytest.mark.parametrize("B,rows,pool,seed", [(12, 2500, 30000, 1), (40, 300, 9000, 2), (3, 5000, 40000, 3)])
+def test_long_rows_and_large_pools(B, rows, pool, seed):
+    """Tables beyond what one workgroup holds, rows of thousands of entries, free pages far behind the first ones."""
+    rng = random.Random(seed)
+    both = Both(context(2, 64, B), B, rows, pool)
+    n = [rng.randint(10 * rows, 16 * rows - 80) for _ in range(B)]
+    ok = both.reserve(None, n, 0)
+    n = [x if o else 0 for x, o in zip(n, ok)]
+    both.reserve(None, n, 64)
+    gone = rng.randrange(B)
+    n[gone] = 0
+    both.release(None, n)
+    forked = both.fork([rng.choice((b, rng.randrange(B))) for b in range(B)], n)
+    n = [n[f] for f in forked]
+    both.reserve(None, n, 70)
+    n = [x // 2 if rng.random() < 0.4 else x for x in n]
+    both.release(None, n)
+    both.compact()
+    both.reserve(None, n, 33)
+    both.fork([B - 1 - b for b in range(B)], n)
+
+
 def test_rows_out_of_range():
     both = Both(context(2, 64, 6), 6, 4, 30)
     both.reserve([0, 0, -1, 40, 0, 0], [20, -1, 5, 20, 64, 65], 0)        # the last one needs a fifth page, row 3 ends before it begins
