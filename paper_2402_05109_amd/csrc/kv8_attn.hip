@@ -370,9 +370,10 @@ __global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8Args p) {
 
     if (__any(bad) && lane == 0) atomicOr(p.flags, FLAG_BAD_PAGE);
 
-    // ---- merge the waves through LDS, one query tile after the other: maxima and sums [QT][NW][2][32], then O[NW][DT * 16][64]
+    // ---- merge the waves through LDS, one query tile after the other: maxima and sums [QT][NW][2][32], then O[NW][DT * 4][64] of four dims each
     __syncthreads();                                         // every wave is done with queries and tiles
-    float *ml = lds, *ob = lds + QT * NW * 64;
+    float *ml = lds;
+    f32x4_t *ob = reinterpret_cast<f32x4_t *>(lds + QT * NW * 64);
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
         const HalfWaves lh = half_waves(l_run[q]);           // each half-wave has summed its own keys
@@ -397,26 +398,23 @@ __global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8Args p) {
 #pragma unroll
         for (int w = 0; w < NW; ++w) l_tot += __builtin_amdgcn_exp2f(mq[w * 64 + col] - m_safe) * mq[w * 64 + 32 + col];
         const float f = __builtin_amdgcn_exp2f(m_run[q] - m_safe);
-        float *dst = ob + (size_t)wave * DT * 16 * 64 + lane;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) dst[(dt * 16 + v) * 64] = o[q][dt][v] * f;
+        for (int id = 0; id < DT * 4; ++id) {
+            const f32x16_t &od = o[q][id >> 2];
+            const int v = 4 * (id & 3);
+            ob[(wave * DT * 4 + id) * 64 + lane] = f32x4_t{od[v] * f, od[v + 1] * f, od[v + 2] * f, od[v + 3] * f};
+        }
         __syncthreads();
         // the (band, group of 4 registers = 4 consecutive dims) items are shared out over the waves
         const float inv = p.key_wgs == 1 ? 1.0f / l_tot : 1.0f;
         for (int id = wave; id < DT * 4; id += NW) {
             const int dt = id >> 2, g4 = id & 3;
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+            f32x4_t acc = ob[id * 64 + lane];
 #pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                const float *src = ob + (size_t)w * DT * 16 * 64 + lane;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] += src[(dt * 16 + 4 * g4 + e) * 64];
-            }
+            for (int w = 1; w < NW; ++w) acc += ob[(w * DT * 4 + id) * 64 + lane];
             const int dim = 32 * dt + 8 * g4 + 4 * hl, m = b * T + query;
             if (p.key_wgs > 1) {
-                *reinterpret_cast<f32x4_t *>(rec + (size_t)query * DH + dim) = f32x4_t{acc[0], acc[1], acc[2], acc[3]};
+                *reinterpret_cast<f32x4_t *>(rec + (size_t)query * DH + dim) = acc;
             } else if (query < T) {
                 store_result<DH>(p, m, h, dim, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
             }
@@ -621,8 +619,9 @@ __global__ __launch_bounds__(KV8_SHORT_WAVES * 64, 2) void kv8_short_kernel(Kv8A
         step16(last, t);
     }
 
-    // ---- merge the waves through LDS: ml[NW][2][32], then O[NW][DT * 16][64] where the queries were
-    float *ml = lds, *ob = lds + NW * 64;
+    // ---- merge the waves through LDS: ml[NW][2][32], then O[NW][DT * 4][64] of four dims each where the queries were
+    float *ml = lds;
+    f32x4_t *ob = reinterpret_cast<f32x4_t *>(lds + NW * 64);
     const HalfWaves lh2 = half_waves(l_run);                 // each half-wave has summed its own keys
     if (hl == 0) {
         ml[(wave * 2 + 0) * 32 + col] = m_run;
@@ -637,23 +636,20 @@ __global__ __launch_bounds__(KV8_SHORT_WAVES * 64, 2) void kv8_short_kernel(Kv8A
 #pragma unroll
     for (int w = 0; w < NW; ++w) l_tot += __builtin_amdgcn_exp2f(ml[(w * 2 + 0) * 32 + col] - m_safe) * ml[(w * 2 + 1) * 32 + col];
     const float f = __builtin_amdgcn_exp2f(m_run - m_safe);
-    float *dst = ob + (size_t)wave * DT * 16 * 64 + lane;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) dst[(dt * 16 + v) * 64] = o[dt][v] * f;
+    for (int id = 0; id < DT * 4; ++id) {
+        const f32x16_t &od = o[id >> 2];
+        const int v = 4 * (id & 3);
+        ob[(wave * DT * 4 + id) * 64 + lane] = f32x4_t{od[v] * f, od[v + 1] * f, od[v + 2] * f, od[v + 3] * f};
+    }
     __syncthreads();
     // the (band, group of 4 registers = 4 consecutive dims) items are shared out over the waves
     const float inv = 1.0f / l_tot;
     for (int id = wave; id < DT * 4; id += NW) {
         const int dt = id >> 2, g4 = id & 3;
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        f32x4_t acc = ob[id * 64 + lane];
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float *src = ob + (size_t)w * DT * 16 * 64 + lane;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) acc[q] += src[(dt * 16 + 4 * g4 + q) * 64];
-        }
+        for (int w = 1; w < NW; ++w) acc += ob[(w * DT * 4 + id) * 64 + lane];
         if (query < T) store_result<DH>(p, b * T + query, h, 32 * (ds * DT + dt) + 8 * g4 + 4 * hl, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
     }
 }
