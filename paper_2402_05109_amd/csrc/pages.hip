@@ -211,18 +211,18 @@ __global__ __launch_bounds__(256) void pages_release_kernel(int32_t *table, int3
     drop_page(ref, n_pages, page, flags);
 }
 
-// Entry i of row b in a fork: the page is named once more by each of the row's `copies`; a row that becomes a copy itself takes its new entry and gives
-// its old page back.
-__device__ __forceinline__ void fork_entry(int32_t *table, int32_t *ref, int n_pages, int max_pages, int b, int i, int src, int copies, const int32_t *seq_len,
+// Entry i of row b in a fork: the page is named once more by each of the row's `copies` (own_whole: the row's whole pages); a row that becomes a copy itself
+// (src != b, whole: the whole pages of src) takes its new entry and gives its old page back.  One addition for all copies: 31 rows that take over a
+// prompt would queue up at its counts.
+__device__ __forceinline__ void fork_entry(int32_t *table, int32_t *ref, int n_pages, int max_pages, int b, int i, int src, int copies, int own_whole, int whole,
                                            int fresh, const int32_t *old, int32_t *flags) {
     if (src == b && copies == 0) return;
     const int was = old[(size_t)b * max_pages + i];
-    if (copies > 0 && was >= 0 && i < seq_len[b] >> 4) {
+    if (copies > 0 && was >= 0 && i < own_whole) {
         if (was < n_pages) atomicAdd(&ref[was], copies);
         else atomicOr(flags, FLAG_BAD_PAGE);
     }
     if (src == b) return;
-    const int whole = seq_len[src] >> 4;
     int page = -1;
     if (i < whole) page = old[(size_t)src * max_pages + i];
     else if (i == whole && fresh >= 0) { page = fresh; atomicAdd(&ref[page], 1); }
@@ -230,41 +230,79 @@ __device__ __forceinline__ void fork_entry(int32_t *table, int32_t *ref, int n_p
     if (was >= 0) drop_page(ref, n_pages, was, flags);
 }
 
-// Which row every row becomes a copy of, and the fresh pages.  ws: fresh page of each row [B] (-1: none), list [B], copies of each row [B].  SMALL (one workgroup; the tables fit
-// its shared memory): the new tables as well; otherwise block 0 plans while the others copy the tables behind the list, for pages_fork_kernel.
+// Which row a row becomes a copy of, by what the caller asks for (src) and the length of that row (L): itself where that is not possible.
+__device__ __forceinline__ int fork_source(int b, int src, int L, int B, int max_pages, int32_t *flags) {
+    if (src == -1 || src == b) return b;
+    if (src < -1 || src >= B) { atomicOr(flags, FLAG_BAD_PATH); return b; }
+    if (L < 0 || (L + 15LL) >> 4 > max_pages) { atomicOr(flags, FLAG_CAPACITY); return b; }
+    return src;
+}
+
+// The whole fork in one workgroup, for tables that fit its shared memory: entries, lengths and sources come in one round trip, the counts in a second one.
 enum { PG_SMALL = 8192 };
-template <bool SMALL>
-__global__ __launch_bounds__(PG_THREADS) void pages_fork_plan_kernel(int32_t *table, int32_t *ref, int n_pages, int max_pages, int B, const int32_t *src_row,
+__global__ __launch_bounds__(PG_THREADS) void pages_fork_small_kernel(int32_t *table, int32_t *ref, int n_pages, int max_pages, int B, const int32_t *src_row,
+                                                                       const int32_t *seq_len, int32_t *copy_src, int32_t *copy_dst, int32_t *forked, int32_t *flags) {
+    __shared__ int part[PG_WAVES];
+    __shared__ int32_t old[PG_SMALL], len[PG_ROWS], copies[PG_ROWS], row[PG_ROWS], fresh[PG_ROWS], list[PG_ROWS];      // B <= PG_ROWS
+    const int tid = (int)threadIdx.x, entries = B * max_pages;
+    int v[PG_SMALL / PG_THREADS];
+#pragma unroll
+    for (int u = 0; u < PG_SMALL / PG_THREADS; ++u) v[u] = table[min(tid + u * PG_THREADS, entries - 1)];
+    const int b = min(tid, B - 1), want = src_row[b];
+    len[tid] = seq_len[b];
+    copies[tid] = 0;
+#pragma unroll
+    for (int u = 0; u < PG_SMALL / PG_THREADS; ++u)
+        if (tid + u * PG_THREADS < entries) old[tid + u * PG_THREADS] = v[u];
+    __syncthreads();
+    int src = b, page = -1;
+    if (tid < B) {
+        src = fork_source(b, want, want >= 0 && want < B ? len[want] : 0, B, max_pages, flags);
+        if (src != b && (len[src] & 15)) page = old[src * max_pages + (len[src] >> 4)];
+    }
+    int all;
+    const int at = block_scan(page >= 0 ? 1 : 0, part, all);
+    const int found = lowest_free(ref, n_pages, min(all, n_pages), list, part);
+    __syncthreads();
+    if (tid < B) {
+        int mine = -1;
+        if (page >= 0) {
+            if (at < found) mine = list[at];
+            else { atomicOr(flags, FLAG_CAPACITY); src = b; page = -1; }          // the pool is exhausted: the row stays as it is
+        }
+        row[b] = forked[b] = src;
+        copy_src[b] = page;
+        fresh[b] = copy_dst[b] = mine;
+        if (src != b) atomicAdd(&copies[src], 1);
+    }
+    __syncthreads();
+    for (int e = tid; e < entries; e += PG_THREADS) {
+        const int r = e / max_pages, from = row[r];
+        fork_entry(table, ref, n_pages, max_pages, r, e - r * max_pages, from, copies[r], len[r] >> 4, len[from] >> 4, fresh[r], old, flags);
+    }
+}
+
+// Larger tables: block 0 plans while the others copy the tables, then pages_fork_kernel.  ws: fresh page of each row [B] (-1: none), list [B], copies of
+// each row [B], tables [B, max_pages]
+__global__ __launch_bounds__(PG_THREADS) void pages_fork_plan_kernel(const int32_t *table, const int32_t *ref, int n_pages, int max_pages, int B, const int32_t *src_row,
                                                                       const int32_t *seq_len, int32_t *ws, int32_t *copy_src, int32_t *copy_dst, int32_t *forked,
                                                                       int32_t *flags) {
     __shared__ int part[PG_WAVES];
-    __shared__ int32_t tables[SMALL ? PG_SMALL : 1];
-    if (SMALL) {
-        for (int i = threadIdx.x; i < B * max_pages; i += PG_THREADS) tables[i] = table[i];
-        __syncthreads();
-    } else if (blockIdx.x > 0) {
+    if (blockIdx.x > 0) {
         int32_t *old = ws + 3 * (size_t)B;
         const size_t n = (size_t)B * max_pages, step = (size_t)(gridDim.x - 1) * PG_THREADS;
         for (size_t i = (size_t)(blockIdx.x - 1) * PG_THREADS + threadIdx.x; i < n; i += step) old[i] = table[i];
         return;
     }
-    const int32_t *old = SMALL ? tables : table;
     int32_t *fresh = ws, *list = ws + B, *copies = ws + 2 * (size_t)B;
     int all = 0;
     for (int b0 = 0; b0 < B; b0 += PG_THREADS) {
         const int b = b0 + (int)threadIdx.x;
         int row = b, page = -1;
         if (b < B) {
-            const int src = src_row[b];
-            if (src < -1 || src >= B) atomicOr(flags, FLAG_BAD_PATH);
-            else if (src >= 0 && src != b) {
-                const int L = seq_len[src];
-                if (L < 0 || (L + 15LL) >> 4 > max_pages) atomicOr(flags, FLAG_CAPACITY);
-                else {
-                    row = src;
-                    if (L & 15) page = old[(size_t)src * max_pages + (L >> 4)];
-                }
-            }
+            const int src = src_row[b], L = src >= 0 && src < B ? seq_len[src] : 0;
+            row = fork_source(b, src, L, B, max_pages, flags);
+            if (row != b && (L & 15)) page = table[(size_t)src * max_pages + (L >> 4)];
         }
         const bool need = page >= 0;
         int total;
@@ -294,18 +332,14 @@ __global__ __launch_bounds__(PG_THREADS) void pages_fork_plan_kernel(int32_t *ta
         copy_dst[b] = page;
         if (forked[b] != b) atomicAdd(&copies[forked[b]], 1);
     }
-    if (!SMALL) return;
-    __syncthreads();
-    for (int e = threadIdx.x; e < B * max_pages; e += PG_THREADS) {
-        const int b = e / max_pages;
-        fork_entry(table, ref, n_pages, max_pages, b, e - b * max_pages, forked[b], copies[b], seq_len, fresh[b], tables, flags);
-    }
 }
 
 __global__ __launch_bounds__(256) void pages_fork_kernel(int32_t *table, int32_t *ref, int n_pages, int max_pages, int B, const int32_t *seq_len,
                                                           const int32_t *ws, const int32_t *forked, int32_t *flags) {
     const int b = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
-    if (i < max_pages) fork_entry(table, ref, n_pages, max_pages, b, i, forked[b], ws[2 * (size_t)B + b], seq_len, ws[b], ws + 3 * (size_t)B, flags);
+    if (i >= max_pages) return;
+    const int src = forked[b];
+    fork_entry(table, ref, n_pages, max_pages, b, i, src, ws[2 * (size_t)B + b], seq_len[b] >> 4, seq_len[src] >> 4, ws[b], ws + 3 * (size_t)B, flags);
 }
 
 __device__ __forceinline__ void remap_entry(int32_t *entry, int n_pages, int U, const int32_t *to, int32_t *flags) {
@@ -481,14 +515,14 @@ int hydra_pages_fork(hydra_ctx *c, void *stream, int B, void *ws, const hydra_pa
     if ((rc = check_ws(ws))) return rc;
     if (!src_row || !seq_len || !copy_src || !copy_dst || !forked) return fail(HYDRA_E_INVALID_ARG, "hydra_pages_fork: NULL argument");
     const size_t entries = (size_t)B * p->max_pages;
-    if (entries <= PG_SMALL) {
-        hipLaunchKernelGGL(pages_fork_plan_kernel<true>, dim3(1), dim3(PG_THREADS), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages, B,
-                           src_row, seq_len, (int32_t *)ws, copy_src, copy_dst, forked, flags_dev(c));
-        HYDRA_LAUNCH_CHECK("pages_fork_plan_kernel");
+    if (entries <= PG_SMALL && B <= PG_ROWS) {
+        hipLaunchKernelGGL(pages_fork_small_kernel, dim3(1), dim3(PG_THREADS), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages, B, src_row,
+                           seq_len, copy_src, copy_dst, forked, flags_dev(c));
+        HYDRA_LAUNCH_CHECK("pages_fork_small_kernel");
         return HYDRA_OK;
     }
     const int copiers = (int)std::min<size_t>(128, (entries + PG_THREADS - 1) / PG_THREADS);
-    hipLaunchKernelGGL(pages_fork_plan_kernel<false>, dim3(1 + copiers), dim3(PG_THREADS), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages, B,
+    hipLaunchKernelGGL(pages_fork_plan_kernel, dim3(1 + copiers), dim3(PG_THREADS), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages, B,
                        src_row, seq_len, (int32_t *)ws, copy_src, copy_dst, forked, flags_dev(c));
     HYDRA_LAUNCH_CHECK("pages_fork_plan_kernel");
     hipLaunchKernelGGL(pages_fork_kernel, dim3(ceil_div(p->max_pages, 256), B), dim3(256), 0, (hipStream_t)stream, p->page_table, p->ref, p->n_pages, p->max_pages,

@@ -10,7 +10,7 @@ from test_kernel_resources import _resource_report
     # (query tiles, waves, request policy) by dims and format; short: shares of the head's dims
     ("kv8_attn.hip", {"kv8_attn_kernel": 26, "kv8_short_kernel": 10, "kv8_merge_kernel": 1}),
     ("kv8_cache.hip", {"kv8_seal_kernel": 4, "kv8_sealed_kernel": 1, "kv8_read_kernel": 4}),
-    ("pages.hip", {"pages_reserve_kernel": 1, "pages_release_kernel": 1, "pages_fork_plan_kernel": 2, "pages_fork_kernel": 1, "pages_compact_plan_kernel": 1,
+    ("pages.hip", {"pages_reserve_kernel": 1, "pages_release_kernel": 1, "pages_fork_small_kernel": 1, "pages_fork_plan_kernel": 1, "pages_fork_kernel": 1, "pages_compact_plan_kernel": 1,
                    "pages_remap_kernel": 1, "copy_pages_kernel": 1}),
 ])
 def test_kernels_keep_everything_in_registers(source, families):
