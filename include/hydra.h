@@ -161,7 +161,7 @@ typedef struct {
 
 /* The pages of a cache as a pool that rows take from, share and give back.  page_table[b, i] is the page of row b's slots
  * 16 i .. 16 i + 15, or -1 where the row holds none; ref[p] is the number of entries that name page p, 0 = free.  Both are
- * the caller's; before the first call the tables are all -1 and the counts all 0.  Every cache that goes by the table (the base
+ * the caller's; before the first call the tables are all -1 and the counts all 0.  Calls on one pool must be ordered on one stream.  Every cache that goes by the table (the base
  * cache, a Hydra++ prefix cache, the sealed pages of an 8-bit cache) shares its page numbers: contents are copied by
  * hydra_kv_copy_pages / hydra_kv8_copy_pages, once for each. */
 typedef struct {
@@ -384,7 +384,8 @@ int tree_attention_kv8(hydra_ctx *ctx, void *stream, int B, int layer, void *ws,
 /* Seals every page that has become whole: per row and layer, pages n_sealed[b] .. seq_len[b] / 16 - 1 go from kv->tail into
  * the codes, then n_sealed[b] = seq_len[b] / 16.  Call it behind kv_compact, once per step or prompt chunk, before the next
  * tree_verify_forward_kv8 writes to the tail again.  A row whose n_sealed is out of range, or for whose pages a table has no
- * valid entry, keeps its n_sealed and raises flag bit 0 or 6. */
+ * valid entry, keeps its n_sealed and raises flag bit 0 or 6.  There is no way back: a row cut to fewer than 16 * n_sealed
+ * tokens has lost the 16 bits of its last page. */
 int hydra_kv8_seal(hydra_ctx *ctx, void *stream, int B, const int32_t *seq_len, const hydra_kv8 *kv);
 
 /* The values that the cache stands for, in plain layout: kv_plain device [B, n_slots, 2, H, Dh] fp32 of one layer, or
@@ -422,7 +423,7 @@ int hydra_pages_release(hydra_ctx *ctx, void *stream, int B, const hydra_pages *
 int hydra_pages_fork(hydra_ctx *ctx, void *stream, int B, void *ws, const hydra_pages *pages, const int32_t *src_row,
                      const int32_t *seq_len, int32_t *copy_src, int32_t *copy_dst, int32_t *forked);
 
-/* Moves the pages in use (U of them) to pages 0 .. U - 1: the k-th lowest page in use at or behind U goes to the k-th lowest free
+/* Moves the pages in use (U of them) to pages 0 .. U - 1 (B: every row that holds any): the k-th lowest page in use at or behind U goes to the k-th lowest free
  * page below U; page tables and counts follow.  Behind it hydra_kv_copy_pages(n = n_pages, move_src, move_dst, counts).
  * Entries of the tables outside the pool are left as they are and flagged (bit 6).
  *   move_src, move_dst device [n_pages] int32 (out), -1 behind the last move

@@ -54,11 +54,11 @@ def step_both(a, b, u):
         assert torch.equal(x, y)
 
 
-@pytest.mark.parametrize("cache_format,prefix", [(None, 0), ("int8", 0), ("e4m3", 0), ("int8", 1), (None, 1)])
-def test_rows_of_a_pool_decode_like_rows_of_their_own(cache_format, prefix):
+@pytest.mark.parametrize("cache_format,prefix,shape", [(None, 0, BASE), ("int8", 0, BASE), ("e4m3", 0, BASE), ("int8", 1, BASE), (None, 1, BASE), (None, 0, CONFIGS[1])])
+def test_rows_of_a_pool_decode_like_rows_of_their_own(cache_format, prefix, shape):
     """Prompts, forks, changes of places, rows that end, and a move of all pages: the same bits as rows that own copies."""
     B = 4
-    cfg = BASE.with_(prefix=prefix)
+    cfg = shape.with_(prefix=prefix)
     W = make_weights(cfg)
     kw = dict(prefill_chunk=32, want_logits=True, cache_format=cache_format)
     pool = gpu_session(cfg, TREE, B, 260, W, pool_pages=60, **kw)
@@ -94,9 +94,10 @@ def test_rows_of_a_pool_decode_like_rows_of_their_own(cache_format, prefix):
     assert torch.equal(named.to(torch.int32), pool.pages.ref)
 
 
-def test_one_prompt_for_all_rows():
+@pytest.mark.parametrize("prefix", [0, 1])
+def test_one_prompt_for_all_rows(prefix):
     """A prompt read once, by the first row alone, and shared: tokens as if every row had read it."""
-    B, cfg = 3, BASE
+    B, cfg = 3, BASE.with_(prefix=prefix)
     W = make_weights(cfg)
     p = prompts(cfg, 1, 90)
     pool = gpu_session(cfg, TREE, B, 200, W, prefill_chunk=32, want_logits=True, pool_pages=30)
@@ -162,6 +163,31 @@ def test_a_pool_that_is_too_small_is_an_error():
     with pytest.raises(RuntimeError, match="exhausted"):
         sess.free_rows([0, 1, 2])
         sess.prefill(prompts(cfg, 3, 96))
+    sess.reset()
+    sess.prefill(prompts(cfg, 2, 64))
+    sess.step()
+    assert sess.main.read_flags() == 1                      # pools too small: the capacity bit of the calls above, nothing else
+
+
+@pytest.mark.parametrize("cache_format", ["int8", "e4m3"])
+def test_generation_behind_an_8_bit_cache(cache_format):
+    """Session.generate takes the steps that a caller would, and leaves the same state."""
+    B, cfg = 2, BASE
+    W = make_weights(cfg)
+    a, b = (gpu_session(cfg, TREE, B, 260, W, prefill_chunk=32, want_logits=True, cache_format=cache_format) for _ in range(2))
+    for s in (a, b):
+        s.prefill(prompts(cfg, B, 100))
+    toks, accs = a.generate(40)
+    got = [[] for _ in range(B)]
+    for _ in accs:
+        b.step()
+        o = b.out()
+        for r in range(B):
+            n = int(o.n_acc[r])
+            got[r] += [int(o.tree_tokens[r, int(o.path[r, j])]) for j in range(n)]
+    assert [t[:40] for t in got] == toks
+    assert torch.equal(a.seq_len, b.seq_len) and torch.equal(a.kv8.n_sealed, a.seq_len // 16) and torch.equal(a.h_last, b.h_last)
+    assert a.main.read_flags() == 0
 
 
 def test_refusals():
