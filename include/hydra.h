@@ -161,8 +161,9 @@ typedef struct {
 
 /* The pages of a cache as a pool that rows take from, share and give back.  page_table[b, i] is the page of row b's slots
  * 16 i .. 16 i + 15, or -1 where the row holds none; ref[p] is the number of entries that name page p, 0 = free.  Both are
- * the caller's; before the first call the tables are all -1 and the counts all 0.  Calls on one pool must be ordered on one stream.  Every cache that goes by the table (the base
- * cache, a Hydra++ prefix cache, the sealed pages of an 8-bit cache) shares its page numbers: contents are copied by
+ * the caller's; before the first call the tables are all -1 and the counts all 0.  Calls on one pool must be ordered on one stream.
+ * Up to 2^30 pages, 2^30 entries of all rows and 2^31 - 16 slots of a row (CAPACITY).  Every cache that goes by the table (the
+ * base cache, a Hydra++ prefix cache, the sealed pages of an 8-bit cache) shares its page numbers: contents are copied by
  * hydra_kv_copy_pages / hydra_kv8_copy_pages, once for each. */
 typedef struct {
     int32_t *page_table;                /* device [B, max_pages], in and out        */

@@ -1,5 +1,6 @@
 // Host side of libhydra: argument validation, arena and workspace layout, and
 // the launch sequences of the four hot-path calls (see include/hydra.h).
+#include <limits.h>
 #include <math.h>
 #include <string.h>
 
@@ -177,6 +178,7 @@ static int check_kv8(hydra_ctx *c, const hydra_kv8 *kv) {
     if (rc) return rc;
     if (!kv->k_codes || !kv->v_codes || !kv->scales || !kv->page_table || !kv->n_sealed) return fail(HYDRA_E_INVALID_ARG, "kv8: one of its pointers is NULL");
     if (kv->n_pages < 1 || kv->max_pages < 1) return fail(HYDRA_E_INVALID_ARG, "kv8: n_pages and max_pages must be positive");
+    if (kv->max_pages > INT_MAX / HYDRA_PAGE || kv->tail.max_pages > INT_MAX / HYDRA_PAGE) return fail(HYDRA_E_CAPACITY, "kv8: a table of 2^31 slots or more");
     if (kv->format != HYDRA_KV8_INT8 && kv->format != HYDRA_KV8_E4M3) return fail(HYDRA_E_INVALID_ARG, "kv8: unknown format");
     if (((uintptr_t)kv->k_codes | (uintptr_t)kv->v_codes | (uintptr_t)kv->tail.k_pages | (uintptr_t)kv->tail.v_pages) & 15)
         return fail(HYDRA_E_INVALID_ARG, "kv8: codes and tail pages must be 16-byte aligned");

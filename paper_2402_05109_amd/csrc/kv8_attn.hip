@@ -6,7 +6,7 @@
 // c = log2(e) / sqrt(Dh), z the product of codes and query,
 //     w = 2^(c s_K z + log2 s_V - M),   O = sum half(w) code_V,   l = sum w / s_V,   result = O / l
 // where M is the running maximum of the exponent.  Dequantising both K and V costs one multiply-add per score that the softmax
-// needs anyway, and w, the only value that is rounded to 16 bits, is at most one whatever the scales are.  A key of the tail has
+// needs anyway, and w, the only value that is rounded to 16 bits, is at most 2^LAZY whatever the scales are.  A key of the tail has
 // s_K = s_V = 1.
 //
 // A wave holds one or two 32-query tiles and takes 32-key tiles (two pages) in turn.  Tiles go to LDS by the LDS DMA, two of them ahead
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8Args p) {
         const int qtile = min(qg * QT + q, QTtot - 1);       // a second tile behind the last query: the first one again, which nobody stores
         qreg[i] = query_piece<DH>(p, b, h, qtile, QTtot, col, 32 * (blk >> 1) + 16 * hl + 8 * (blk & 1));
     }
-    if (L < 0 || L + T > p.max_pages * 16 || ns < 0 || ns > (L >> 4) || ns > p.max_pages8) {     // uniform over the workgroup
+    if (L < 0 || L > p.max_pages * 16 - T || ns < 0 || ns > (L >> 4) || ns > p.max_pages8) {     // uniform over the workgroup
         if (tid == 0 && j == 0 && h == 0) atomicOr(p.flags, FLAG_CAPACITY);
         return;
     }
@@ -467,7 +467,7 @@ __global__ __launch_bounds__(KV8_SHORT_WAVES * 64, 2) void kv8_short_kernel(Kv8A
     }
     const int L = p.seq_len[b], ns = p.n_sealed[b];
     if (wave < KS) qs[wave * 64 + lane] = query_piece<DH>(p, b, h, qtile, QTtot, col, 32 * (wave >> 1) + 16 * hl + 8 * (wave & 1));
-    if (L < 0 || L + T > p.max_pages * 16 || ns < 0 || ns > (L >> 4) || ns > p.max_pages8) {     // uniform over the workgroup
+    if (L < 0 || L > p.max_pages * 16 - T || ns < 0 || ns > (L >> 4) || ns > p.max_pages8) {     // uniform over the workgroup
         if (tid == 0 && j == 0 && h == 0) atomicOr(p.flags, FLAG_CAPACITY);
         return;
     }
@@ -679,7 +679,7 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(const float *__restrict_
         }
     }
     const int L = seq_len[b], ns = n_sealed[b];
-    if (L < 0 || L + T > max_pages * 16 || ns < 0 || ns > (L >> 4) || ns > max_pages8 || !live) return;
+    if (L < 0 || L > max_pages * 16 - T || ns < 0 || ns > (L >> 4) || ns > max_pages8 || !live) return;
     float mt = -INFINITY;
 #pragma unroll
     for (int u = 0; u < KV8_MERGE_MAX; ++u) mt = fmaxf(mt, mu[u]);

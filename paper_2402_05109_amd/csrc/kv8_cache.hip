@@ -25,7 +25,7 @@ __device__ __forceinline__ float kv8_scale(float top) {
     return __uint_as_float((uint32_t)e << 23);
 }
 
-// A wave's four values -> four codes.  r = 1 / scale.
+// A lane's four values (finite: the cache saturates what is written) -> four codes.  r = 1 / scale.
 template <int FMT>
 __device__ __forceinline__ uint32_t kv8_codes(const float *x, float s, float r) {
     if (FMT == KV8_INT8) {

@@ -3,6 +3,7 @@
 // The tables and counts are small integers in device memory, so that no call waits for the host and all of them can be captured
 // into a graph.  Every result is a function of the inputs alone: pages are handed out lowest first, by row, and counts are sums.
 #include <algorithm>
+#include <climits>
 
 #include "device_common.h"
 #include "internal.h"
@@ -461,6 +462,9 @@ static int check_pages(hydra_ctx *c, int B, const hydra_pages *p) {
     if (!c->arena) return fail(HYDRA_E_STATE, "no weight arena bound (hydra_bind_weights)");
     if (!p || !p->page_table || !p->ref) return fail(HYDRA_E_INVALID_ARG, "pages or one of its pointers is NULL");
     if (p->n_pages < 1 || p->max_pages < 1) return fail(HYDRA_E_INVALID_ARG, "pages: n_pages and max_pages must be positive");
+    // sums over entries and numbers of pages, with a workgroup's step behind them, are ints
+    if (p->n_pages > (1 << 30) || (int64_t)B * p->max_pages > (1 << 30) || p->max_pages > INT_MAX / HYDRA_PAGE)
+        return fail(HYDRA_E_CAPACITY, "pages: more than 2^30 pages or table entries, or a table of 2^31 slots");
     return HYDRA_OK;
 }
 static int check_ws(const void *ws) {

@@ -83,3 +83,20 @@ def test_other_arguments(ctx):
     assert lib.hydra_kv_copy_pages(h, None, kv, 0, P, P, None) == hb.HYDRA_OK
     torch.cuda.synchronize()
     assert ctx.read_flags() == 0
+
+
+@pytest.mark.parametrize("name", POOL)
+@pytest.mark.parametrize("large", [dict(n_pages=2 ** 30 + 1), dict(max_pages=2 ** 27), dict(max_pages=2 ** 31 - 1)])
+def test_pools_whose_numbers_would_not_fit(ctx, name, large):
+    assert calls(ctx._h, None, pages_desc(**large), None)[name]() == hb.E_CAPACITY
+
+
+def test_pools_with_too_many_entries_in_all_rows():
+    c = context(1, 128, 16, 1, 1)
+    assert calls(c._h, None, pages_desc(max_pages=2 ** 27 - 1), None, B=9)["hydra_pages_release"]() == hb.E_CAPACITY
+
+
+@pytest.mark.parametrize("name", KV8)
+@pytest.mark.parametrize("large", [dict(max_pages=2 ** 27), dict(tail=kv_desc(max_pages=2 ** 27))])
+def test_tables_whose_slots_would_not_fit(ctx, name, large):
+    assert calls(ctx._h, kv8_desc(**large), None, None)[name]() == hb.E_CAPACITY

@@ -310,3 +310,22 @@ def test_caches_beyond_4_gib(fmt):
     c.hydra_kv_copy_pages(kv8.tail, 1, tail, to[:1])
     block = H * 16 * Dh
     assert torch.equal(kv8.tail.k_pages[:block], kv8.tail.k_pages[int(tail) * block:(int(tail) + 1) * block]) and c.read_flags() == 0
+
+
+@pytest.mark.parametrize("H,B", [(2, 1), (32, 9)])                          # all keys in one workgroup; keys split over waves
+@pytest.mark.parametrize("length", [2 ** 31 - 1, 2 ** 31 - 3, -2 ** 31])
+def test_lengths_at_the_ends_of_the_integers(H, B, length):
+    """Such a row is left alone and flagged; the others are what they would be without it."""
+    Dh, T = 64, 4
+    c = context(H, Dh, B, T, 1, 128)
+    kv8 = caches(H, Dh, B, 1, 112, "int8", seed=2)
+    n = fill(c, kv8, random_kv(3, B, 112, H, Dh), [100] * B)
+    q = torch.randn(B, T, H, Dh, generator=torch.Generator(device=DEV).manual_seed(5), device=DEV).half()
+    want = torch.zeros_like(q)
+    c.tree_attention_kv8(B, 0, c.ws, q, n, kv8, want)
+    n[B - 1] = length
+    out = torch.full_like(q, 7.0)
+    c.tree_attention_kv8(B, 0, c.ws, q, n, kv8, out)
+    assert torch.equal(out[:B - 1], want[:B - 1]) and bool((out[B - 1] == 7.0).all())
+    c.hydra_kv8_seal(B, n, kv8)
+    assert kv8.n_sealed.tolist() == [6] * B and c.read_flags() == 1
