@@ -392,6 +392,7 @@ class Session:
                     self.prefix_attention(name, B)    # hint: still the length before this chunk
                 pos += n
                 self.host_len += n
+                self._growth_since_copy += n          # a length on its way to the host was read before these
         except BaseException:
             if behind is not None:                    # broken off: back to the text that h_last and root belong to
                 self.seq_len.copy_(behind[0])

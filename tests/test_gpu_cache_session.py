@@ -208,3 +208,20 @@ def test_refusals():
         pool.fork([0])
     with pytest.raises(ValueError):
         pool.fork([0, 2])
+
+
+@pytest.mark.parametrize("pool", [None, 40])
+def test_text_behind_steps_stays_below_the_bound(pool):
+    """The host's bound on the lengths comes from a copy that may be older than a later prompt."""
+    cfg = BASE
+    sess = gpu_session(cfg, TREE, 2, 256, make_weights(cfg), prefill_chunk=32, pool_pages=pool)
+    sess.prefill(prompts(cfg, 2, 20))
+    for _ in range(8):                                      # the last one asks for a copy of the lengths
+        sess.step()
+    assert sess._len_event is not None
+    sess.prefill(prompts(cfg, 2, 90, 5))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        sess.step()
+        assert sess.host_len >= int(sess.seq_len.max())
+    assert sess.main.read_flags() == 0
