@@ -326,6 +326,8 @@ class Session:
     def free_rows(self, rows: Sequence[int]) -> None:
         """The rows' text ends: they start again from nothing, and their pages (where no other row shares them) are free."""
         self._need_pool()
+        if any(r != int(r) or r < 0 or r >= self.B for r in rows):
+            raise ValueError(f"free_rows: rows of [0, {self.B})")
         at = torch.tensor(list(rows), dtype=torch.int64, device=self.dev)
         for t in [self.seq_len, self.h_last, self.root] + ([self.pseq_len] if self.prefix else []) + ([self.kv8.n_sealed] if self.kv8 is not None else []):
             t.index_fill_(0, at, 0)

@@ -225,3 +225,16 @@ def test_text_behind_steps_stays_below_the_bound(pool):
         sess.step()
         assert sess.host_len >= int(sess.seq_len.max())
     assert sess.main.read_flags() == 0
+
+
+@pytest.mark.parametrize("rows", [[2], [0, -1], [0.5], [10 ** 12]])
+def test_rows_to_free_that_are_not_there(rows):
+    cfg = BASE
+    sess = gpu_session(cfg, TREE, 2, 64, make_weights(cfg), prefill_chunk=16, pool_pages=12)
+    sess.prefill(prompts(cfg, 2, 20))
+    with pytest.raises(ValueError, match="free_rows"):
+        sess.free_rows(rows)
+    sess.free_rows([])
+    assert sess.seq_len.tolist() == [20, 20]
+    sess.free_rows([1, 1])
+    assert sess.seq_len.tolist() == [20, 0] and sess.main.read_flags() == 0
