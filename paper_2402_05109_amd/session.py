@@ -117,6 +117,7 @@ class Session:
         self.h_last = torch.zeros(B, shape.d, dtype=torch.float32, device=self.dev)
         self.root = torch.zeros(B, dtype=torch.int32, device=self.dev)
         self.host_len = 0                     # host upper bound on seq_len (hint only)
+        self._other_len = 0                   # the same of the rows that take no part in a prompt
         # the bound is tightened without stalling: every few steps seq_len is copied to pinned memory and picked
         # up once the copy has landed
         self._len_pinned = torch.zeros(B, dtype=torch.int32).pin_memory()
@@ -240,6 +241,8 @@ class Session:
 
     # ---- steps ----------------------------------------------------------------
     def _hint(self, T: int) -> None:
+        if self.pool and self.host_len + T > min(self.max_pages * 16, self._max_pos):
+            self.sync_len()                           # rows may have been freed since: only the real lengths are refused
         self.kv.seq_len_hint = self.host_len
 
     def reset(self) -> None:
@@ -287,7 +290,9 @@ class Session:
             lo = self.kv8.n_sealed * 16
             self.main.hydra_pages_release(B, self.tail_pages, lo, self.seq_len)
             self.main.hydra_pages_reserve(B, self._pages_ws, self.tail_pages, lo, self.seq_len, T)
-        if self.B * ((self.host_len + T + 15) // 16) > self.n_pages and not bool(ok[:B].all()):
+        # a row may hold pages that the nodes of a larger tree than this one needed
+        most = max(c.T for c in self._ctx.values())
+        if self.B * ((max(self.host_len, self._other_len) + most + 15) // 16) > self.n_pages and not bool(ok[:B].all()):
             raise RuntimeError(f"the pool of {self.n_pages} pages is exhausted")
 
     def fork(self, src_rows: Sequence[int]) -> None:
@@ -324,7 +329,8 @@ class Session:
         self._len_event = None                        # a length on its way to the host may be another row's
 
     def free_rows(self, rows: Sequence[int]) -> None:
-        """The rows' text ends: they start again from nothing, and their pages (where no other row shares them) are free."""
+        """The rows' text ends: they start again from nothing, and their pages (where no other row shares them) are free.
+        A step adds to such a row as to any other: free it again before it takes its next prompt."""
         self._need_pool()
         if any(r != int(r) or r < 0 or r >= self.B for r in rows):
             raise ValueError(f"free_rows: rows of [0, {self.B})")
@@ -362,7 +368,12 @@ class Session:
         # argmax, whose results nobody can read once the call is over.  Not where the prefix layer reads every chunk's hidden states, and not where the prompt
         # does not fit (the chunks in front of the one that is refused then keep their outputs and the state behind them).  Not behind an 8-bit
         # cache either: the 16-bit pages of the text in front are taken again two chunks later, so there would be no way back to it.
-        layers_only = not self.prefix and self.kv8 is None and self.host_len + L <= min(self.max_pages * 16, self._max_pos)
+        room = min(self.max_pages * 16, self._max_pos)
+        if self.pool and self.host_len + L > room:    # rows may have been freed since, and the longest one may take no part
+            lens = self.seq_len.tolist()
+            self._other_len = max(lens[B:], default=0)
+            self._set_len(max(lens[:B]))
+        layers_only = not self.prefix and self.kv8 is None and self.host_len + L <= room
         last = {n: i for i, n in enumerate(chunks)}
         pos = 0
         behind = None                                 # seq_len and its bound behind the last chunk that h_last and root know of, if others followed
@@ -400,6 +411,8 @@ class Session:
                 self.seq_len.copy_(behind[0])
                 self.host_len = behind[1]
             raise
+        finally:
+            self.host_len, self._other_len = max(self.host_len, self._other_len), 0
 
     def draft(self, name: str = "main") -> None:
         c, o = self.ctx(name), self._out[name]

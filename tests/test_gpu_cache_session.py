@@ -238,3 +238,47 @@ def test_rows_to_free_that_are_not_there(rows):
     assert sess.seq_len.tolist() == [20, 20]
     sess.free_rows([1, 1])
     assert sess.seq_len.tolist() == [20, 0] and sess.main.read_flags() == 0
+
+
+@pytest.mark.parametrize("cache_format", [None, "int8"])
+def test_rows_that_end_make_room_for_the_next_text(cache_format):
+    """Prompt after prompt in the same row, also while another row is nearly full: what counts is the lengths that the rows have."""
+    cfg = BASE
+    W = make_weights(cfg)
+    sess = gpu_session(cfg, TREE, 2, 112, W, prefill_chunk=16, pool_pages=16, cache_format=cache_format, max_pos=144)
+    alone = gpu_session(cfg, TREE, 1, 112, W, prefill_chunk=16, cache_format=cache_format, max_pos=144)
+    for i in range(4):
+        sess.free_rows([0])
+        if i == 1:
+            sess.free_rows([1])
+            sess.prefill(prompts(cfg, 2, 96, 9))            # 96 of the 112: row 1 stays as long as that
+            sess.free_rows([0])
+        text = prompts(cfg, 1, 60, 20 + i)
+        sess.prefill(text)
+        alone.reset()
+        alone.prefill(text)
+        assert sess.seq_len.tolist() == [60, 0 if i == 0 else 96] and sess.host_len >= int(sess.seq_len.max())
+        assert torch.equal(sess.h_last[0], alone.h_last[0]) and torch.equal(sess.root[:1], alone.root)
+    sess.step()
+    assert sess.main.read_flags() == 0
+    with pytest.raises(Exception, match="capacity|CAPACITY|shorter|max_pos|exhausted"):
+        sess.prefill(prompts(cfg, 1, 80, 3))                # 60 + 80 are more than the 128 slots of a row
+
+
+def test_a_pool_that_a_larger_tree_has_used_up():
+    """Pages behind the text that a wide tree needed are not there for a narrow one: an error, not a row without pages."""
+    cfg = BASE
+    sess = gpu_session(cfg, TREE, 3, 256, make_weights(cfg), prefill_chunk=16, pool_pages=16)
+    sess.add_tree("wide", [-1] + [(n - 1) // 8 for n in range(1, 64)])
+    sess.prefill(prompts(cfg, 3, 16))
+    sess.free_rows([1, 2])
+    sess.out("wide").tree_tokens.zero_()
+    sess.verify("wide")                                     # 5 + 4 + 4 of the 16 pages
+    sess.ctx("chain4")
+    o = sess.out("chain4")
+    o.tree_tokens.zero_(); o.path.copy_(torch.arange(4, dtype=torch.int32, device=sess.dev).expand(3, 4)); o.n_acc.fill_(4); o.last_node.fill_(3)
+    with pytest.raises(RuntimeError, match="exhausted"):
+        for _ in range(40):
+            sess.verify("chain4")
+            assert sess.main.read_flags() == 0
+            sess.compact("chain4")
