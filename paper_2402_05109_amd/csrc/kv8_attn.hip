@@ -6,7 +6,7 @@
 // c = log2(e) / sqrt(Dh), z the product of codes and query,
 //     w = 2^(c s_K z + log2 s_V - M),   O = sum half(w) code_V,   l = sum w / s_V,   result = O / l
 // where M is the running maximum of the exponent.  Dequantising both K and V costs one multiply-add per score that the softmax
-// needs anyway, and w, the only value that is rounded to 16 bits, is at most 2^LAZY whatever the scales are.  A key of the tail has
+// needs anyway, and w, the only value that is rounded to 16 bits, is at most 1 whatever the scales are.  A key of the tail has
 // s_K = s_V = 1.
 //
 // A wave holds one or two 32-query tiles and takes 32-key tiles (two pages) in turn.  Tiles go to LDS by the LDS DMA, two of them ahead
@@ -20,16 +20,15 @@ namespace hydra {
 
 static constexpr float LOG2E = 1.44269504f;
 
-// How far (in powers of two) a query's maximum may trail its exponents before what was accumulated is rescaled.  Weights are then at most
-// 2^LAZY; being floating, they keep their 11 bits.  16 rows x 64 nodes x 2048 tokens 69.6 -> 66.0 us, 4 rows 29.8 -> 27.7 against LAZY = 0 (the maximum of
-// 32 queries moves in nearly every one of a wave's tiles); the error against 64 bits 2.2e-4 -> 2.6e-4, of which 2.1e-4 is the rounding of the result.
-// The sum takes the weights in 32 bits, as they are before they are rounded: where V is small its page's weights are, and after the rounding
-// nothing might be left of them, while the sum divides them by that scale again.
-static constexpr float LAZY = 8.f;
-
 struct TileScale { float k0, k1, v0, v1, r0, r1; };      // of a tile's two pages: c s_K, log2 s_V, 1 / s_V
 
 // Products of one 32-key tile -> weights as the P^T operands of the two pages, the running maximum, and this half-wave's share of the sum.
+// The maximum is exact at every tile, so the largest weight is a power of two, 1 in the end, which 16 bits hold: error against 64 bits 2.2e-4 of the
+// 2-norm, of which 2.1e-4 is the rounding of the result.  A maximum that may trail by up to 2^8 saves most of the rescaling (16 rows x 64 nodes x 2048 tokens
+// 63.6 us instead of 69.9, 32003 tokens 64.3 instead of 67.4), but the largest weights are then rounded too (2.6e-4 to 2.8e-4), and since a wave rescales all of
+// its queries when one of them asks, a query's result depends on what the places behind the last query hold.
+// The sum takes the weights in 32 bits, as they are before they are rounded: where V is small its page's weights are, and after the rounding
+// nothing might be left of them, while the sum divides them by that scale again.
 template <int DT>
 __device__ __forceinline__ void kv8_softmax(const f32x16_t &z, const TileScale &ts, float &m_run, float &l_run, f32x16_t (&o)[DT], u32x4_t (&pb)[2]) {
     float a = z[0], b = z[8];
@@ -38,7 +37,7 @@ __device__ __forceinline__ void kv8_softmax(const f32x16_t &z, const TileScale &
     float top = fmaxf(fmaf(a, ts.k0, ts.v0), fmaf(b, ts.k1, ts.v1));
     const HalfWaves h = half_waves(top);
     top = fmaxf(h.lo, h.hi);
-    if (__any(top > m_run + LAZY)) {
+    if (__any(top > m_run)) {
         const float m_new = fmaxf(m_run, top);
         const float alpha = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
