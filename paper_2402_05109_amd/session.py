@@ -280,8 +280,14 @@ class Session:
         if not self.pool:
             raise ValueError("rows of this session have pages of their own: create the Session with pool_pages")
 
+    def _drop_scratch(self) -> None:
+        """The pages behind every row's text go back."""
+        for p in self._pools():
+            self.main.hydra_pages_release(self.B, p, None, self.seq_len)
+
     def _reserve(self, T: int, B: int) -> None:
-        """Pages for T more slots of the first B rows.  Waits for the device only where the pool might be too small."""
+        """Pages for T more slots of the first B rows.  Waits for the device only where the pool might be too small: a row holds no
+        pages but those of its text and of the nodes of one tree or chunk, so whatever shortens a text gives pages back too."""
         if not self.pool:
             return
         ok = self._lists[4]
@@ -304,8 +310,7 @@ class Session:
         B, m = self.B, self.main
         want = torch.tensor([b if r < 0 else r for b, r in enumerate(src_rows)], dtype=torch.int32, device=self.dev)
         src, dst, forked = self._lists[0], self._lists[1], self._lists[3]
-        for p in self._pools():                       # what lies behind the text (scratch of the last step) goes back first
-            m.hydra_pages_release(B, p, None, self.seq_len)
+        self._drop_scratch()                          # what the last step left goes back first
         m.hydra_pages_fork(B, self._pages_ws, self.pages, want, self.seq_len, src, dst, forked)
         if not torch.equal(forked[:B], want):
             got = forked[:B].clone()
@@ -337,15 +342,13 @@ class Session:
         at = torch.tensor(list(rows), dtype=torch.int64, device=self.dev)
         for t in [self.seq_len, self.h_last, self.root] + ([self.pseq_len] if self.prefix else []) + ([self.kv8.n_sealed] if self.kv8 is not None else []):
             t.index_fill_(0, at, 0)
-        for p in self._pools():
-            self.main.hydra_pages_release(self.B, p, None, self.seq_len)
+        self._drop_scratch()
 
     def defragment(self) -> int:
         """Gives back what no text needs, moves the pages in use to the front of the pool and returns how many they are (waits for the device)."""
         self._need_pool()
         m, (src, dst, counts) = self.main, self._lists[:3]
-        for p in self._pools():
-            m.hydra_pages_release(self.B, p, None, self.seq_len)
+        self._drop_scratch()
         m.hydra_pages_compact(self.B, self._pages_ws, self.pages, src, dst, counts)
         if self.kv8 is None:
             m.hydra_kv_copy_pages(self.kv, self.n_pages, src, dst, counts)
@@ -410,6 +413,9 @@ class Session:
             if behind is not None:                    # broken off: back to the text that h_last and root belong to
                 self.seq_len.copy_(behind[0])
                 self.host_len = behind[1]
+            if self.pool:                             # what _reserve goes by: no row holds more than its text and one step need
+                self._drop_scratch()
+                self.sync_len()
             raise
         finally:
             self.host_len, self._other_len = max(self.host_len, self._other_len), 0
