@@ -160,10 +160,16 @@ class Session:
         ctx.bind_weights(self.arena, self._next_slot)
         self._next_slot += 1
 
+    def _check_nodes(self, T: int) -> None:
+        """Behind an 8-bit cache the 16-bit pages are taken in turn: the nodes of a larger tree would overwrite each other."""
+        if self.kv8 is not None and T > self._T_max:
+            raise ValueError(f"an 8-bit cache of this session has 16-bit pages for trees of up to {self._T_max} nodes")
+
     def ctx(self, name: str) -> hb.Hydra:
         """'main', 'ar' (one-node tree) or 'chainN' (N-token causal chunk), created on demand."""
         if name not in self._ctx:
             parent = [-1] if name == "ar" else chain_parent(int(name[5:]))
+            self._check_nodes(len(parent))
             c = self._make_ctx(name, parent)
             self._bind(c)
             need = c.workspace_bytes(self.B)
@@ -177,8 +183,7 @@ class Session:
         room for 16 contexts in all)."""
         if name in self._ctx:
             raise ValueError(f"context {name!r} exists")
-        if self.kv8 is not None and len(parent) > self._T_max:
-            raise ValueError(f"an 8-bit cache of this session has 16-bit pages for trees of up to {self._T_max} nodes")
+        self._check_nodes(len(parent))
         c = self._make_ctx(name, list(parent))
         self._bind(c)
         need = c.workspace_bytes(self.B)
@@ -293,6 +298,8 @@ class Session:
         ok = self._lists[4]
         self.main.hydra_pages_reserve(B, self._pages_ws, self.pages, None, self.seq_len, T, ok)
         if self.kv8 is not None:
+            # never short of pages: no tree has more than _T_max nodes (_check_nodes), so a row holds at most a ring of them, and fork() takes
+            # one more for each row
             lo = self.kv8.n_sealed * 16
             self.main.hydra_pages_release(B, self.tail_pages, lo, self.seq_len)
             self.main.hydra_pages_reserve(B, self._pages_ws, self.tail_pages, lo, self.seq_len, T)

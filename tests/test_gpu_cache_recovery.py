@@ -61,3 +61,20 @@ def test_pages_of_a_prompt_that_the_pool_had_no_room_for(cache_format, front):
     same_steps(sess, fresh, 2)
     assert sess.main.read_flags() == 0
 
+
+@pytest.mark.parametrize("pool", [None, 30])
+def test_chains_that_the_16_bit_pages_cannot_hold(pool):
+    """An 8-bit session keeps 16-bit pages for the trees that it was made for: a longer chain is refused, by name and by every call that would create it."""
+    cfg = BASE
+    W = make_weights(cfg)
+    sess = gpu_session(cfg, TREE, 2, 200, W, prefill_chunk=24, cache_format="int8", pool_pages=pool)
+    sess.prefill(prompts(cfg, 2, 40))
+    for call in (sess.ctx, sess.draft, sess.verify, lambda name: sess.generate(1, name)):
+        with pytest.raises(ValueError, match="16-bit pages"):
+            call("chain25")
+    assert "chain25" not in sess._ctx
+    assert sess.ctx("chain24").T == 24 and sess.ctx("ar").T == 1
+    wide = gpu_session(cfg, TREE, 2, 200, W, prefill_chunk=24, pool_pages=pool)
+    assert wide.ctx("chain25").T == 25                       # a 16-bit cache has a page for every slot
+    sess.step()
+    assert sess.main.read_flags() == 0
