@@ -312,7 +312,7 @@ class Session:
         """Row b becomes a copy of row src_rows[b] as it is now (b or -1: stays).  Whole pages are shared; only the last, incomplete page
         is copied.  For samples of one prompt, or beams that change places."""
         self._need_pool()
-        if len(src_rows) != self.B or any(r < -1 or r >= self.B for r in src_rows):
+        if len(src_rows) != self.B or any(r < -1 or r >= self.B or r != int(r) for r in src_rows):
             raise ValueError(f"fork: {self.B} rows of [-1, {self.B})")
         B, m = self.B, self.main
         want = torch.tensor([b if r < 0 else r for b, r in enumerate(src_rows)], dtype=torch.int32, device=self.dev)

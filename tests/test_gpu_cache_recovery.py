@@ -78,3 +78,17 @@ def test_chains_that_the_16_bit_pages_cannot_hold(pool):
     assert wide.ctx("chain25").T == 25                       # a 16-bit cache has a page for every slot
     sess.step()
     assert sess.main.read_flags() == 0
+
+
+@pytest.mark.parametrize("rows", [[0.5, 1], [0, 1.5], [float("nan"), 0], [0, float("inf")], [-1.5, 0], [0], [0, 2]])
+def test_fork_of_rows_that_are_not_there(rows):
+    cfg = BASE
+    sess = gpu_session(cfg, TREE, 2, 64, make_weights(cfg), prefill_chunk=16, pool_pages=12)
+    sess.prefill(prompts(cfg, 2, 20))
+    before = [t.clone() for t in (sess.page_table, sess.pages.ref, sess.h_last, sess.root)]
+    with pytest.raises(ValueError):
+        sess.fork(rows)
+    for t, w in zip((sess.page_table, sess.pages.ref, sess.h_last, sess.root), before):
+        assert torch.equal(t, w)
+    sess.fork([1, -1])
+    assert torch.equal(sess.h_last[0], before[2][1]) and sess.main.read_flags() == 0
