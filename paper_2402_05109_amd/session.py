@@ -79,7 +79,7 @@ class Session:
         if self.pool:
             self.page_table = torch.full((B, self.max_pages), -1, **i32)
             self.pages = hb.Pages(self.page_table, torch.zeros(self.n_pages, **i32))
-            self._lists = torch.zeros(5, max(B, self.n_pages), **i32)              # copies or moves, their counts, forked rows, rows served
+            self._lists = torch.zeros(5, max(B, self.n_pages, 2), **i32)           # copies or moves, their (two) counts, forked rows, rows served
         else:
             if page_perm_seed is None:
                 perm = torch.arange(self.n_pages, dtype=torch.int32)

@@ -92,3 +92,16 @@ def test_fork_of_rows_that_are_not_there(rows):
         assert torch.equal(t, w)
     sess.fork([1, -1])
     assert torch.equal(sess.h_last[0], before[2][1]) and sess.main.read_flags() == 0
+
+
+def test_a_pool_of_one_page():
+    """The lists that the calls fill are as long as the calls need, also where the pool and the batch are smaller than a pair of counts."""
+    cfg = BASE
+    sess = gpu_session(cfg, [-1], 1, 16, make_weights(cfg), prefill_chunk=4, pool_pages=1)
+    assert all(t.numel() >= 2 for t in sess._lists)          # the moves' counts are two
+    sess.prefill(prompts(cfg, 1, 8))
+    h = sess.h_last.clone()
+    assert sess.defragment() == 1 and sess._lists[3].tolist() == [0] * sess._lists.shape[1]
+    assert torch.equal(sess.h_last, h) and sess.page_table[0].tolist()[:1] == [0] and sess.main.read_flags() == 0
+    sess.free_rows([0])
+    assert sess.defragment() == 0
