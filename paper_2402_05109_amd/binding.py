@@ -127,10 +127,16 @@ def _check(rc: int) -> None:
         raise HydraError(rc, last_error())
 
 
-def _stream() -> int:
-    # the handle of torch.cuda.current_stream() without the Stream object around it, which took half of a short call's time on the host
-    # (tree_attention_kv8 9.6 us a call, 6.8 without)
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+def _pick_stream():
+    # The handle of torch.cuda.current_stream() without the Stream object around it, which takes half of a short call's time on the host
+    # (tree_attention_kv8 9.6 us a call, 6.8 without).  The two names are not torch's public ones: where it does not have them, the public way.
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is None or device is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    return lambda: raw(device())
+
+
+_stream = _pick_stream()
 
 
 def _ptr(t: Optional[torch.Tensor], dtype: torch.dtype, name: str) -> Optional[int]:
