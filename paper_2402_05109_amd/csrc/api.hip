@@ -151,7 +151,7 @@ WsLayout ws_layout(const hydra_ctx *c, int B) {
     return w;
 }
 
-int check_common(hydra_ctx *c, int B, const void *ws) {
+static int check_common(hydra_ctx *c, int B, const void *ws) {
     if (!c) return fail(HYDRA_E_INVALID_ARG, "ctx is NULL");
     if (B < 1 || B > c->max_batch) return fail(HYDRA_E_CAPACITY, "B outside [1, max_batch]");
     if (!ws) return fail(HYDRA_E_INVALID_ARG, "workspace is NULL");
@@ -160,7 +160,7 @@ int check_common(hydra_ctx *c, int B, const void *ws) {
     return HYDRA_OK;
 }
 
-int check_kv(hydra_ctx *c, const hydra_kv *kv) {
+static int check_kv(hydra_ctx *c, const hydra_kv *kv) {
     if (!kv || !kv->k_pages || !kv->v_pages || !kv->page_table) return fail(HYDRA_E_INVALID_ARG, "kv or one of its pointers is NULL");
     if (kv->n_pages < 1 || kv->max_pages < 1) return fail(HYDRA_E_INVALID_ARG, "kv: n_pages and max_pages must be positive");
     if (kv->seq_len_hint < 0) return fail(HYDRA_E_INVALID_ARG, "kv: seq_len_hint is negative");

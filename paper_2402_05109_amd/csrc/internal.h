@@ -208,10 +208,6 @@ int kv8_max_dynamic_lds();
 int launch_kv8_seal(hydra_ctx *c, hipStream_t s, int B, const int32_t *seq_len, const hydra_kv8 *kv);
 int launch_kv8_read(hydra_ctx *c, hipStream_t s, int B, int layer, const hydra_kv8 *kv, int first_slot, int n_slots, float *plain);
 
-// checks of arguments shared by the entry points (api.hip)
-int check_common(hydra_ctx *c, int B, const void *ws);
-int check_kv(hydra_ctx *c, const hydra_kv *kv);
-
 inline const TreeDev *tree_dev(const hydra_ctx *c) {
     return reinterpret_cast<const TreeDev *>(c->arena + c->off_tables + (size_t)c->table_slot * TABLE_SLOT_BYTES);
 }
