@@ -164,9 +164,9 @@ static int check_kv(hydra_ctx *c, const hydra_kv *kv) {
     if (!kv || !kv->k_pages || !kv->v_pages || !kv->page_table) return fail(HYDRA_E_INVALID_ARG, "kv or one of its pointers is NULL");
     if (kv->n_pages < 1 || kv->max_pages < 1) return fail(HYDRA_E_INVALID_ARG, "kv: n_pages and max_pages must be positive");
     if (kv->seq_len_hint < 0) return fail(HYDRA_E_INVALID_ARG, "kv: seq_len_hint is negative");
-    if (kv->seq_len_hint > 0 && kv->seq_len_hint + c->tree.T > kv->max_pages * HYDRA_PAGE)
+    if (kv->seq_len_hint > 0 && (int64_t)kv->seq_len_hint + c->tree.T > (int64_t)kv->max_pages * HYDRA_PAGE)
         return fail(HYDRA_E_CAPACITY, "kv: page table shorter than seq_len_hint + T slots");
-    if (kv->seq_len_hint > 0 && kv->seq_len_hint + c->tree.max_depth >= c->m.max_pos)
+    if (kv->seq_len_hint > 0 && (int64_t)kv->seq_len_hint + c->tree.max_depth >= c->m.max_pos)
         return fail(HYDRA_E_CAPACITY, "kv: seq_len_hint + tree depth reaches max_pos");
     return HYDRA_OK;
 }
