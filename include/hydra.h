@@ -147,7 +147,7 @@ typedef struct {
  *                   nearest even; scale = the smallest power of two with max |x| / scale <= 448
  * A block of zeros has scale 1.  k_codes and v_codes each hold n_layers * n_pages * H * 16 * Dh bytes; page p of layer l, head h
  * starts at byte ((l * n_pages + p) * H + h) * 16 * Dh, 16-byte aligned; placement inside is private to the library.
- * scales holds (scale of K, scale of V) of it at [((l * n_pages + p) * H + h) * 2]. */
+ * scales holds (scale of K, scale of V) of it at [((l * n_pages + p) * H + h) * 2].  Tables name up to 2^31 - 32 slots of a row (CAPACITY). */
 enum { HYDRA_KV8_INT8 = 0, HYDRA_KV8_E4M3 = 1 };
 typedef struct {
     hydra_kv       tail;                /* 16-bit pages of the slots that are not sealed; tail.seq_len_hint bounds seq_len   */

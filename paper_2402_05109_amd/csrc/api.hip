@@ -178,7 +178,9 @@ static int check_kv8(hydra_ctx *c, const hydra_kv8 *kv) {
     if (rc) return rc;
     if (!kv->k_codes || !kv->v_codes || !kv->scales || !kv->page_table || !kv->n_sealed) return fail(HYDRA_E_INVALID_ARG, "kv8: one of its pointers is NULL");
     if (kv->n_pages < 1 || kv->max_pages < 1) return fail(HYDRA_E_INVALID_ARG, "kv8: n_pages and max_pages must be positive");
-    if (kv->max_pages > INT_MAX / HYDRA_PAGE || kv->tail.max_pages > INT_MAX / HYDRA_PAGE) return fail(HYDRA_E_CAPACITY, "kv8: a table of 2^31 slots or more");
+    // slots are ints, and attention counts to the end of a tile of 32 behind the last one
+    const int most = INT_MAX / HYDRA_PAGE - 1;
+    if (kv->max_pages > most || kv->tail.max_pages > most) return fail(HYDRA_E_CAPACITY, "kv8: a table of more than 2^31 - 32 slots");
     if (kv->format != HYDRA_KV8_INT8 && kv->format != HYDRA_KV8_E4M3) return fail(HYDRA_E_INVALID_ARG, "kv8: unknown format");
     if (((uintptr_t)kv->k_codes | (uintptr_t)kv->v_codes | (uintptr_t)kv->tail.k_pages | (uintptr_t)kv->tail.v_pages) & 15)
         return fail(HYDRA_E_INVALID_ARG, "kv8: codes and tail pages must be 16-byte aligned");

@@ -25,3 +25,11 @@ def test_hints_that_end_behind_the_integers(ctx, hint):
     assert lib.tree_verify_forward(h, None, 2, P, P, P, kv, P, P, None, None) == hb.E_CAPACITY
     assert lib.hydra_prefill_chunk(h, None, 2, P, P, P, kv) == hb.E_CAPACITY
     assert lib.tree_attention(h, None, 2, 0, P, P, P, kv, P) == hb.E_CAPACITY
+
+
+@pytest.mark.parametrize("name", KV8)
+def test_tables_whose_last_tile_ends_behind_the_integers(ctx, name):
+    """A text of more than 2^31 - 32 slots has its last tile of 32 keys end at 2^31 or more, which came out negative."""
+    pages = 2 ** 27 - 1
+    assert calls(ctx._h, kv8_desc(max_pages=pages), None, None)[name]() == hb.E_CAPACITY and hb.last_error()
+    assert calls(ctx._h, kv8_desc(tail=kv_desc(max_pages=pages)), None, None)[name]() == hb.E_CAPACITY
