@@ -277,6 +277,35 @@ class Session:
         if self.kv8 is not None:
             c.hydra_kv8_seal(B, self.seq_len, self.kv8)
 
+    def _incomplete(self) -> torch.Tensor:
+        """The 16-bit page of every row that its next token goes to (any page where the row holds none there)."""
+        at = (self.seq_len // 16).clamp(max=self.max_pages - 1).long()
+        return self.kv.page_table.gather(1, at[:, None])[:, 0].clamp(min=0).long()
+
+    def _mark(self):
+        """What _back_to needs to return to the text as it is now.  Behind an 8-bit cache 16-bit pages are taken again as the text grows:
+        every row's incomplete one is kept apart.  Sealed pages are never written again."""
+        mark = [self.seq_len.clone(), self.host_len]
+        if self.kv8 is not None:
+            pages = self._incomplete()
+            mark += [self.kv8.n_sealed.clone()] + [t.view(self.shape.NL, self.n_tail, -1)[:, pages] for t in (self.k_pages, self.v_pages)]
+        return mark
+
+    def _back_to(self, mark) -> None:
+        self.seq_len.copy_(mark[0])
+        self.host_len = mark[1]
+        if self.kv8 is None:
+            return
+        self.kv8.n_sealed.copy_(mark[2])
+        if self.pool:
+            lo = self.kv8.n_sealed * 16
+            self.main.hydra_pages_release(self.B, self.tail_pages, lo, self.seq_len)
+            self.main.hydra_pages_reserve(self.B, self._pages_ws, self.tail_pages, lo, self.seq_len, 0)
+        rows = (self.seq_len % 16).nonzero()[:, 0]
+        pages = self._incomplete()[rows]
+        for t, kept in zip((self.k_pages, self.v_pages), mark[3:]):
+            t.view(self.shape.NL, self.n_tail, -1)[:, pages] = kept[:, rows]
+
     # ---- pages ------------------------------------------------------------------
     def _pools(self) -> List[hb.Pages]:
         return [self.pages] if self.kv8 is None else [self.pages, self.tail_pages]
@@ -376,17 +405,16 @@ class Session:
         chunks = [min(self.prefill_chunk, L - pos) for pos in range(0, L, self.prefill_chunk)]
         # A chunk whose outputs a later chunk of the same length writes again ends behind the decoder layers: no final norm, LM head and
         # argmax, whose results nobody can read once the call is over.  Not where the prefix layer reads every chunk's hidden states, and not where the prompt
-        # does not fit (the chunks in front of the one that is refused then keep their outputs and the state behind them).  Not behind an 8-bit
-        # cache either: the 16-bit pages of the text in front are taken again two chunks later, so there would be no way back to it.
+        # does not fit (the chunks in front of the one that is refused then keep their outputs and the state behind them).
         room = min(self.max_pages * 16, self._max_pos)
         if self.pool and self.host_len + L > room:    # rows may have been freed since, and the longest one may take no part
             lens = self.seq_len.tolist()
             self._other_len = max(lens[B:], default=0)
             self._set_len(max(lens[:B]))
-        layers_only = not self.prefix and self.kv8 is None and self.host_len + L <= room
+        layers_only = not self.prefix and self.host_len + L <= room
         last = {n: i for i, n in enumerate(chunks)}
         pos = 0
-        behind = None                                 # seq_len and its bound behind the last chunk that h_last and root know of, if others followed
+        behind = None                                 # the text behind the last chunk that h_last and root know of, if others followed
         try:
             for i, n in enumerate(chunks):
                 name = f"chain{n}"
@@ -402,9 +430,12 @@ class Session:
                 h_last, root = self.h_last, self.root
                 if layers_only and i < last[n]:
                     if behind is None:
-                        behind = self.seq_len.clone(), self.host_len
+                        behind = self._mark()
                     h_last, root = torch.empty_like(h_last), torch.empty_like(root)       # of outputs that are not written
-                    c.hydra_prefill_chunk(B, self.ws, o.tree_tokens, self.seq_len, self.kv)
+                    if self.kv8 is None:
+                        c.hydra_prefill_chunk(B, self.ws, o.tree_tokens, self.seq_len, self.kv)
+                    else:
+                        c.hydra_prefill_chunk_kv8(B, self.ws, o.tree_tokens, self.seq_len, self.kv8)
                 else:
                     self._forward(c, o, B)
                     o.next_root.copy_(o.argmax[:, n - 1])
@@ -418,8 +449,7 @@ class Session:
                 self._growth_since_copy += n          # a length on its way to the host was read before these
         except BaseException:
             if behind is not None:                    # broken off: back to the text that h_last and root belong to
-                self.seq_len.copy_(behind[0])
-                self.host_len = behind[1]
+                self._back_to(behind)
             if self.pool:                             # what _reserve goes by: no row holds more than its text and one step need
                 self._drop_scratch()
                 self.sync_len()
