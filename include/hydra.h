@@ -402,7 +402,7 @@ size_t hydra_pages_workspace_bytes(int B, int n_pages, int max_pages);
 /* Row b gets a page for every logical page lo[b] / 16 .. ceil((hi[b] + extra) / 16) - 1 that it does not hold (lo == NULL: from 0).
  * Pages are the lowest-numbered free ones, handed out by row, then by logical page.  Rows are served in order and whole:
  * the first one that the pool has too few pages left for, and every later one that needs any, gets none (flag bit 0), as does a
- * row with lo < 0, hi + extra < lo or more pages than max_pages.
+ * row with lo < 0, hi < 0, hi + extra < lo or more pages than max_pages.
  *   lo, hi device [B] int32 (lo may be NULL)   extra host, >= 0   ok device [B] int32 (out) or NULL: 1 = the row has its pages */
 int hydra_pages_reserve(hydra_ctx *ctx, void *stream, int B, void *ws, const hydra_pages *pages,
                         const int32_t *lo, const int32_t *hi, int extra, int32_t *ok);
@@ -433,7 +433,7 @@ int hydra_pages_compact(hydra_ctx *ctx, void *stream, int B, void *ws, const hyd
 
 /* Copies whole pages of every layer, K and V: src[i] -> dst[i] for i < n, or i < *count where that is less (count: device, or NULL).
  * An entry with a negative page is skipped; one outside the cache is skipped and flagged (bit 6).  No page may be a
- * destination twice, or a destination and a source.  Of kv only the pages and n_pages are used. */
+ * destination twice, or a destination and a source.  Of kv only the pages (16-byte aligned) and n_pages are used. */
 int hydra_kv_copy_pages(hydra_ctx *ctx, void *stream, const hydra_kv *kv, int n, const int32_t *src, const int32_t *dst, const int32_t *count);
 int hydra_kv8_copy_pages(hydra_ctx *ctx, void *stream, const hydra_kv8 *kv, int n, const int32_t *src, const int32_t *dst, const int32_t *count);
 

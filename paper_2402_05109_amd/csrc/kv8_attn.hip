@@ -733,10 +733,10 @@ int launch_kv8_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const vo
     a.max_pages8 = kv->max_pages; a.n_pages8 = kv->n_pages; a.max_pages = kv->tail.max_pages; a.n_pages = kv->tail.n_pages; a.layer = layer;
     a.T = T; a.H = H; a.groups = H * B; a.plain = plain ? 1 : 0; a.c = LOG2E / sqrtf((float)Dh);
     // Short contexts, while a workgroup per (row, head, 32-query tile) fits one round of the chip: no records and no merge, and the head's dims shared out over
-    // more workgroups while those fit the round too (us: 64 nodes behind 777 tokens, 32 heads 10.0 / 10.7 / 13.8 with 4 / 2 / 1 shares, 16.7 with records
-    // and merge; 4 rows of it 19.1 against 24.0; beyond one round 16 rows of 400 tokens 40 against 26).  Up to 36 key tiles (one node, 32 heads,
-    // 701 / 1250 / 2000 tokens 9.8 / 12.4 / 14.8 against 12.3 / 11.7 / 13.0), 56 with more than one query tile (64 nodes, 1300 / 1650 / 2000 tokens 13.0 / 14.6 / 15.8
-    // against 13.7 / 14.5 / 15.1; 2 rows of 1500 15.8 against 18.4; 128 nodes, 1650 tokens 15.7 against 17.5).
+    // more workgroups while those fit the round too (us: 64 nodes behind 777 tokens, 32 heads 10.0 / 10.2 / 11.6 with 4 / 2 / 1 shares, 13.0 with records
+    // and merge; 4 rows of it 14.8 against 14.6; beyond one round 16 rows of 400 tokens 38.5 against 25.4).  Up to 36 key tiles (one node, 32 heads,
+    // 701 / 1100 / 1250 / 2000 tokens 8.7 / 10.7 / 12.3 / 15.3 against 9.8 / 10.8 / 11.0 / 11.9), 56 with more than one query tile (64 nodes, 1300 / 1650 / 2000 tokens
+    // 13.7 / 15.7 / 16.9 against 13.9 / 14.5 / 15.0; 2 rows of 1500 16.5 against 17.7; 128 nodes, 1650 tokens 17.3 against 18.1).
     if (tiles <= (QTtot > 1 ? 56 : 36) && QTtot * H * B <= 256) {
         int ds = Dh / 32;
         while (ds > 1 && QTtot * H * B * ds > 256) ds >>= 1;
@@ -751,16 +751,16 @@ int launch_kv8_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const vo
     }
     // Beyond that the keys of a head are split over waves and, while the chip has room, over workgroups.
     //   query tiles of a wave: one while a workgroup for each fits one round (a tile then takes half as long and K/V come from L2 the second time: 64
-    //     nodes, 32 heads, 2000 / 8000 tokens 14.6 / 27.4 us against 18.9 / 27.3, 4 rows of 2048 25.8 against 30.2), two beyond (16 rows of 2048 61.2
-    //     against 73.8)
+    //     nodes, 32 heads, 2000 / 8000 tokens 15.2 / 27.2 us against 20.3 / 29.4, 4 rows of 2048 24.2 against 30.1), two beyond (16 rows of 2048 69.5
+    //     against 81.8)
     //   waves of a workgroup: eight; four with more (row, head, query group)s than CUs, two or more workgroups to a CU, so that one's first
-    //     round trips and merge lie under another's stream (16 rows of 2048 61.2 against 70.4; 8 rows of 128 nodes 30.3 against 39.7), and for up to 32 nodes with
-    //     128 dims (32003 tokens, 40 heads 57.8 against 63.2; 8000 tokens 19.4 against 21.2; with 64 dims 17.2 against 16.2)
+    //     round trips and merge lie under another's stream (16 rows of 2048 67.6 against 79.2; 8 rows of 128 nodes 61.7 against 70.9), and for up to 32 nodes with
+    //     128 dims (32003 tokens, 40 heads 59.1 against 61.9; 8000 tokens 21.3 against 21.6; with 64 dims 16.2 against 15.1)
     const int qt = QTtot > 1 && H * B * QTtot > 256 ? 2 : 1, qgroups = ceil_div(QTtot, qt), hb = H * B * qgroups;
     const int nw = hb > 256 || (Dh == 128 && QTtot == 1) ? 4 : 8;
     const int wgs = std::max(1, std::min({ceil_div(tiles, nw * 2), std::max(1, 256 / hb), units_max, (int)KV8_MERGE_MAX}));
     a.key_wgs = wgs;
-    // K and V that one workgroup alone reads are requested nontemporal (32003 tokens 63.8 -> 57.8 us, 16 rows of 2048 and 32 nodes 60.3 -> 56.8)
+    // K and V that one workgroup alone reads are requested nontemporal (32003 tokens 62.0 -> 58.3 us, 16 rows of 2048 and 32 nodes 60.7 -> 57.6)
     const int aux = qgroups == 1 ? 2 : 0;
     const dim3 grid(ceil_div(H * B, 8) * 8 * qgroups * wgs), block(nw * 64);
     const size_t lds = kv8_lds_bytes(Dh, qt, nw);
