@@ -285,14 +285,15 @@ class Session:
     def _mark(self):
         """What _back_to needs to return to the text as it is now.  Behind an 8-bit cache 16-bit pages are taken again as the text grows:
         every row's incomplete one is kept apart.  Sealed pages are never written again."""
-        mark = [self.seq_len.clone(), self.host_len]
+        mark = [[t.clone() for t in (self.seq_len, self.h_last, self.root)], self.host_len]
         if self.kv8 is not None:
             pages = self._incomplete()
             mark += [self.kv8.n_sealed.clone()] + [t.view(self.shape.NL, self.n_tail, -1)[:, pages] for t in (self.k_pages, self.v_pages)]
         return mark
 
     def _back_to(self, mark) -> None:
-        self.seq_len.copy_(mark[0])
+        for t, kept in zip((self.seq_len, self.h_last, self.root), mark[0]):
+            t.copy_(kept)
         self.host_len = mark[1]
         if self.kv8 is None:
             return
@@ -450,9 +451,11 @@ class Session:
         except BaseException:
             if behind is not None:                    # broken off: back to the text that h_last and root belong to
                 self._back_to(behind)
+            elif self.kv8 is not None:                # a whole chunk may have been broken off between its compaction and its seal
+                self.main.hydra_kv8_seal(self.B, self.seq_len, self.kv8)
             if self.pool:                             # what _reserve goes by: no row holds more than its text and one step need
                 self._drop_scratch()
-                self.sync_len()
+            self.sync_len()
             raise
         finally:
             self.host_len, self._other_len = max(self.host_len, self._other_len), 0

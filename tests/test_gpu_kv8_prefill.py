@@ -131,3 +131,39 @@ def test_chunks_whose_outputs_nobody_reads_take_the_decoder_layers_alone(monkeyp
     sess.prefill(prompts(cfg, 2, 16 * 5 + 7))
     assert taken == [("hydra_prefill_chunk_kv8", 16)] * 4 + [("tree_verify_forward_kv8", 16), ("tree_verify_forward_kv8", 7)]
     assert sess.seq_len.tolist() == [87, 87] and sess.main.read_flags() == 0
+
+
+@pytest.mark.parametrize("chunks,at", [(8, 5), (8, 8), (1, 1)])
+@pytest.mark.parametrize("pool", [None, 40])
+def test_a_prompt_that_is_broken_off_before_its_pages_are_sealed(monkeypatch, chunks, at, pool):
+    """Between the compaction of a chunk, which writes h_last and root where the chunk was computed whole, and the sealing of its pages: back to the text in
+    front where chunks without outputs were computed, behind the chunk where it was the only one."""
+    from paper_2402_05109_amd import binding as hb
+    cfg = BASE
+    W = make_weights(cfg)
+    sess, other = (gpu_session(cfg, TREE, 2, 260, W, prefill_chunk=16, cache_format="int8", pool_pages=pool) for _ in range(2))
+    for s in (sess, other):
+        s.prefill(prompts(cfg, 2, 37))
+    calls, real = [0], hb.Hydra.hydra_kv8_seal
+
+    def broken(self, *args):
+        calls[0] += 1
+        if calls[0] == at:
+            raise Stop
+        return real(self, *args)
+
+    text = prompts(cfg, 2, 16 * chunks, 5)
+    monkeypatch.setattr(hb.Hydra, "hydra_kv8_seal", broken)
+    with pytest.raises(Stop):
+        sess.prefill(text)
+    monkeypatch.undo()
+    if chunks == 1:
+        other.prefill(text)
+    assert sess.seq_len.tolist() == other.seq_len.tolist() and sess.host_len == int(sess.seq_len.max())
+    for s in (sess, other):
+        for _ in range(4):
+            s.step()
+    torch.cuda.synchronize()
+    for x, y in zip(state(sess), state(other)):
+        assert torch.equal(x, y)
+    assert sess.main.read_flags() == 0
