@@ -159,6 +159,26 @@ typedef struct {
     int32_t        format;              /* HYDRA_KV8_INT8 or HYDRA_KV8_E4M3         */
 } hydra_kv8;
 
+/* Part of a paged KV cache (fp32 or 16 bits): what a text of any length keeps within bounds.  Slots are positions: node n of row b stands
+ * at position p = seq_len[b] + depth[n], and sees the cached slot s, or the node a among its ancestors at position s = seq_len[b] + depth[a], if
+ *   s >= first[b]  and  (window == 0  or  s > p - window  or  s < first[b] + n_sinks);
+ * itself always.  So a sliding window of `window` positions, with the first n_sinks positions kept in sight; slots below first[b] hold nothing any
+ * more (hydra_kv_evict).  Pages that hold no slot that a node of the call sees need no valid entry in kv.page_table (hydra_pages_release_span).
+ * A row with first[b] < 0 or first[b] > seq_len[b] is skipped and flagged (bit 0).
+ * score (NULL: none): attention weight received so far, by layer, row, head and slot, at [((layer * score_rows + b) * H + h) * 16 * kv.max_pages + s].
+ * Attention adds, for each cached slot that a node of the call sees, the weights that nodes 0 .. n_scored - 1 give it (the softmax's, which sum to
+ * one for a node and head), and sets those of the nodes' own slots seq_len[b] .. seq_len[b] + T - 1, which hold no token yet, to the weights
+ * that they got.  The sums are taken in a fixed order.  Start from zeros. */
+typedef struct {
+    hydra_kv       kv;                  /* pages 16-byte aligned; tables of up to 2^31 - 32 slots of a row */
+    int32_t       *first;               /* device [B], or NULL: 0 in every row      */
+    int32_t        n_sinks, window;     /* >= 0                                     */
+    int32_t        span_hint;           /* host upper bound on max_b (seq_len - first), or 0 = unknown: sizes launch grids only             */
+    int32_t        n_scored;            /* 0..T; used where score is given          */
+    float         *score;               /* device [n_layers, score_rows, H, 16 * kv.max_pages] or NULL */
+    int32_t        score_rows;          /* >= B where score is given                */
+} hydra_kv_span;
+
 /* The pages of a cache as a pool that rows take from, share and give back.  page_table[b, i] is the page of row b's slots
  * 16 i .. 16 i + 15, or -1 where the row holds none; ref[p] is the number of entries that name page p, 0 = free.  Both are
  * the caller's; before the first call the tables are all -1 and the counts all 0.  Calls on one pool must be ordered on one stream.
@@ -311,6 +331,19 @@ int accept_typical_static(hydra_ctx *ctx, void *stream, int B,
                           const int32_t *tree_tokens, const float *logits, float tau, float eps, float alpha,
                           const float *u, int32_t *n_acc, int32_t *path, int32_t *next_root, int32_t *last_node);
 
+/* What the model thinks of given tokens (section 6.3's p = softmax(logits[n] / tau), as accept_typical has it), row by row of the logits:
+ *   logprob[n] = log p(tokens[n])       rank[n] = number of tokens with a larger logit       entropy[n] = H(p) in nats
+ *   top_ids[n, i], top_logprobs[n, i]: the k most likely tokens in order (logit descending, token id ascending) and their log p
+ * tokens[n] = -1: no token (logprob 0, rank -1); any other one outside [0, V) is taken as 0 (flag bit 1).  A logit of -infinity has p = 0; a row with a NaN or
+ * +infinity, or without a finite logit, has NaN for what is computed from sums (NaN counts as -infinity in ranks and orders).
+ *   logits device [B, T, V] fp32: tree_verify_forward's optional output       tokens device [B, T] int32
+ *   logprob, entropy device [B, T] fp32 (out)       rank device [B, T] int32 (out)       each NULL where not wanted (tokens too, if neither logprob nor rank is)
+ *   top_ids [B, T, k] int32, top_logprobs [B, T, k] fp32 (out): NULL if k == 0
+ * Sums are fp32 and taken relative to the largest logit, so small entropies and log probabilities near 0 keep their digits.  k <= HYDRA_MAX_TOPK and <= V;
+ * tau and 1 / tau positive and finite. */
+int hydra_token_logprobs(hydra_ctx *ctx, void *stream, int B, void *ws, const float *logits, const int32_t *tokens, float tau, int k,
+                         float *logprob, int32_t *rank, float *entropy, int32_t *top_ids, float *top_logprobs);
+
 /* Sections 1 and 2 (speculative decoding: the accepted tokens are appended to the
  * sequence, the rest of the candidates is discarded; section 3: the next step's
  * heads read the hidden state of the last accepted token).
@@ -393,6 +426,49 @@ int hydra_kv8_seal(hydra_ctx *ctx, void *stream, int B, const int32_t *seq_len, 
  * [n_layers, B, n_slots, 2, H, Dh] with layer = -1.  Sealed slots come from the codes, others from kv->tail; slots whose
  * table entry is out of range are left as they are (flag bit 6).  Slots 0 .. 16 * tail.max_pages - 1 can be read. */
 int hydra_kv8_read(hydra_ctx *ctx, void *stream, int B, int layer, const hydra_kv8 *kv, int first_slot, int n_slots, float *kv_plain);
+
+/* ---- part of a cache: windows, accumulated weights, eviction ------------------- */
+
+/* tree_verify_forward and hydra_prefill_chunk behind part of a cache: K and V of the nodes go to their slots of span->kv, attention sees what
+ * hydra_kv_span says, and adds up its weights in span->score.  kv_compact takes &span->kv.  Errors as there. */
+int tree_verify_forward_span(hydra_ctx *ctx, void *stream, int B, void *ws,
+                             const int32_t *tree_tokens, const int32_t *seq_len, const hydra_kv_span *span,
+                             float *hidden, int32_t *argmax, float *margin, float *logits);
+int hydra_prefill_chunk_span(hydra_ctx *ctx, void *stream, int B, void *ws,
+                             const int32_t *tree_tokens, const int32_t *seq_len, const hydra_kv_span *span);
+
+/* The attention of one layer of tree_verify_forward_span on its own, in the format of its cache (fp32, or IEEE half for HYDRA_BF16):
+ *   q   device [B, T, H, Dh], already rotated, 16-byte aligned
+ *   out device [B, T, H, Dh], 16-byte aligned
+ * K/V of the T nodes must already be in slots seq_len[b] .. seq_len[b]+T-1 (see hydra_kv_write). */
+int tree_attention_span(hydra_ctx *ctx, void *stream, int B, int layer, void *ws,
+                        const void *q, const int32_t *seq_len, const hydra_kv_span *span, void *out);
+
+/* The accumulated weights of accepted nodes follow them: score slot seq_len + path[j] -> slot seq_len + j for j < n_acc, every layer and
+ * head.  Call it in front of kv_compact (seq_len is the length before that), where the accepted path is not the identity; a path that
+ * is not strictly increasing inside [0, T) ends at the offending entry (flag bit 2). */
+int hydra_score_compact(hydra_ctx *ctx, void *stream, int B, const int32_t *n_acc, const int32_t *path,
+                        const int32_t *seq_len, const hydra_kv_span *span);
+
+/* Eviction by accumulated weight.  Every row that holds more than keep + slack tokens (slots first[b] .. seq_len[b] - 1) is cut to `keep` of them:
+ * the first span->n_sinks, the last n_recent, and between those, for each layer and head on its own, the keep - n_sinks - n_recent ones with the
+ * largest score (ties: the lower slot; a NaN counts as -infinity).  In their order they become slots seq_len[b] - keep .. seq_len[b] - 1, their scores with
+ * them, and first[b] = seq_len[b] - keep; the last n_recent keep their slots, and so do positions of tokens to come.
+ *   dst_table NULL: in place.  A row one of whose pages has ref[page] > 1 (ref: device [n_pages], or NULL: no page is shared) then stays whole (flag bit 0)
+ *             otherwise device [B, kv.max_pages]: pages, other than any that a row still needs, that the kept tokens are copied to (logical
+ *             pages (seq_len - keep) / 16 .. (seq_len - 1) / 16); span->kv.page_table and what it names stay as they are, and the caller goes on with dst_table for the rows cut
+ *   kept      device [n_layers, B, H, keep] int32 (out): the slots that the tokens had; entries of rows that stay whole are left as they are
+ *   evicted   device [B] int32 (out): 1 = the row was cut
+ * A row with first < 0, first > seq_len or seq_len beyond its table is skipped (flag bit 0), one for whose slots a table has no valid entry too
+ * (bit 6).  Needs span->first and span->score; span->window and n_scored play no part. */
+int hydra_kv_evict(hydra_ctx *ctx, void *stream, int B, const int32_t *seq_len, const hydra_kv_span *span, int keep, int n_recent, int slack,
+                   const int32_t *dst_table, const int32_t *ref, int32_t *kept, int32_t *evicted);
+
+/* hydra_pages_release for rows of part of a cache: every page goes back that holds no slot which a node behind seq_len[b] tokens can see, whatever
+ * its depth, those behind the last token among them.
+ *   lo device [B] int32 (out) or NULL: the first slot of the window (first[b] where there is none): hydra_pages_reserve(lo, seq_len, T) then takes pages
+ *      for the T nodes of a step and not for what lies between sinks and window */
+int hydra_pages_release_span(hydra_ctx *ctx, void *stream, int B, const hydra_pages *pages, const int32_t *seq_len, const hydra_kv_span *span, int32_t *lo);
 
 /* ---- pages: take, give back, share, move -------------------------------------- */
 

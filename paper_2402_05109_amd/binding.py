@@ -28,7 +28,9 @@ EXPORTS = ["hydra_create", "hydra_destroy", "hydra_last_error", "hydra_weights_b
            "tree_verify_forward", "tree_attention", "accept_greedy", "accept_typical", "accept_typical_static", "kv_compact", "hydra_prefill_chunk", "hydra_prefix_attention", "hydra_tree_depth",
            "hydra_kv_write", "hydra_kv_read", "hydra_profile_begin", "hydra_profile_end", "hydra_layer_kernel_info",
            "tree_verify_forward_kv8", "hydra_prefill_chunk_kv8", "tree_attention_kv8", "hydra_kv8_seal", "hydra_kv8_read", "hydra_pages_workspace_bytes",
-           "hydra_pages_reserve", "hydra_pages_release", "hydra_pages_fork", "hydra_pages_compact", "hydra_kv_copy_pages", "hydra_kv8_copy_pages"]
+           "hydra_pages_reserve", "hydra_pages_release", "hydra_pages_fork", "hydra_pages_compact", "hydra_kv_copy_pages", "hydra_kv8_copy_pages",
+           "tree_verify_forward_span", "hydra_prefill_chunk_span", "tree_attention_span", "hydra_score_compact", "hydra_kv_evict", "hydra_pages_release_span",
+           "hydra_token_logprobs"]
 
 
 class ModelDesc(C.Structure):
@@ -54,6 +56,11 @@ class KVDesc(C.Structure):
 class KV8Desc(C.Structure):
     _fields_ = [("tail", KVDesc), ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("scales", C.c_void_p), ("page_table", C.c_void_p),
                 ("n_sealed", C.c_void_p), ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("format", C.c_int32)]
+
+
+class KVSpanDesc(C.Structure):
+    _fields_ = [("kv", KVDesc), ("first", C.c_void_p), ("n_sinks", C.c_int32), ("window", C.c_int32), ("span_hint", C.c_int32), ("n_scored", C.c_int32),
+                ("score", C.c_void_p), ("score_rows", C.c_int32)]
 
 
 class PagesDesc(C.Structure):
@@ -108,6 +115,14 @@ def _load() -> C.CDLL:
     lib.hydra_pages_compact.argtypes = [vp, vp, i32, vp, pg, vp, vp, vp]
     lib.hydra_kv_copy_pages.argtypes = [vp, vp, C.POINTER(KVDesc), i32, vp, vp, vp]
     lib.hydra_kv8_copy_pages.argtypes = [vp, vp, kv8, i32, vp, vp, vp]
+    span = C.POINTER(KVSpanDesc)
+    lib.tree_verify_forward_span.argtypes = [vp, vp, i32, vp, vp, vp, span, vp, vp, vp, vp]
+    lib.hydra_prefill_chunk_span.argtypes = [vp, vp, i32, vp, vp, vp, span]
+    lib.tree_attention_span.argtypes = [vp, vp, i32, i32, vp, vp, vp, span, vp]
+    lib.hydra_score_compact.argtypes = [vp, vp, i32, vp, vp, vp, span]
+    lib.hydra_kv_evict.argtypes = [vp, vp, i32, vp, span, i32, i32, i32, vp, vp, vp, vp]
+    lib.hydra_pages_release_span.argtypes = [vp, vp, i32, pg, vp, span, vp]
+    lib.hydra_token_logprobs.argtypes = [vp, vp, i32, vp, vp, vp, C.c_float, i32, vp, vp, vp, vp, vp]
     return lib
 
 
@@ -177,6 +192,22 @@ class KV8:
                        self.n_sealed.data_ptr(), self.n_pages, self.max_pages, self.format)
 
 
+class KVSpan:
+    """Part of a caller-owned paged KV cache: window, sinks, what is left after evictions, accumulated weights (see hydra_kv_span in the header)."""
+
+    def __init__(self, kv: KV, first: Optional[torch.Tensor] = None, n_sinks: int = 0, window: int = 0, span_hint: int = 0,
+                 score: Optional[torch.Tensor] = None, n_scored: int = 0):
+        _ptr(first, torch.int32, "first"), _ptr(score, torch.float32, "score")
+        if score is not None and (score.dim() != 4 or score.shape[-1] != 16 * kv.max_pages):
+            raise ValueError(f"score: expected [n_layers, rows, H, {16 * kv.max_pages}], got {tuple(score.shape)}")
+        self.kv, self.first, self.score = kv, first, score
+        self.n_sinks, self.window, self.span_hint, self.n_scored = int(n_sinks), int(window), int(span_hint), int(n_scored)
+
+    def desc(self) -> KVSpanDesc:
+        return KVSpanDesc(self.kv.desc(), None if self.first is None else self.first.data_ptr(), self.n_sinks, self.window, self.span_hint, self.n_scored,
+                          None if self.score is None else self.score.data_ptr(), 0 if self.score is None else self.score.shape[1])
+
+
 class Pages:
     """Caller-owned page tables [B, max_pages] and counts [n_pages] of a pool of pages (see hydra_pages in the header)."""
 
@@ -209,6 +240,7 @@ class Hydra:
         self.max_batch = max_batch
         self.depth = _lib.hydra_tree_depth(self._h)
         self.torch_dtype = torch.bfloat16 if dtype == HYDRA_BF16 else torch.float32
+        self._cache_dtype = torch.float16 if dtype == HYDRA_BF16 else torch.float32
 
     def close(self):
         if getattr(self, "_h", None) and _lib is not None:
@@ -282,6 +314,12 @@ class Hydra:
                                           _ptr(path, torch.int32, "path"), _ptr(next_root, torch.int32, "next_root"),
                                           _ptr(last_node, torch.int32, "last_node")))
 
+    def hydra_token_logprobs(self, B, ws, logits, tokens, tau=1.0, k=0, logprob=None, rank=None, entropy=None, top_ids=None, top_logprobs=None) -> None:
+        _check(_lib.hydra_token_logprobs(self._h, _stream(), B, _ptr(ws, torch.uint8, "ws"), _ptr(logits, torch.float32, "logits"),
+                                         _ptr(tokens, torch.int32, "tokens"), float(tau), int(k), _ptr(logprob, torch.float32, "logprob"),
+                                         _ptr(rank, torch.int32, "rank"), _ptr(entropy, torch.float32, "entropy"), _ptr(top_ids, torch.int32, "top_ids"),
+                                         _ptr(top_logprobs, torch.float32, "top_logprobs")))
+
     def kv_compact(self, B, n_acc, path, next_root, last_node, hidden, kv: KV, seq_len, h_last, root, kv_index=None) -> None:
         d = kv.desc()
         _check(_lib.kv_compact(self._h, _stream(), B, _ptr(n_acc, torch.int32, "n_acc"), _ptr(path, torch.int32, "path"),
@@ -321,6 +359,38 @@ class Hydra:
     def kv8_read(self, B, layer, kv: KV8, first_slot, n_slots, plain) -> None:
         d = kv.desc()
         _check(_lib.hydra_kv8_read(self._h, _stream(), B, layer, C.byref(d), first_slot, n_slots, _ptr(plain, torch.float32, "kv_plain")))
+
+    # ---- part of a cache
+    def tree_verify_forward_span(self, B, ws, tree_tokens, seq_len, span: KVSpan, hidden, argmax, margin=None, logits=None) -> None:
+        d = span.desc()
+        _check(_lib.tree_verify_forward_span(self._h, _stream(), B, _ptr(ws, torch.uint8, "ws"), _ptr(tree_tokens, torch.int32, "tree_tokens"),
+                                             _ptr(seq_len, torch.int32, "seq_len"), C.byref(d), _ptr(hidden, torch.float32, "hidden"),
+                                             _ptr(argmax, torch.int32, "argmax"), _ptr(margin, torch.float32, "margin"), _ptr(logits, torch.float32, "logits")))
+
+    def hydra_prefill_chunk_span(self, B, ws, tree_tokens, seq_len, span: KVSpan) -> None:
+        d = span.desc()
+        _check(_lib.hydra_prefill_chunk_span(self._h, _stream(), B, _ptr(ws, torch.uint8, "ws"), _ptr(tree_tokens, torch.int32, "tree_tokens"),
+                                             _ptr(seq_len, torch.int32, "seq_len"), C.byref(d)))
+
+    def tree_attention_span(self, B, layer, ws, q, seq_len, span: KVSpan, out) -> None:
+        d = span.desc()
+        _check(_lib.tree_attention_span(self._h, _stream(), B, layer, _ptr(ws, torch.uint8, "ws"), _ptr(q, self._cache_dtype, "q"),
+                                        _ptr(seq_len, torch.int32, "seq_len"), C.byref(d), _ptr(out, self._cache_dtype, "out")))
+
+    def hydra_score_compact(self, B, n_acc, path, seq_len, span: KVSpan) -> None:
+        d = span.desc()
+        _check(_lib.hydra_score_compact(self._h, _stream(), B, _ptr(n_acc, torch.int32, "n_acc"), _ptr(path, torch.int32, "path"),
+                                        _ptr(seq_len, torch.int32, "seq_len"), C.byref(d)))
+
+    def hydra_kv_evict(self, B, seq_len, span: KVSpan, keep, n_recent, slack, kept, evicted, dst_table=None, ref=None) -> None:
+        d = span.desc()
+        _check(_lib.hydra_kv_evict(self._h, _stream(), B, _ptr(seq_len, torch.int32, "seq_len"), C.byref(d), int(keep), int(n_recent), int(slack),
+                                   _ptr(dst_table, torch.int32, "dst_table"), _ptr(ref, torch.int32, "ref"), _ptr(kept, torch.int32, "kept"),
+                                   _ptr(evicted, torch.int32, "evicted")))
+
+    def hydra_pages_release_span(self, B, pages: Pages, seq_len, span: KVSpan, lo=None) -> None:
+        d, s = pages.desc(), span.desc()
+        _check(_lib.hydra_pages_release_span(self._h, _stream(), B, C.byref(d), _ptr(seq_len, torch.int32, "seq_len"), C.byref(s), _ptr(lo, torch.int32, "lo")))
 
     # ---- pages
     def hydra_pages_reserve(self, B, ws, pages: Pages, lo, hi, extra, ok=None) -> None:

@@ -147,6 +147,8 @@ WsLayout ws_layout(const hydra_ctx *c, int B) {
     w.ss = off;    off += align_up((d / 32 + 1) * rows * 4, 256);
     w.topk = off;  off += align_up(topk_scratch_bytes(c, (int)std::max<size_t>(Md, 1)), 256);
     w.mega = off;  off += align_up(layers_mega_ws_bytes(c, B), 256);     // per-layer buffers of the persistent layer kernel (0 if the shape cannot take it)
+    w.stats = off; off += align_up((size_t)B * c->m.n_heads * Tq * 8, 256);
+    w.logprob = off; off += align_up(logprob_scratch_bytes(c, (int)M), 256);
     w.total = off;
     return w;
 }
@@ -186,6 +188,30 @@ static int check_kv8(hydra_ctx *c, const hydra_kv8 *kv) {
         return fail(HYDRA_E_INVALID_ARG, "kv8: codes and tail pages must be 16-byte aligned");
     if ((uintptr_t)kv->scales & 7) return fail(HYDRA_E_INVALID_ARG, "kv8: scales must be 8-byte aligned");
     return HYDRA_OK;
+}
+
+static int check_span(hydra_ctx *c, int B, const hydra_kv_span *span) {
+    if (!span) return fail(HYDRA_E_INVALID_ARG, "span is NULL");
+    int rc = check_kv(c, &span->kv);
+    if (rc) return rc;
+    // slots are ints, and attention counts to the end of a tile of 32 behind the last one
+    if (span->kv.max_pages > INT_MAX / HYDRA_PAGE - 1) return fail(HYDRA_E_CAPACITY, "span: a table of more than 2^31 - 32 slots");
+    if (((uintptr_t)span->kv.k_pages | (uintptr_t)span->kv.v_pages) & 15) return fail(HYDRA_E_INVALID_ARG, "span: pages must be 16-byte aligned");
+    if (span->n_sinks < 0 || span->window < 0 || span->span_hint < 0) return fail(HYDRA_E_INVALID_ARG, "span: n_sinks, window or span_hint is negative");
+    if (span->score) {
+        if (span->n_scored < 0 || span->n_scored > c->tree.T) return fail(HYDRA_E_INVALID_ARG, "span: n_scored outside [0, T]");
+        if (span->score_rows < B) return fail(HYDRA_E_CAPACITY, "span: score has fewer rows than B");
+    }
+    return HYDRA_OK;
+}
+
+// Where attention over part of a cache leaves the records of workgroups that share a head's keys, and for how many there is room: in the fp32 family, whose
+// own attention has none, the larger of two buffers that are not in use then.
+static float *span_records(const hydra_ctx *c, int B, const WsLayout &w, char *W, int *units) {
+    if (c->bf16) { *units = w.attn_units; return (float *)(W + w.apart); }
+    const size_t Tq = align_up(c->tree.T, 32), rec = (size_t)B * c->m.n_heads * (Tq * c->m.head_dim + 2 * Tq) * 4, xb = w.part - w.xb, part = w.qbuf - w.part;
+    *units = (int)std::min<size_t>(std::max(xb, part) / rec, 16);
+    return (float *)(W + (xb >= part ? w.xb : w.part));
 }
 
 static inline int32_t *flags_ptr(hydra_ctx *c) {
@@ -293,6 +319,9 @@ int hydra_bind_weights(hydra_ctx *c, void *stream, void *arena, int table_slot) 
         if ((rc = attn_max_dynamic_lds(c))) return rc;
         if ((rc = layers_mega_set_attr(c))) return rc;
         if ((rc = kv8_max_dynamic_lds())) return rc;
+        if ((rc = span_max_dynamic_lds())) return rc;
+    } else if (int rc = span_f32_max_dynamic_lds()) {
+        return rc;
     }
     return HYDRA_OK;
 }
@@ -481,13 +510,14 @@ static int lm_head_tail(hydra_ctx *c, hipStream_t s, const float *x, const void 
 // The decoder layers of the context over its B * T tree rows.  lm_tail: final RMSNorm, LM head, argmax (the
 // verify step); otherwise the residual stream after the last layer is left in the workspace's x, unless the rows are tokens: those
 // take the same kernels with and without the tail, also the persistent layer kernel, which has a buffer of its own for it.
-// kv8 (16-bit family): the cache whose tail `kv` is; attention then reads its sealed pages.
+// kv8 (16-bit family): the cache whose tail `kv` is; attention then reads its sealed pages.  span: the part of `kv` that attention sees.
 static int forward_layers(hydra_ctx *c, hipStream_t s, int B, void *ws, const RowSource &src, const int32_t *seq_len,
-                          const hydra_kv *kv, const hydra_kv8 *kv8, bool lm_tail, float *hidden, int32_t *argmax, float *margin, float *logits) {
+                          const hydra_kv *kv, const hydra_kv8 *kv8, const hydra_kv_span *span, bool lm_tail, float *hidden, int32_t *argmax, float *margin, float *logits) {
     int rc;
     const WsLayout w = ws_layout(c, B);
     char *W = (char *)ws, *A = c->arena;
     float *x = (float *)(W + w.x), *part = (float *)(W + w.part), *apart = (float *)(W + w.apart);
+    float *stats = (float *)(W + w.stats);
     void *xa = W + w.xa, *xb = W + w.xb, *qbuf = W + w.qbuf;
     int32_t *flags = flags_ptr(c);
     const int d = c->m.d, F = c->m.ffn, V = c->m.vocab, M = B * c->tree.T;
@@ -498,7 +528,7 @@ static int forward_layers(hydra_ctx *c, hipStream_t s, int B, void *ws, const Ro
         const int Mpad = (int)align_up(std::max<size_t>(M, 1), 128);
         RowScale rs = {ss, 1, Mpad, d, c->m.rms_eps};        // rs.nb: rows of ss the last producer filled (1 = a complete sum per row)
         const float *gain0 = (const float *)(A + c->layer[0].attn_norm);
-        if (src.tokens && !kv8 && layers_mega_eligible(c, B, kv)) {
+        if (src.tokens && !kv8 && !span && layers_mega_eligible(c, B, kv)) {
             // up to 64 rows and a bounded context: all layers in one persistent kernel (bf16_layers.hip)
             LayersMegaIO io;
             if ((rc = launch_layers_mega(c, s, B, W + w.mega, seq_len, kv, flags, &io, false))) return rc;
@@ -513,8 +543,9 @@ static int forward_layers(hydra_ctx *c, hipStream_t s, int B, void *ws, const Ro
         for (int l = 0; l < c->m.n_layers; ++l) {
             const LayerOff &o = c->layer[l];
             const float *next_gain = (const float *)(A + (l + 1 < c->m.n_layers ? c->layer[l + 1].attn_norm : c->off_final_norm));
-            if ((rc = launch_gemm_qkv_rope(c, s, xa, A + o.wqkv, M, rs, l, seq_len, kv, qbuf, part, flags, !kv8))) return rc;
-            if (kv8) { if ((rc = launch_kv8_attention(c, s, B, l, qbuf, false, seq_len, kv8, apart, w.attn_units, xb, flags))) return rc; }
+            if ((rc = launch_gemm_qkv_rope(c, s, xa, A + o.wqkv, M, rs, l, seq_len, kv, qbuf, part, flags, !kv8 && !span))) return rc;
+            if (span) { if ((rc = launch_span_attention(c, s, B, l, qbuf, false, seq_len, span, apart, w.attn_units, stats, xb, flags))) return rc; }
+            else if (kv8) { if ((rc = launch_kv8_attention(c, s, B, l, qbuf, false, seq_len, kv8, apart, w.attn_units, xb, flags))) return rc; }
             else     { if ((rc = launch_attention(c, s, B, l, qbuf, seq_len, kv, apart, w.attn_units, xb, nullptr, flags))) return rc; }
             if ((rc = launch_gemm_resid(c, s, xb, A + o.wo, M, d, d, x, (const float *)(A + o.ffn_norm), xa, ss, Mpad, part, &rs.nb))) return rc;
             if ((rc = launch_gemm_silu(c, s, xa, A + o.wgu, M, F, d, ss, rs.nb, Mpad, xb))) return rc;
@@ -529,7 +560,11 @@ static int forward_layers(hydra_ctx *c, hipStream_t s, int B, void *ws, const Ro
         const LayerOff &o = c->layer[l];
         auto weights = [&](size_t off) { return (const float *)(A + off); };
         if ((rc = launch_f32_qkv_rope(c, s, x, weights(o.attn_norm), weights(o.wqkv), M, l, seq_len, kv, (float *)qbuf, flags))) return rc;
-        if ((rc = launch_attention(c, s, B, l, qbuf, seq_len, kv, apart, w.attn_units, xa, nullptr, flags))) return rc;
+        if (span) {
+            int units;
+            float *records = span_records(c, B, w, W, &units);
+            if ((rc = launch_span_attention(c, s, B, l, qbuf, true, seq_len, span, records, units, stats, xa, flags))) return rc;
+        } else if ((rc = launch_attention(c, s, B, l, qbuf, seq_len, kv, apart, w.attn_units, xa, nullptr, flags))) return rc;
         if ((rc = launch_f32_add(c, s, (const float *)xa, weights(o.wo), x, M, d))) return rc;
         if ((rc = launch_f32_swiglu(c, s, x, weights(o.ffn_norm), weights(o.wgu), (float *)xb, M))) return rc;
         if ((rc = launch_f32_add(c, s, (const float *)xb, weights(o.wdown), x, M, F))) return rc;
@@ -555,7 +590,7 @@ int tree_verify_forward(hydra_ctx *c, void *stream, int B, void *ws, const int32
     if (!tree_tokens || !seq_len || !hidden || !argmax) return fail(HYDRA_E_INVALID_ARG, "tree_verify_forward: NULL argument");
     if ((rc = check_kv(c, kv))) return rc;
     const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
-    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, kv, nullptr, true, hidden, argmax, margin, logits);
+    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, kv, nullptr, nullptr, true, hidden, argmax, margin, logits);
 }
 
 int hydra_prefill_chunk(hydra_ctx *c, void *stream, int B, void *ws, const int32_t *tree_tokens, const int32_t *seq_len, const hydra_kv *kv) {
@@ -564,7 +599,7 @@ int hydra_prefill_chunk(hydra_ctx *c, void *stream, int B, void *ws, const int32
     if (!tree_tokens || !seq_len) return fail(HYDRA_E_INVALID_ARG, "hydra_prefill_chunk: NULL argument");
     if ((rc = check_kv(c, kv))) return rc;
     const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
-    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, kv, nullptr, false, nullptr, nullptr, nullptr, nullptr);
+    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, kv, nullptr, nullptr, false, nullptr, nullptr, nullptr, nullptr);
 }
 
 // ---------------------------------------------------------------------------
@@ -577,7 +612,7 @@ int tree_verify_forward_kv8(hydra_ctx *c, void *stream, int B, void *ws, const i
     if (!tree_tokens || !seq_len || !hidden || !argmax) return fail(HYDRA_E_INVALID_ARG, "tree_verify_forward_kv8: NULL argument");
     if ((rc = check_kv8(c, kv))) return rc;
     const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
-    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, &kv->tail, kv, true, hidden, argmax, margin, logits);
+    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, &kv->tail, kv, nullptr, true, hidden, argmax, margin, logits);
 }
 
 int hydra_prefill_chunk_kv8(hydra_ctx *c, void *stream, int B, void *ws, const int32_t *tree_tokens, const int32_t *seq_len, const hydra_kv8 *kv) {
@@ -586,7 +621,7 @@ int hydra_prefill_chunk_kv8(hydra_ctx *c, void *stream, int B, void *ws, const i
     if (!tree_tokens || !seq_len) return fail(HYDRA_E_INVALID_ARG, "hydra_prefill_chunk_kv8: NULL argument");
     if ((rc = check_kv8(c, kv))) return rc;
     const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
-    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, &kv->tail, kv, false, nullptr, nullptr, nullptr, nullptr);
+    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, &kv->tail, kv, nullptr, false, nullptr, nullptr, nullptr, nullptr);
 }
 
 int tree_attention_kv8(hydra_ctx *c, void *stream, int B, int layer, void *ws, const void *q, const int32_t *seq_len, const hydra_kv8 *kv, void *out) {
@@ -624,6 +659,79 @@ int hydra_kv8_read(hydra_ctx *c, void *stream, int B, int layer, const hydra_kv8
 }
 
 // ---------------------------------------------------------------------------
+// part of a cache
+// ---------------------------------------------------------------------------
+int tree_verify_forward_span(hydra_ctx *c, void *stream, int B, void *ws, const int32_t *tree_tokens, const int32_t *seq_len, const hydra_kv_span *span,
+                             float *hidden, int32_t *argmax, float *margin, float *logits) {
+    int rc = check_common(c, B, ws);
+    if (rc) return rc;
+    if (!tree_tokens || !seq_len || !hidden || !argmax) return fail(HYDRA_E_INVALID_ARG, "tree_verify_forward_span: NULL argument");
+    if ((rc = check_span(c, B, span))) return rc;
+    const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
+    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, &span->kv, nullptr, span, true, hidden, argmax, margin, logits);
+}
+
+int hydra_prefill_chunk_span(hydra_ctx *c, void *stream, int B, void *ws, const int32_t *tree_tokens, const int32_t *seq_len, const hydra_kv_span *span) {
+    int rc = check_common(c, B, ws);
+    if (rc) return rc;
+    if (!tree_tokens || !seq_len) return fail(HYDRA_E_INVALID_ARG, "hydra_prefill_chunk_span: NULL argument");
+    if ((rc = check_span(c, B, span))) return rc;
+    const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
+    return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, &span->kv, nullptr, span, false, nullptr, nullptr, nullptr, nullptr);
+}
+
+int tree_attention_span(hydra_ctx *c, void *stream, int B, int layer, void *ws, const void *q, const int32_t *seq_len, const hydra_kv_span *span, void *out) {
+    int rc = check_common(c, B, ws);
+    if (rc) return rc;
+    if (!q || !seq_len || !out) return fail(HYDRA_E_INVALID_ARG, "tree_attention_span: NULL argument");
+    if (((uintptr_t)q | (uintptr_t)out) & 15) return fail(HYDRA_E_INVALID_ARG, "tree_attention_span: q and out must be 16-byte aligned");
+    if (layer < 0 || layer >= c->m.n_layers) return fail(HYDRA_E_INVALID_ARG, "layer out of range");
+    if ((rc = check_span(c, B, span))) return rc;
+    const WsLayout w = ws_layout(c, B);
+    int units;
+    float *records = span_records(c, B, w, (char *)ws, &units);
+    return launch_span_attention(c, (hipStream_t)stream, B, layer, q, true, seq_len, span, records, units, (float *)((char *)ws + w.stats), out, flags_ptr(c));
+}
+
+// of calls that work on the scores of a span
+static int check_scores(hydra_ctx *c, int B, const int32_t *seq_len, const hydra_kv_span *span) {
+    if (B < 1 || B > c->max_batch) return fail(HYDRA_E_CAPACITY, "B outside [1, max_batch]");
+    if (!c->arena) return fail(HYDRA_E_STATE, "no weight arena bound");
+    if (!seq_len) return fail(HYDRA_E_INVALID_ARG, "seq_len is NULL");
+    int rc = check_span(c, B, span);
+    if (rc) return rc;
+    if (!span->score) return fail(HYDRA_E_INVALID_ARG, "span: score is NULL");
+    return HYDRA_OK;
+}
+
+int hydra_score_compact(hydra_ctx *c, void *stream, int B, const int32_t *n_acc, const int32_t *path, const int32_t *seq_len, const hydra_kv_span *span) {
+    if (!c || !n_acc || !path) return fail(HYDRA_E_INVALID_ARG, "hydra_score_compact: NULL argument");
+    int rc = check_scores(c, B, seq_len, span);
+    if (rc) return rc;
+    return launch_score_compact(c, (hipStream_t)stream, B, n_acc, path, seq_len, span);
+}
+
+int hydra_kv_evict(hydra_ctx *c, void *stream, int B, const int32_t *seq_len, const hydra_kv_span *span, int keep, int n_recent, int slack, const int32_t *dst_table,
+                   const int32_t *ref, int32_t *kept, int32_t *evicted) {
+    if (!c || !kept || !evicted) return fail(HYDRA_E_INVALID_ARG, "hydra_kv_evict: NULL argument");
+    int rc = check_scores(c, B, seq_len, span);
+    if (rc) return rc;
+    if (!span->first) return fail(HYDRA_E_INVALID_ARG, "hydra_kv_evict: span->first is NULL");
+    if (keep < 1 || n_recent < 0 || slack < 0) return fail(HYDRA_E_INVALID_ARG, "hydra_kv_evict: need keep >= 1, n_recent >= 0, slack >= 0");
+    if ((int64_t)span->n_sinks + n_recent > keep) return fail(HYDRA_E_SHAPE, "hydra_kv_evict: more sinks and recent tokens than are kept");
+    if (dst_table == span->kv.page_table) return fail(HYDRA_E_INVALID_ARG, "hydra_kv_evict: dst_table is the cache's own table (NULL: in place)");
+    return launch_kv_evict(c, (hipStream_t)stream, B, seq_len, span, keep, n_recent, slack, dst_table, ref, kept, evicted);
+}
+
+int hydra_pages_release_span(hydra_ctx *c, void *stream, int B, const hydra_pages *pages, const int32_t *seq_len, const hydra_kv_span *span, int32_t *lo) {
+    int rc = check_pages(c, B, pages);
+    if (rc) return rc;
+    if (!seq_len || !span) return fail(HYDRA_E_INVALID_ARG, "hydra_pages_release_span: NULL argument");
+    if (span->n_sinks < 0 || span->window < 0) return fail(HYDRA_E_INVALID_ARG, "span: n_sinks or window is negative");
+    return launch_release_span(c, (hipStream_t)stream, B, pages, seq_len, span, lo);
+}
+
+// ---------------------------------------------------------------------------
 // Hydra++ prefix attention
 // ---------------------------------------------------------------------------
 int hydra_prefix_attention(hydra_ctx *c, void *stream, int B, void *ws, const float *hidden, int T_src,
@@ -638,7 +746,7 @@ int hydra_prefix_attention(hydra_ctx *c, void *stream, int B, void *ws, const fl
     if ((rc = check_kv(c, kv))) return rc;
     hipStream_t s = (hipStream_t)stream;
     const RowSource src = {nullptr, hidden, T_src, path, n_acc};
-    if ((rc = forward_layers(c, s, B, ws, src, seq_len, kv, nullptr, false, nullptr, nullptr, nullptr, nullptr))) return rc;
+    if ((rc = forward_layers(c, s, B, ws, src, seq_len, kv, nullptr, nullptr, false, nullptr, nullptr, nullptr, nullptr))) return rc;
     const WsLayout w = ws_layout(c, B);
     return launch_prefix_select(c, s, B, (const float *)((char *)ws + w.x), n_acc, kv, seq_len, h_out);
 }
@@ -683,6 +791,20 @@ int accept_typical(hydra_ctx *c, void *stream, int B, void *ws, const int32_t *t
     int32_t *ok = (int32_t *)((char *)ws + w.part);          // B * T flags; the GEMM partial buffer is free between calls
     return launch_accept_typical(c, (hipStream_t)stream, B, tree_tokens, logits, tau, eps, alpha, u, ok, flags_ptr(c), n_acc, path,
                                  next_root, last_node);
+}
+
+int hydra_token_logprobs(hydra_ctx *c, void *stream, int B, void *ws, const float *logits, const int32_t *tokens, float tau, int k, float *logprob, int32_t *rank,
+                         float *entropy, int32_t *top_ids, float *top_logprobs) {
+    int rc = check_common(c, B, ws);
+    if (rc) return rc;
+    if (!logits || ((logprob || rank) && !tokens) || (k > 0 && (!top_ids || !top_logprobs)) || (!logprob && !rank && !entropy && k == 0))
+        return fail(HYDRA_E_INVALID_ARG, "hydra_token_logprobs: NULL argument");
+    if (!(tau > 0.f) || !(tau < INFINITY) || !(1.0f / tau < INFINITY)) return fail(HYDRA_E_INVALID_ARG, "hydra_token_logprobs: tau and 1 / tau must be positive and finite");
+    if (k < 0 || k > HYDRA_MAX_TOPK || k > c->m.vocab) return fail(HYDRA_E_UNSUPPORTED, "hydra_token_logprobs: k outside [0, min(32, V)]");
+    if (!logprob_fits(c)) return fail(HYDRA_E_UNSUPPORTED, "hydra_token_logprobs: more than 2^21 tokens");
+    const WsLayout w = ws_layout(c, B);
+    return launch_token_logprobs(c, (hipStream_t)stream, B * c->tree.T, (float *)((char *)ws + w.logprob), logits, logprob || rank ? tokens : nullptr, tau, k, logprob, rank,
+                                 entropy, top_ids, top_logprobs);
 }
 
 int kv_compact(hydra_ctx *c, void *stream, int B, const int32_t *n_acc, const int32_t *path,

@@ -98,7 +98,7 @@ inline int    ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // ---- workspace ------------------------------------------------------------
 struct WsLayout {
-    size_t flags, x, xa, xb, part, qbuf, apart, z, ss, topk, mega, total;
+    size_t flags, x, xa, xb, part, qbuf, apart, z, ss, topk, mega, stats, logprob, total;
     int attn_units;     // split-KV units per (row, head, query group)
 };
 WsLayout ws_layout(const hydra_ctx *c, int B);
@@ -207,6 +207,23 @@ int launch_kv8_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const vo
 int kv8_max_dynamic_lds();
 int launch_kv8_seal(hydra_ctx *c, hipStream_t s, int B, const int32_t *seq_len, const hydra_kv8 *kv);
 int launch_kv8_read(hydra_ctx *c, hipStream_t s, int B, int layer, const hydra_kv8 *kv, int first_slot, int n_slots, float *plain);
+
+// part of a cache (span_attn.hip, span_f32.hip, span_evict.hip).  plain: queries and result are [B, T, H, Dh] in the cache's format; otherwise, in the 16-bit
+// family, qbuf and the next GEMM's input.  stats: 2 floats per query and head, where the span has scores
+int launch_span_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const void *q, bool plain, const int32_t *seq_len, const hydra_kv_span *span,
+                          float *apart, int units_max, float *stats, void *out, int32_t *flags);
+int span_max_dynamic_lds();
+int span_f32_max_dynamic_lds();
+int launch_kv_evict(hydra_ctx *c, hipStream_t s, int B, const int32_t *seq_len, const hydra_kv_span *span, int keep, int n_recent, int slack, const int32_t *dst_table,
+                    const int32_t *ref, int32_t *kept, int32_t *evicted);
+int launch_score_compact(hydra_ctx *c, hipStream_t s, int B, const int32_t *n_acc, const int32_t *path, const int32_t *seq_len, const hydra_kv_span *span);
+int check_pages(hydra_ctx *c, int B, const hydra_pages *p);             // arguments that the calls on a pool of pages share
+int launch_release_span(hydra_ctx *c, hipStream_t s, int B, const hydra_pages *pages, const int32_t *seq_len, const hydra_kv_span *span, int32_t *lo);
+// log probabilities (logprobs.hip)
+bool logprob_fits(const hydra_ctx *c);                                  // whether the vocabulary does
+size_t logprob_scratch_bytes(const hydra_ctx *c, int rows);
+int launch_token_logprobs(hydra_ctx *c, hipStream_t s, int rows, float *records, const float *logits, const int32_t *tokens, float tau, int k, float *logprob, int32_t *rank,
+                          float *entropy, int32_t *top_ids, float *top_logprobs);
 
 inline const TreeDev *tree_dev(const hydra_ctx *c) {
     return reinterpret_cast<const TreeDev *>(c->arena + c->off_tables + (size_t)c->table_slot * TABLE_SLOT_BYTES);

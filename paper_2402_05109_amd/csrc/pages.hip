@@ -456,7 +456,7 @@ static int launch_copy(hydra_ctx *c, hipStream_t s, CopyPlanes pl, int n, const 
     return HYDRA_OK;
 }
 
-static int check_pages(hydra_ctx *c, int B, const hydra_pages *p) {
+int check_pages(hydra_ctx *c, int B, const hydra_pages *p) {
     if (!c) return fail(HYDRA_E_INVALID_ARG, "ctx is NULL");
     if (B < 1 || B > c->max_batch) return fail(HYDRA_E_CAPACITY, "B outside [1, max_batch]");
     if (!c->arena) return fail(HYDRA_E_STATE, "no weight arena bound (hydra_bind_weights)");

@@ -1,0 +1,455 @@
+// Tree attention over part of a 16-bit cache: a sliding window, the first tokens that stay in sight, what evictions have left; and the sums of
+// the weights that every slot receives, by which tokens are evicted.
+//
+// A query is a column of both products, S^T = K Q^T and O^T = V^T P^T, as in bf16_attn.hip, so maxima, sums, masks and rescale factors are per-lane scalars
+// and the weights are in the order that the second product needs.  With c = log2(e) / sqrt(Dh), M the running maximum of the unscaled scores z of a query,
+//     w = 2^((z - M) c),   l = sum w,   O = sum half(w) V,   result = O / l
+// Only tiles that some node sees are read: those of the sinks and those from the root's window on (SpanRow); masks are made for the tiles at the edges.
+#include <algorithm>
+#include <climits>
+
+#include "attn_bf16.h"
+#include "span.h"
+
+namespace hydra {
+
+static constexpr float LOG2E = 1.44269504f;
+
+// 16 bytes of a query: dims d0 .. d0 + 7 of column `col` of a query tile (queries past the last one: zeros, or whatever the packed buffer holds; nobody
+// stores their result)
+template <int DH>
+__device__ __forceinline__ u32x4_t span_query_piece(const SpanArgs &p, int b, int h, int qtile, int QTtot, int col, int d0) {
+    if (!p.plain) return reinterpret_cast<const u32x4_t *>(p.q)[((((size_t)b * p.H + h) * QTtot + qtile) * (DH / 16) + (d0 >> 4)) * 64 + ((d0 >> 3) & 1) * 32 + col];
+    const int query = qtile * 32 + col;
+    u32x4_t v = {0u, 0u, 0u, 0u};
+    if (query < p.T) v = *reinterpret_cast<const u32x4_t *>(reinterpret_cast<const a16_t *>(p.q) + ((size_t)(b * p.T + query) * p.H + h) * DH + d0);
+    return v;
+}
+// four dims of a result
+template <int DH>
+__device__ __forceinline__ void span_store(const SpanArgs &p, int m, int h, int dim, f32x4_t v) {
+    a16_t *to = reinterpret_cast<a16_t *>(p.out) + (p.plain ? ((size_t)m * p.H + h) * DH + dim : x_index<true>(m, h * DH + dim, p.H * DH));
+    *reinterpret_cast<u32x2_t *>(to) = u32x2_t{f2a_pack(v[0], v[1]), f2a_pack(v[2], v[3])};
+}
+
+static size_t span_lds_bytes(int Dh, int qt, int nw) {        // queries and tiles, or maxima, sums and O of one query tile
+    return std::max(((size_t)qt * (Dh / 16) + (size_t)nw * (Dh / 8)) * 1024, (size_t)qt * nw * 256 + (size_t)nw * Dh * 128);
+}
+
+// Masked slots leave a weight of 0, and V of slots that no node of the row may see is replaced by 0: those hold what was never written or has been
+// evicted.  (Values that are held are finite: whatever writes the cache clamps them.)
+template <int DH, int QT, int NW, bool STREAM>
+__global__ __launch_bounds__(NW * 64, 2) void span_attn_kernel(SpanArgs p) {
+    constexpr int KS = DH / 16, DT = DH / 32, TILE = KS + 2 * DT;    // KiB of a K and V tile
+    extern __shared__ float lds[];                          // queries [QT][KS] and a tile per wave [NW][TILE] of 1 KiB blocks; then maxima and sums, O of one query tile
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hl = lane >> 5, col = lane & 31;
+    const int T = p.T, H = p.H;
+    const int QTtot = (T + 31) >> 5, QG = (QTtot + QT - 1) / QT, per = QG * p.key_wgs;
+    const int seq = (int)blockIdx.x >> 3;
+    const int group = seq / per * 8 + ((int)blockIdx.x & 7), j = seq % per;
+    if (group >= p.groups) return;
+    const int b = group / H, h = group - b * H, qg = j % QG, key_wg = j / QG;
+    const int units = p.key_wgs * NW, unit = key_wg * NW + wave;
+    const SpanRow r = span_row<32>(p, b);
+    if (!r.ok) {                                            // uniform over the workgroup
+        if (tid == 0 && j == 0 && h == 0) atomicOr(p.flags, FLAG_CAPACITY);
+        return;
+    }
+    const int32_t *pt = p.table + (size_t)b * p.max_pages;
+    const int mine_n = unit < r.n ? (r.n - unit + units - 1) / units : 0;      // this wave's tiles: unit, unit + units, ...
+    // page ids of this wave's next 32 tiles, two per tile, one per lane; a page that no node sees may have none: the other one of its tile then
+    auto page_ids = [&](int first) {
+        int lp = 2 * r.tile(min(unit + (first + (lane >> 1)) * units, r.n - 1)) + (lane & 1);
+        if (!r.holds(lp)) lp ^= 1;
+        return pt[min(lp, p.max_pages - 1)];
+    };
+    int pgs = page_ids(0);
+    u32x4_t *qs = reinterpret_cast<u32x4_t *>(lds);
+    for (int i = wave; i < QT * KS; i += NW) {
+        const int qtile = min(qg * QT + i / KS, QTtot - 1);  // a second tile behind the last query: the first one again, which nobody stores
+        qs[i * 64 + lane] = span_query_piece<DH>(p, b, h, qtile, QTtot, col, 16 * (i % KS) + 8 * hl);
+    }
+    SpanQuery sq[QT];
+#pragma unroll
+    for (int q = 0; q < QT; ++q) sq[q] = span_query(p, r, (qg * QT + q) * 32 + col);
+    __syncthreads();
+
+    u32x4_t *mine = qs + (QT * KS + wave * TILE) * 64;      // this wave's tile: K blocks, then V blocks [page][dims / 32]
+    const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)mine;
+    auto dma = [&](const u32x4_t *src, int block) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
+                                         (__attribute__((address_space(3))) void *)(uintptr_t)(mine_at + (uint32_t)block * 1024u), 16, 0, STREAM ? 2 : 0);      // 2: nontemporal
+    };
+    const a16_t *kpages = reinterpret_cast<const a16_t *>(p.kpages), *vpages = reinterpret_cast<const a16_t *>(p.vpages);
+    int p0 = 0, p1 = 0;                                     // pages of the tile that is requested next
+    auto next_pages = [&](int it) {
+        if (it > 0 && (it & 31) == 0) { pgs = page_ids(it); asm volatile("" : "+v"(pgs)); }      // awaited in here, not behind the branch
+        p0 = checked_page(__builtin_amdgcn_readlane(pgs, 2 * (it & 31)), p.n_pages, p.flags);
+        p1 = checked_page(__builtin_amdgcn_readlane(pgs, 2 * (it & 31) + 1), p.n_pages, p.flags);
+    };
+    auto request_k = [&] {
+        const u32x4_t *kp = reinterpret_cast<const u32x4_t *>(kpages + kv_block_base(p.layer, p.n_pages, (col >> 4) ? p1 : p0, H, h, DH)) + hl * 16 + (col & 15);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) dma(kp + s * 32, s);
+    };
+    auto request_v = [&] {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const u32x4_t *vp = reinterpret_cast<const u32x4_t *>(vpages + kv_block_base(p.layer, p.n_pages, g ? p1 : p0, H, h, DH)) + col * 2 + hl;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) dma(vp + dt * 64, KS + g * DT + dt);
+        }
+    };
+    f32x16_t o[QT][DT];
+#pragma unroll
+    for (int q = 0; q < QT; ++q)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[q][dt][v] = 0.f;
+    float m_run[QT], l_run[QT];
+#pragma unroll
+    for (int q = 0; q < QT; ++q) { m_run[q] = -INFINITY; l_run[q] = 0.f; }
+    // these have arrived: nothing in the loop is to wait for an ordinary load, which would be a wait for the DMA as well
+    asm volatile("" : "+v"(pgs));
+#pragma unroll
+    for (int q = 0; q < QT; ++q) asm volatile("" : "+v"(sq[q].from), "+v"(sq[q].sinks), "+v"(sq[q].anc0), "+v"(sq[q].anc1));
+    if (mine_n > 0) { next_pages(0); request_k(); request_v(); }
+    for (int it = 0; it < mine_n; ++it) {
+        const bool more = it + 1 < mine_n;
+        const int slot0 = r.tile(unit + it * units) * 32;
+        const bool whole = span_whole<32>(p, r, slot0);     // uniform
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * DT) : "memory");             // K has landed: of what was asked for only V may be missing
+        f32x16_t sc[QT];
+#pragma unroll
+        for (int q = 0; q < QT; ++q)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sc[q][v] = 0.f;
+        int at = lane;
+        asm volatile("" : "+v"(at));                        // keeps the reads of the queries inside the loop
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const a16x8_t k = __builtin_bit_cast(a16x8_t, mine[s * 64 + lane]);
+#pragma unroll
+            for (int q = 0; q < QT; ++q) sc[q] = HYDRA_MFMA16(k, __builtin_bit_cast(a16x8_t, qs[at + (q * KS + s) * 64]), sc[q]);
+        }
+        if (more) {
+            next_pages(it + 1);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                    // K is read
+            request_k();
+        }
+        u32x4_t pb[QT][2];
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+            if (!whole) {
+                const uint32_t seen = span_seen(r, sq[q], slot0) >> (4 * hl);
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sc[q][v] = (seen >> (8 * (v >> 2) + (v & 3))) & 1u ? sc[q][v] : -INFINITY;
+            }
+            float cmax = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) cmax = fmaxf(cmax, sc[q][v]);
+            const HalfWaves cm = half_waves(cmax);
+            cmax = fmaxf(cm.lo, cm.hi);
+            if (__any(cmax > m_run[q])) {                                          // always on the first visible tile
+                const float m_new = fmaxf(m_run[q], cmax);
+                const float alpha = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run[q] - m_new) * p.c);
+                m_run[q] = m_new;
+                l_run[q] *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) o[q][dt][v] *= alpha;
+            }
+            const float ref = m_run[q] == -INFINITY ? 0.f : m_run[q];
+            float rs = 0.f;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const float w = __builtin_amdgcn_exp2f((sc[q][v] - ref) * p.c);   // 0 for masked slots, exactly 1 for the largest
+                sc[q][v] = w;
+                rs += w;
+            }
+            const HalfWaves rh = half_waves(rs);
+            l_run[q] += rh.lo + rh.hi;
+            // P^T operands: page g uses accumulator registers 8g .. 8g+7 in order
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) pb[q][g][w] = half_pack(sc[q][8 * g + 2 * w], sc[q][8 * g + 2 * w + 1]);
+        }
+        if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KS) : "memory");       // V has landed: only the next K may be missing
+        else      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (!whole) {
+            const uint32_t held = span_held(r, slot0);
+            if (held != 0xffffffffu) {
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    u32x4_t keep;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        // dword w holds keys i = 2w, 2w+1 of this half-wave: token = 8*(i/4) + 4*hl + i%4
+                        const int i0 = 2 * w, i1 = 2 * w + 1;
+                        const int s0 = 16 * g + 8 * (i0 >> 2) + 4 * hl + (i0 & 3), s1 = 16 * g + 8 * (i1 >> 2) + 4 * hl + (i1 & 3);
+                        keep[w] = ((held >> s0) & 1u ? 0x0000ffffu : 0u) | ((held >> s1) & 1u ? 0xffff0000u : 0u);
+                    }
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) mine[(KS + g * DT + dt) * 64 + lane] &= keep;      // each lane its own 16 bytes
+                }
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const a16x8_t v = __builtin_bit_cast(a16x8_t, mine[(KS + g * DT + dt) * 64 + lane]);
+#pragma unroll
+                for (int q = 0; q < QT; ++q) o[q][dt] = HYDRA_MFMA16(v, __builtin_bit_cast(a16x8_t, pb[q][g]), o[q][dt]);
+            }
+        if (more) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                    // V is read
+            request_v();
+        }
+    }
+
+    // ---- merge the waves through LDS, one query tile after the other: maxima and sums [QT][NW][2][32], then O[NW][DT * 4][64] of four dims each
+    __syncthreads();                                         // every wave is done with queries and tiles
+    float *ml = lds;
+    f32x4_t *ob = reinterpret_cast<f32x4_t *>(lds + QT * NW * 64);
+    if (hl == 0) {
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+            ml[(q * NW + wave) * 64 + col] = m_run[q];
+            ml[(q * NW + wave) * 64 + 32 + col] = l_run[q];
+        }
+    }
+    __syncthreads();
+    const int Tq = QTtot * 32;
+    float *rec = p.apart + (((size_t)b * H + h) * p.key_wgs + key_wg) * apart_record(Tq, DH);
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+        const int qtile = qg * QT + q, query = qtile * 32 + col;
+        if (qtile >= QTtot) break;                           // uniform over the workgroup
+        const float *mq = ml + q * NW * 64;
+        float m_tot = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) m_tot = fmaxf(m_tot, mq[w * 64 + col]);
+        const float m_safe = m_tot == -INFINITY ? 0.f : m_tot;
+        float l_tot = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) l_tot += __builtin_amdgcn_exp2f((mq[w * 64 + col] - m_safe) * p.c) * mq[w * 64 + 32 + col];
+        const float f = __builtin_amdgcn_exp2f((m_run[q] - m_safe) * p.c);
+#pragma unroll
+        for (int id = 0; id < DT * 4; ++id) {
+            const f32x16_t &od = o[q][id >> 2];
+            const int v = 4 * (id & 3);
+            ob[(wave * DT * 4 + id) * 64 + lane] = f32x4_t{od[v] * f, od[v + 1] * f, od[v + 2] * f, od[v + 3] * f};
+        }
+        __syncthreads();
+        // the (band, group of 4 registers = 4 consecutive dims) items are shared out over the waves
+        const float inv = 1.0f / l_tot;
+        for (int id = wave; id < DT * 4; id += NW) {
+            const int dt = id >> 2, g4 = id & 3;
+            f32x4_t acc = ob[id * 64 + lane];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) acc += ob[(w * DT * 4 + id) * 64 + lane];
+            const int dim = 32 * dt + 8 * g4 + 4 * hl;
+            if (p.key_wgs > 1) *reinterpret_cast<f32x4_t *>(rec + (size_t)query * DH + dim) = acc;
+            else if (query < T) span_store<DH>(p, b * T + query, h, dim, acc * inv);
+        }
+        if (wave == 0 && hl == 0) {
+            if (p.key_wgs > 1) {
+                rec[(size_t)Tq * DH + query] = m_tot;
+                rec[(size_t)Tq * DH + Tq + query] = l_tot;
+            } else if (p.stats) {
+                p.stats[((size_t)b * H + h) * Tq + query] = SpanStat{m_tot, inv};
+            }
+        }
+        if (q + 1 < QT) __syncthreads();                     // the next query tile's sums go where these were
+    }
+}
+
+// out = sum_u 2^((m_u - m) c) O_u / sum_u 2^((m_u - m) c) l_u over the records of a head: one thread per (query, 4 dims), all its loads in one round trip.
+template <bool F32>
+__global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs p, int Dh) {
+    const int h = blockIdx.y, b = blockIdx.z, T = p.T, H = p.H;
+    const int per_q = Dh >> 2;
+    const int n = blockIdx.x * (256 / per_q) + threadIdx.x / per_q;
+    const int dim = (threadIdx.x % per_q) * 4;
+    const int Tq = ((T + 31) >> 5) * 32;
+    const size_t recsz = apart_record(Tq, Dh);
+    const float *base = p.apart + (((size_t)b * H + h) * p.key_wgs) * recsz;
+    const bool live = n < T;
+    float mu[SPAN_MERGE_MAX], lu[SPAN_MERGE_MAX];
+    f32x4_t ou[SPAN_MERGE_MAX];
+#pragma unroll
+    for (int u = 0; u < SPAN_MERGE_MAX; ++u) {
+        mu[u] = -INFINITY; lu[u] = 0.f; ou[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (u < p.key_wgs && live) {
+            const float *r = base + u * recsz;
+            mu[u] = r[(size_t)Tq * Dh + n];
+            lu[u] = r[(size_t)Tq * Dh + Tq + n];
+            ou[u] = *reinterpret_cast<const f32x4_t *>(r + (size_t)n * Dh + dim);
+        }
+    }
+    if (!live || !span_row<32>(p, b).ok) return;
+    float mt = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < SPAN_MERGE_MAX; ++u) mt = fmaxf(mt, mu[u]);
+    const float m_safe = mt == -INFINITY ? 0.f : mt;
+    float den = 0.f;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < SPAN_MERGE_MAX; ++u) {
+        const float w = u < p.key_wgs ? __builtin_amdgcn_exp2f((mu[u] - m_safe) * p.c) : 0.f;
+        den += w * lu[u];
+        acc += ou[u] * w;
+    }
+    const float inv = 1.0f / den;
+    if (F32) *reinterpret_cast<f32x4_t *>(reinterpret_cast<float *>(p.out) + ((size_t)(b * T + n) * H + h) * Dh + dim) = acc * inv;
+    else if (Dh == 128) span_store<128>(p, b * T + n, h, dim, acc * inv);
+    else           span_store<64>(p, b * T + n, h, dim, acc * inv);
+    if (p.stats && dim == 0) p.stats[((size_t)b * H + h) * Tq + n] = SpanStat{mt, inv};
+}
+
+// The weights that every slot receives from nodes 0 .. n_scored - 1, behind the attention that has left each query's maximum and sum:
+//     score[s] += sum_n 2^((z_ns - M_n) c) / l_n
+// Queries are the rows of S = Q K^T here, so that a lane holds one slot and adds over its registers.  A wave takes 32-key tiles in turn; no two waves
+// hold the same slot, so no sum depends on an order of arrival.
+enum { SCORE_WAVES = 4 };
+template <int DH>
+__global__ __launch_bounds__(SCORE_WAVES * 64) void span_score_kernel(SpanArgs p) {
+    constexpr int KS = DH / 16, NW = SCORE_WAVES;
+    extern __shared__ float lds[];                          // queries [tiles][KS] of 1 KiB, then of each query its maximum, 1 / sum and what it sees
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hl = lane >> 5, col = lane & 31;
+    const int T = p.T, H = p.H, QTtot = (T + 31) >> 5, QS = (p.n_scored + 31) >> 5, Tq = QTtot * 32;
+    const int seq = (int)blockIdx.x >> 3;
+    const int group = seq / p.key_wgs * 8 + ((int)blockIdx.x & 7), key_wg = seq % p.key_wgs;
+    if (group >= p.groups) return;
+    const int b = group / H, h = group - b * H;
+    const SpanRow r = span_row<32>(p, b);
+    if (!r.ok) return;                                      // reported by the attention
+    const int units = p.key_wgs * NW, unit = key_wg * NW + wave;
+    const int32_t *pt = p.table + (size_t)b * p.max_pages;
+    u32x4_t *qs = reinterpret_cast<u32x4_t *>(lds);
+    SpanStat *st = reinterpret_cast<SpanStat *>(qs + QS * KS * 64);
+    SpanQuery *sq = reinterpret_cast<SpanQuery *>(st + QS * 32);
+    for (int i = wave; i < QS * KS; i += NW) qs[i * 64 + lane] = span_query_piece<DH>(p, b, h, i / KS, QTtot, col, 16 * (i % KS) + 8 * hl);
+    for (int i = tid; i < QS * 32; i += NW * 64) {
+        const bool counts = i < p.n_scored;
+        const SpanStat s = p.stats[((size_t)b * H + h) * Tq + (counts ? i : 0)];
+        st[i] = counts ? s : SpanStat{0.f, 0.f};
+        sq[i] = span_query(p, r, i);
+    }
+    __syncthreads();
+    float *row = p.score + ((size_t)b * H + h) * ((size_t)p.max_pages * 16);
+    const a16_t *kpages = reinterpret_cast<const a16_t *>(p.kpages);
+    for (int u = unit; u < r.n; u += units) {
+        const int t = r.tile(u), slot0 = t * 32;
+        const bool whole = span_whole<32>(p, r, slot0);
+        int lp = 2 * t + (col >> 4);
+        if (!r.holds(lp)) lp ^= 1;
+        const int raw = pt[min(lp, p.max_pages - 1)], page = (unsigned)raw < (unsigned)p.n_pages ? raw : 0;      // reported by the attention
+        const u32x4_t *kp = reinterpret_cast<const u32x4_t *>(kpages + kv_block_base(p.layer, p.n_pages, page, H, h, DH)) + hl * 16 + (col & 15);
+        u32x4_t k[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) k[s] = kp[s * 32];
+        float sum = 0.f;
+        for (int q = 0; q < QS; ++q) {
+            f32x16_t z;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) z[v] = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) z = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, qs[(q * KS + s) * 64 + lane]), __builtin_bit_cast(a16x8_t, k[s]), z);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int query = q * 32 + 8 * (v >> 2) + 4 * hl + (v & 3);
+                const SpanStat s = st[query];
+                bool seen = query < p.n_scored;
+                if (!whole) seen = seen && ((span_seen(r, sq[query], slot0) >> col) & 1u);
+                sum += seen ? __builtin_amdgcn_exp2f((z[v] - s.m) * p.c) * s.r : 0.f;
+            }
+        }
+        const HalfWaves two = half_waves(sum);
+        const int slot = slot0 + col;
+        if (hl == 0 && ((span_held(r, slot0) >> col) & 1u)) row[slot] = (slot < r.L ? row[slot] : 0.f) + (two.lo + two.hi);
+    }
+}
+
+// (query tiles of a wave, waves, request policy) that the rules below choose from
+#define SPAN_EACH_OF(X, DHv) X(DHv, 1, 8, true) X(DHv, 1, 8, false) X(DHv, 2, 8, true) X(DHv, 2, 8, false) X(DHv, 1, 4, true) X(DHv, 1, 4, false) X(DHv, 2, 4, true) X(DHv, 2, 4, false)
+#define SPAN_EACH(X) SPAN_EACH_OF(X, 128) SPAN_EACH_OF(X, 64)
+
+int span_max_dynamic_lds() {
+    hipError_t e = hipSuccess;
+#define ATTR(DHv, QTv, NWv, STv) \
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)span_attn_kernel<DHv, QTv, NWv, STv>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    SPAN_EACH(ATTR)
+#undef ATTR
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)span_score_kernel<128>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)span_score_kernel<64>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (e != hipSuccess) return hip_fail(e, "hipFuncSetAttribute(attention over part of a cache)");
+    return HYDRA_OK;
+}
+
+int launch_span_merge(hydra_ctx *c, hipStream_t s, const SpanArgs &a) {
+    const int Dh = c->m.head_dim;
+    const dim3 grid(ceil_div(a.T, 256 / (Dh / 4)), a.H, a.groups / a.H);
+    if (c->bf16) hipLaunchKernelGGL(span_merge_kernel<false>, grid, dim3(256), 0, s, a, Dh);
+    else         hipLaunchKernelGGL(span_merge_kernel<true>, grid, dim3(256), 0, s, a, Dh);
+    HYDRA_LAUNCH_CHECK("span_merge_kernel");
+    return HYDRA_OK;
+}
+
+// host bound on the slots of a row that a call's nodes see
+static int span_slots(const hydra_ctx *c, const hydra_kv_span *span) {
+    int64_t len = span->span_hint > 0 ? span->span_hint : span->kv.seq_len_hint > 0 ? span->kv.seq_len_hint : c->m.max_pos;
+    if (span->window > 0) len = std::min(len, (int64_t)span->window - 1 + std::min<int64_t>(span->n_sinks, len));
+    return (int)std::min<int64_t>(len + c->tree.T, INT_MAX / 2);
+}
+
+static SpanArgs span_args(hydra_ctx *c, int B, int layer, const void *q, bool plain, const int32_t *seq_len, const hydra_kv_span *span, float *apart, float *stats, void *out, int32_t *flags) {
+    SpanArgs a;
+    const int H = c->m.n_heads;
+    a.q = q; a.kpages = span->kv.k_pages; a.vpages = span->kv.v_pages; a.table = span->kv.page_table; a.seq_len = seq_len; a.first = span->first;
+    a.tree = tree_dev(c); a.apart = apart; a.out = out; a.flags = flags;
+    a.max_pages = span->kv.max_pages; a.n_pages = span->kv.n_pages; a.layer = layer; a.T = c->tree.T; a.H = H; a.groups = H * B; a.key_wgs = 1;
+    a.n_sinks = span->n_sinks; a.window = span->window; a.plain = plain ? 1 : 0; a.c = LOG2E / sqrtf((float)c->m.head_dim);
+    a.n_scored = span->score ? span->n_scored : 0;
+    a.stats = span->score ? reinterpret_cast<SpanStat *>(stats) : nullptr;
+    a.score = span->score ? span->score + (size_t)layer * span->score_rows * H * ((size_t)span->kv.max_pages * 16) : nullptr;
+    return a;
+}
+
+int launch_span_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const void *q, bool plain, const int32_t *seq_len, const hydra_kv_span *span,
+                          float *apart, int units_max, float *stats, void *out, int32_t *flags) {
+    SpanArgs a = span_args(c, B, layer, q, plain, seq_len, span, apart, stats, out, flags);
+    const int T = a.T, H = a.H, Dh = c->m.head_dim, QTtot = ceil_div(T, 32), slots = span_slots(c, span);
+    if (!c->bf16) return launch_span_f32(c, s, a, slots, std::min(units_max, (int)SPAN_MERGE_MAX));
+    const int tiles = ceil_div(slots, 32) + 2;
+    const int qt = QTtot > 1 && H * B * QTtot > 256 ? 2 : 1, qgroups = ceil_div(QTtot, qt), hb = H * B * qgroups;
+    const int nw = hb > 256 ? 4 : 8;
+    const bool stream = qgroups == 1;
+    a.key_wgs = std::max(1, std::min({ceil_div(tiles, nw * 2), std::max(1, 256 / hb), units_max, (int)SPAN_MERGE_MAX}));
+    const dim3 grid(ceil_div(H * B, 8) * 8 * qgroups * a.key_wgs), block(nw * 64);
+    const size_t lds = span_lds_bytes(Dh, qt, nw);
+#define LAUNCH(DHv, QTv, NWv, STv) \
+    if (Dh == DHv && qt == QTv && nw == NWv && stream == STv) hipLaunchKernelGGL((span_attn_kernel<DHv, QTv, NWv, STv>), grid, block, lds, s, a);
+    SPAN_EACH(LAUNCH)
+#undef LAUNCH
+    HYDRA_LAUNCH_CHECK("span_attn_kernel");
+    if (a.key_wgs > 1)
+        if (int rc = launch_span_merge(c, s, a)) return rc;
+    if (!a.score) return HYDRA_OK;
+    const int QS = ceil_div(a.n_scored, 32);
+    a.key_wgs = std::max(1, std::min(ceil_div(tiles, SCORE_WAVES), std::max(1, 1024 / (H * B))));
+    const dim3 sgrid(ceil_div(H * B, 8) * 8 * a.key_wgs), sblock(SCORE_WAVES * 64);
+    const size_t slds = (size_t)QS * ((Dh / 16) * 1024 + 32 * (sizeof(SpanStat) + sizeof(SpanQuery)));
+    if (Dh == 128) hipLaunchKernelGGL(span_score_kernel<128>, sgrid, sblock, slds, s, a);
+    else           hipLaunchKernelGGL(span_score_kernel<64>, sgrid, sblock, slds, s, a);
+    HYDRA_LAUNCH_CHECK("span_score_kernel");
+    return HYDRA_OK;
+}
+
+}  // namespace hydra

@@ -1,0 +1,285 @@
+// Tree attention over part of an fp32 cache, and the sums of the weights that every slot receives: span_attn.hip's operators for fp32 contexts.
+//
+// The products run on the fp32 matrix instruction (16x16x4, exact products and fp32 sums), one 16-token page at a time:
+//   S^T[key][query] = K[key][:] . Q[query][:]       lane: key lane % 16, dims 16 i + 4 g .. + 3 with g = lane / 16 (any order of the dims will do for a sum)
+//   O^T[dim][query] += V^T[dim][key] P^T[key][query]  step e takes keys 4 g + e, which is where the accumulator has them
+// so K and V come in 16-byte loads straight from the page and a query is a column of both.  A wave holds 32 queries.
+#include <algorithm>
+
+#include "span.h"
+
+namespace hydra {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+#define SPAN_MFMA4(a, b, c) __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0)
+
+// over the four lanes that hold a query's keys; the same in all of them
+template <class Op>
+__device__ __forceinline__ float over_keys(float v, Op op) {
+    const HalfWaves h = half_waves(v);
+    v = op(h.lo, h.hi);
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+enum { SPAN32_WAVES = 4, SPAN32_QT = 2 };
+template <int DH>
+__global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p) {
+    constexpr int KS = DH / 16, J = DH / 64, NW = SPAN32_WAVES, QT = SPAN32_QT;
+    __shared__ f32x4_t qs[QT * KS * 64];
+    __shared__ f32x4_t ob[NW * J * 4 * 64];
+    __shared__ float ml[QT * NW * 32];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = lane >> 4, col = lane & 15;
+    const int T = p.T, H = p.H, QG = (T + 16 * QT - 1) / (16 * QT), per = QG * p.key_wgs;
+    const int seq = (int)blockIdx.x >> 3;
+    const int group = seq / per * 8 + ((int)blockIdx.x & 7), j = seq % per;
+    if (group >= p.groups) return;
+    const int b = group / H, h = group - b * H, qg = j % QG, key_wg = j / QG;
+    const int units = p.key_wgs * NW, unit = key_wg * NW + wave;
+    const SpanRow r = span_row<16>(p, b);
+    if (!r.ok) {                                            // uniform over the workgroup
+        if (tid == 0 && j == 0 && h == 0) atomicOr(p.flags, FLAG_CAPACITY);
+        return;
+    }
+    const int32_t *pt = p.table + (size_t)b * p.max_pages;
+    const float *q = reinterpret_cast<const float *>(p.q), *kpages = reinterpret_cast<const float *>(p.kpages), *vpages = reinterpret_cast<const float *>(p.vpages);
+    SpanQuery sq[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        const int query = (qg * QT + t) * 16 + col;
+        sq[t] = span_query(p, r, query);
+        for (int i = wave; i < KS; i += NW) {
+            f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+            if (query < T) v = *reinterpret_cast<const f32x4_t *>(q + ((size_t)(b * T + query) * H + h) * DH + 16 * i + 4 * g);
+            qs[(t * KS + i) * 64 + lane] = v;
+        }
+    }
+    __syncthreads();
+    f32x4_t o[QT][J * 4];                                   // [4 jj + e]: dims 64 jj + 16 g + 4 rr + e, rr the place in the vector
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int i = 0; i < J * 4; ++i) o[t][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m_run[QT], l_run[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) { m_run[t] = -INFINITY; l_run[t] = 0.f; }
+    for (int u = unit; u < r.n; u += units) {
+        const int lp = r.tile(u), slot0 = lp * 16;
+        const bool whole = span_whole<16>(p, r, slot0);     // uniform
+        const size_t base = kv_block_base(p.layer, p.n_pages, checked_page(pt[lp], p.n_pages, p.flags), H, h, DH);
+        f32x4_t k[KS], v[4][J];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) k[i] = *reinterpret_cast<const f32x4_t *>(kpages + base + col * DH + 16 * i + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int jj = 0; jj < J; ++jj) v[e][jj] = *reinterpret_cast<const f32x4_t *>(vpages + base + (4 * g + e) * DH + 64 * jj + 4 * col);
+        bool odd = false;                                   // something that is not finite in a tile that not every query sees whole
+        if (!whole) {
+            const uint32_t held = span_held(r, slot0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int jj = 0; jj < J; ++jj) {
+                    if (!((held >> (4 * g + e)) & 1u)) v[e][jj] = f32x4_t{0.f, 0.f, 0.f, 0.f};      // never written, or evicted
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) odd |= !(fabsf(v[e][jj][d]) < INFINITY);
+                }
+            odd = __any(odd);
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const f32x4_t qv = qs[(t * KS + i) * 64 + lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s = SPAN_MFMA4(k[i][e], qv[e], s);
+            }
+            if (!whole) {
+                const uint32_t seen = span_seen(r, sq[t], slot0) >> (4 * g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] = (seen >> e) & 1u ? s[e] : -INFINITY;
+            }
+            const float top = over_keys(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), [](float a, float c) { return fmaxf(a, c); });
+            const float m_new = fmaxf(m_run[t], top), ref = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = __builtin_amdgcn_exp2f((m_run[t] - ref) * p.c);
+            if (__any(m_new != m_run[t])) {
+#pragma unroll
+                for (int i = 0; i < J * 4; ++i) o[t][i] *= alpha;
+            }
+            m_run[t] = m_new;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] = __builtin_amdgcn_exp2f((s[e] - ref) * p.c);       // 0 for masked slots
+            l_run[t] = l_run[t] * alpha + over_keys((s[0] + s[1]) + (s[2] + s[3]), [](float a, float c) { return a + c; });
+            if (!odd) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int jj = 0; jj < J; ++jj)
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) o[t][4 * jj + d] = SPAN_MFMA4(v[e][jj][d], s[e], o[t][4 * jj + d]);
+            } else {                                         // what a query does not see must not reach it as 0 * infinity: key by key
+                for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float w = __shfl(s[e], kk * 16 + col, 64);
+                        const float *vp = vpages + base + (4 * kk + e) * DH + 16 * g;
+                        if (w == 0.f) continue;
+#pragma unroll
+                        for (int jj = 0; jj < J; ++jj)
+#pragma unroll
+                            for (int rr = 0; rr < 4; ++rr)
+#pragma unroll
+                                for (int d = 0; d < 4; ++d) o[t][4 * jj + d][rr] = fmaf(w, vp[64 * jj + 4 * rr + d], o[t][4 * jj + d][rr]);
+                    }
+            }
+        }
+    }
+    // ---- merge the waves through LDS, one query tile after the other
+    if (g == 0) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            ml[(t * NW + wave) * 32 + col] = m_run[t];
+            ml[(t * NW + wave) * 32 + 16 + col] = l_run[t];
+        }
+    }
+    const int Tq = ((T + 31) >> 5) * 32;
+    float *rec = p.apart + (((size_t)b * H + h) * p.key_wgs + key_wg) * ((size_t)Tq * DH + 2 * (size_t)Tq);
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        const int query = (qg * QT + t) * 16 + col;
+        if ((qg * QT + t) * 16 >= T) break;                  // uniform over the workgroup
+        __syncthreads();                                     // maxima and sums are there; the tile before this one is stored
+        float m_tot = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) m_tot = fmaxf(m_tot, ml[(t * NW + w) * 32 + col]);
+        const float m_safe = m_tot == -INFINITY ? 0.f : m_tot;
+        float l_tot = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) l_tot += __builtin_amdgcn_exp2f((ml[(t * NW + w) * 32 + col] - m_safe) * p.c) * ml[(t * NW + w) * 32 + 16 + col];
+        const float f = __builtin_amdgcn_exp2f((m_run[t] - m_safe) * p.c);
+#pragma unroll
+        for (int jj = 0; jj < J; ++jj)
+#pragma unroll
+            for (int rr = 0; rr < 4; ++rr)
+                ob[(wave * J * 4 + jj * 4 + rr) * 64 + lane] = f32x4_t{o[t][4 * jj][rr], o[t][4 * jj + 1][rr], o[t][4 * jj + 2][rr], o[t][4 * jj + 3][rr]} * f;
+        __syncthreads();
+        const float inv = 1.0f / l_tot;
+        for (int id = wave; id < J * 4; id += NW) {
+            f32x4_t acc = ob[id * 64 + lane];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) acc += ob[(w * J * 4 + id) * 64 + lane];
+            const int dim = 64 * (id >> 2) + 16 * g + 4 * (id & 3);
+            if (p.key_wgs > 1) *reinterpret_cast<f32x4_t *>(rec + (size_t)query * DH + dim) = acc;
+            else if (query < T) *reinterpret_cast<f32x4_t *>(reinterpret_cast<float *>(p.out) + ((size_t)(b * T + query) * H + h) * DH + dim) = acc * inv;
+        }
+        if (wave == 0 && g == 0) {
+            if (p.key_wgs > 1) {
+                rec[(size_t)Tq * DH + query] = m_tot;
+                rec[(size_t)Tq * DH + Tq + query] = l_tot;
+            } else if (p.stats) {
+                p.stats[((size_t)b * H + h) * Tq + query] = SpanStat{m_tot, inv};
+            }
+        }
+    }
+}
+
+// The weights that every slot receives from nodes 0 .. n_scored - 1, behind the attention (span_attn.hip): queries are the rows of S = Q K^T here, a lane
+// holds one slot.
+template <int DH>
+__global__ __launch_bounds__(SPAN32_WAVES * 64) void span_score_f32_kernel(SpanArgs p) {
+    constexpr int KS = DH / 16, NW = SPAN32_WAVES;
+    extern __shared__ float lds[];                          // queries [tiles][KS] of 1 KiB, then of each query its maximum, 1 / sum and what it sees
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = lane >> 4, col = lane & 15;
+    const int T = p.T, H = p.H, QS = (p.n_scored + 15) >> 4, Tq = ((T + 31) >> 5) * 32;
+    const int seq = (int)blockIdx.x >> 3;
+    const int group = seq / p.key_wgs * 8 + ((int)blockIdx.x & 7), key_wg = seq % p.key_wgs;
+    if (group >= p.groups) return;
+    const int b = group / H, h = group - b * H;
+    const SpanRow r = span_row<16>(p, b);
+    if (!r.ok) return;                                      // reported by the attention
+    const int units = p.key_wgs * NW, unit = key_wg * NW + wave;
+    const int32_t *pt = p.table + (size_t)b * p.max_pages;
+    const float *q = reinterpret_cast<const float *>(p.q), *kpages = reinterpret_cast<const float *>(p.kpages);
+    f32x4_t *qs = reinterpret_cast<f32x4_t *>(lds);
+    SpanStat *st = reinterpret_cast<SpanStat *>(qs + QS * KS * 64);
+    SpanQuery *sq = reinterpret_cast<SpanQuery *>(st + QS * 16);
+    for (int i = wave; i < QS * KS; i += NW) {
+        const int query = i / KS * 16 + col;
+        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+        if (query < T) v = *reinterpret_cast<const f32x4_t *>(q + ((size_t)(b * T + query) * H + h) * DH + 16 * (i % KS) + 4 * g);
+        qs[i * 64 + lane] = v;
+    }
+    for (int i = tid; i < QS * 16; i += NW * 64) {
+        const bool counts = i < p.n_scored;
+        const SpanStat s = p.stats[((size_t)b * H + h) * Tq + (counts ? i : 0)];
+        st[i] = counts ? s : SpanStat{0.f, 0.f};
+        sq[i] = span_query(p, r, i);
+    }
+    __syncthreads();
+    float *row = p.score + ((size_t)b * H + h) * ((size_t)p.max_pages * 16);
+    for (int u = unit; u < r.n; u += units) {
+        const int lp = r.tile(u), slot0 = lp * 16;
+        const bool whole = span_whole<16>(p, r, slot0);
+        const int raw = pt[lp], page = (unsigned)raw < (unsigned)p.n_pages ? raw : 0;            // reported by the attention
+        const float *kp = kpages + kv_block_base(p.layer, p.n_pages, page, H, h, DH) + col * DH + 4 * g;
+        f32x4_t k[KS];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) k[i] = *reinterpret_cast<const f32x4_t *>(kp + 16 * i);
+        float sum = 0.f;
+        for (int t = 0; t < QS; ++t) {
+            f32x4_t z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const f32x4_t qv = qs[(t * KS + i) * 64 + lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z = SPAN_MFMA4(qv[e], k[i][e], z);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int query = t * 16 + 4 * g + e;
+                const SpanStat s = st[query];
+                bool seen = query < p.n_scored;
+                if (!whole) seen = seen && ((span_seen(r, sq[query], slot0) >> col) & 1u);
+                sum += seen ? __builtin_amdgcn_exp2f((z[e] - s.m) * p.c) * s.r : 0.f;
+            }
+        }
+        sum = over_keys(sum, [](float a, float c) { return a + c; });
+        const int slot = slot0 + col;
+        if (g == 0 && ((span_held(r, slot0) >> col) & 1u)) row[slot] = (slot < r.L ? row[slot] : 0.f) + sum;
+    }
+}
+
+int span_f32_max_dynamic_lds() {
+    hipError_t e = hipFuncSetAttribute((const void *)span_score_f32_kernel<128>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)span_score_f32_kernel<64>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (e != hipSuccess) return hip_fail(e, "hipFuncSetAttribute(attention over part of an fp32 cache)");
+    return HYDRA_OK;
+}
+
+int launch_span_f32(hydra_ctx *c, hipStream_t s, SpanArgs a, int slots, int units_max) {
+    const int T = a.T, Dh = c->m.head_dim, pages = ceil_div(slots, 16) + 2, hb = a.groups * ceil_div(T, 16 * SPAN32_QT);
+    a.key_wgs = std::max(1, std::min({ceil_div(pages, SPAN32_WAVES * 2), std::max(1, 512 / hb), units_max}));
+    const dim3 grid(ceil_div(a.groups, 8) * 8 * ceil_div(T, 16 * SPAN32_QT) * a.key_wgs), block(SPAN32_WAVES * 64);
+    if (Dh == 128) hipLaunchKernelGGL(span_f32_kernel<128>, grid, block, 0, s, a);
+    else           hipLaunchKernelGGL(span_f32_kernel<64>, grid, block, 0, s, a);
+    HYDRA_LAUNCH_CHECK("span_f32_kernel");
+    if (a.key_wgs > 1) {
+        int rc = launch_span_merge(c, s, a);
+        if (rc) return rc;
+    }
+    if (!a.score) return HYDRA_OK;
+    const int QS = ceil_div(a.n_scored, 16);
+    a.key_wgs = std::max(1, std::min(ceil_div(pages, SPAN32_WAVES), std::max(1, 1024 / a.groups)));
+    const dim3 sgrid(ceil_div(a.groups, 8) * 8 * a.key_wgs);
+    const size_t lds = (size_t)QS * ((Dh / 16) * 1024 + 16 * (sizeof(SpanStat) + sizeof(SpanQuery)));
+    if (Dh == 128) hipLaunchKernelGGL(span_score_f32_kernel<128>, sgrid, block, lds, s, a);
+    else           hipLaunchKernelGGL(span_score_f32_kernel<64>, sgrid, block, lds, s, a);
+    HYDRA_LAUNCH_CHECK("span_score_f32_kernel");
+    return HYDRA_OK;
+}
+
+}  // namespace hydra
