@@ -801,7 +801,6 @@ int hydra_token_logprobs(hydra_ctx *c, void *stream, int B, void *ws, const floa
         return fail(HYDRA_E_INVALID_ARG, "hydra_token_logprobs: NULL argument");
     if (!(tau > 0.f) || !(tau < INFINITY) || !(1.0f / tau < INFINITY)) return fail(HYDRA_E_INVALID_ARG, "hydra_token_logprobs: tau and 1 / tau must be positive and finite");
     if (k < 0 || k > HYDRA_MAX_TOPK || k > c->m.vocab) return fail(HYDRA_E_UNSUPPORTED, "hydra_token_logprobs: k outside [0, min(32, V)]");
-    if (!logprob_fits(c)) return fail(HYDRA_E_UNSUPPORTED, "hydra_token_logprobs: more than 2^21 tokens");
     const WsLayout w = ws_layout(c, B);
     return launch_token_logprobs(c, (hipStream_t)stream, B * c->tree.T, (float *)((char *)ws + w.logprob), logits, logprob || rank ? tokens : nullptr, tau, k, logprob, rank,
                                  entropy, top_ids, top_logprobs);

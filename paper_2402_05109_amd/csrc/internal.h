@@ -220,7 +220,6 @@ int launch_score_compact(hydra_ctx *c, hipStream_t s, int B, const int32_t *n_ac
 int check_pages(hydra_ctx *c, int B, const hydra_pages *p);             // arguments that the calls on a pool of pages share
 int launch_release_span(hydra_ctx *c, hipStream_t s, int B, const hydra_pages *pages, const int32_t *seq_len, const hydra_kv_span *span, int32_t *lo);
 // log probabilities (logprobs.hip)
-bool logprob_fits(const hydra_ctx *c);                                  // whether the vocabulary does
 size_t logprob_scratch_bytes(const hydra_ctx *c, int rows);
 int launch_token_logprobs(hydra_ctx *c, hipStream_t s, int rows, float *records, const float *logits, const int32_t *tokens, float tau, int k, float *logprob, int32_t *rank,
                           float *entropy, int32_t *top_ids, float *top_logprobs);
