@@ -30,12 +30,14 @@ __device__ __forceinline__ uint32_t score_key(float v) {
 }
 
 // One workgroup per (head, row, layer) finds what it keeps.  The key of the last token that is kept (`want` tokens have it or a larger one) is found from
-// its upper bits down, two at a time, by counting; tokens with that very key are taken from the lowest slot on.  A thread holds EV_PER neighbouring
-// candidates in registers, so up to EV_PIECE are read once; longer rows are read again for every count.
-enum { EV_THREADS = 1024, EV_PER = 8, EV_PIECE = EV_THREADS * EV_PER };
-__global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
-    __shared__ int cnt[3][3];
-    __shared__ int part[EV_THREADS / 64];
+// its upper bits down, two at a time, by counting; tokens with that very key are taken from the lowest slot on.  Counting is scalar work (a comparison per candidate and
+// bound, its lanes counted by the scalar unit), a turn a barrier; it ends as soon as a bound has just `want` candidates, for distinct scores after log2(n) / 2 turns or
+// a little more.  A thread holds PER neighbouring candidates in registers; rows that have more than THREADS * PER are read again for every count.
+template <int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
+    constexpr int WAVES = THREADS / 64, PIECE = THREADS * PER;
+    __shared__ int4 cnt[2][WAVES];
+    __shared__ int part[WAVES];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int h = blockIdx.x, b = blockIdx.y, layer = blockIdx.z, H = gridDim.x, B = gridDim.y;
     const bool speaks = tid == 0 && h == 0 && layer == 0;
@@ -48,15 +50,29 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
         if (speaks) a.evicted[b] = 0;
         return;
     }
+    float *score = a.score + (((size_t)layer * a.score_rows + b) * H + h) * ((size_t)a.max_pages * 16);
+    int32_t *kept = a.kept + (((size_t)layer * B + b) * H + h) * (size_t)a.keep;
+    const int c0 = F + a.n_sinks, n = L - a.n_recent - c0, want = a.keep - a.n_sinks - a.n_recent;      // candidates, and how many of them stay: want < n
+    const int pieces = (n + PIECE - 1) / PIECE;
+    uint32_t key[PER];
+    auto load = [&](int piece) {
+        const int id = piece * PIECE + tid * PER;
+        float x[PER];
+#pragma unroll
+        for (int e = 0; e < PER; ++e) x[e] = score[c0 + min(id + e, n - 1)];
+#pragma unroll
+        for (int e = 0; e < PER; ++e) key[e] = id + e < n ? score_key(x[e]) : 0u;
+    };
+    load(0);
     const int32_t *pt = a.table + (size_t)b * a.max_pages;
     int bad = 0;                                            // 1: an entry that names no page, 2: a page that is shared
-    for (int lp = (F >> 4) + tid; lp <= (L - 1) >> 4; lp += EV_THREADS) {
+    for (int lp = (F >> 4) + tid; lp <= (L - 1) >> 4; lp += THREADS) {
         const int page = pt[lp];
         if ((unsigned)page >= (unsigned)a.n_pages) bad |= 1;
         else if (a.ref && !a.dst_table && a.ref[page] > 1) bad |= 2;
     }
     if (a.dst_table)
-        for (int lp = ((L - a.keep) >> 4) + tid; lp <= (L - 1) >> 4; lp += EV_THREADS)
+        for (int lp = ((L - a.keep) >> 4) + tid; lp <= (L - 1) >> 4; lp += THREADS)
             if ((unsigned)a.dst_table[(size_t)b * a.max_pages + lp] >= (unsigned)a.n_pages) bad |= 1;
     const int none = __syncthreads_or(bad & 1), shared = __syncthreads_or(bad & 2);
     if (none || shared) {
@@ -65,45 +81,29 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
     }
     if (speaks) a.evicted[b] = 1;
 
-    float *score = a.score + (((size_t)layer * a.score_rows + b) * H + h) * ((size_t)a.max_pages * 16);
-    int32_t *kept = a.kept + (((size_t)layer * B + b) * H + h) * (size_t)a.keep;
-    const int c0 = F + a.n_sinks, n = L - a.n_recent - c0, want = a.keep - a.n_sinks - a.n_recent;      // candidates, and how many of them stay: want < n
-    for (int j = tid; j < a.n_sinks; j += EV_THREADS) kept[j] = F + j;
-    for (int j = tid; j < a.n_recent; j += EV_THREADS) kept[a.keep - a.n_recent + j] = L - a.n_recent + j;
-    const int pieces = (n + EV_PIECE - 1) / EV_PIECE;
-    uint32_t key[EV_PER];
-    auto load = [&](int piece) {
-        const int id = piece * EV_PIECE + tid * EV_PER;
-        float x[EV_PER];
-#pragma unroll
-        for (int e = 0; e < EV_PER; ++e) x[e] = score[c0 + min(id + e, n - 1)];
-#pragma unroll
-        for (int e = 0; e < EV_PER; ++e) key[e] = id + e < n ? score_key(x[e]) : 0u;
-    };
+    for (int j = tid; j < a.n_sinks; j += THREADS) kept[j] = F + j;
+    for (int j = tid; j < a.n_recent; j += THREADS) kept[a.keep - a.n_recent + j] = L - a.n_recent + j;
     if (want > 0) {
-        load(0);
-        if (tid < 9) cnt[tid / 3][tid % 3] = 0;
-        __syncthreads();
         int turn = 0;
         // how many candidates have a key of at least t[0], t[1], t[2]
         auto count = [&](const uint32_t (&t)[3], int (&c)[3]) {
-            int s[3] = {0, 0, 0};
+            c[0] = c[1] = c[2] = 0;
             for (int pc = 0; pc < pieces; ++pc) {
                 if (pieces > 1) load(pc);
 #pragma unroll
-                for (int e = 0; e < EV_PER; ++e)
+                for (int e = 0; e < PER; ++e)
 #pragma unroll
-                    for (int i = 0; i < 3; ++i) s[i] += __popcll(__ballot(key[e] >= t[i]));
+                    for (int i = 0; i < 3; ++i) c[i] += __popcll(__ballot(key[e] >= t[i]));
             }
-            if (lane == 0)
-#pragma unroll
-                for (int i = 0; i < 3; ++i) atomicAdd(&cnt[turn][i], s[i]);
+            if (lane == 0) cnt[turn][wave] = make_int4(c[0], c[1], c[2], 0);
             __syncthreads();
+            c[0] = c[1] = c[2] = 0;
 #pragma unroll
-            for (int i = 0; i < 3; ++i) c[i] = cnt[turn][i];
-            const int again = turn == 0 ? 2 : turn - 1;     // read by everybody before this barrier, next used behind the next one
-            if (tid < 3) cnt[again][tid] = 0;
-            turn = turn == 2 ? 0 : turn + 1;
+            for (int w = 0; w < WAVES; ++w) {
+                const int4 v = cnt[turn][w];
+                c[0] += v.x; c[1] += v.y; c[2] += v.z;
+            }
+            turn ^= 1;                                      // read by everybody before the next barrier, written again behind it
         };
         uint32_t last = 0u;
         for (int bit = 30; bit >= 0; bit -= 2) {
@@ -126,8 +126,8 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
             if (pieces > 1) load(pc);
             int mine = 0;
 #pragma unroll
-            for (int e = 0; e < EV_PER; ++e) mine += (key[e] > last ? 1 : 0) + (key[e] == last && key[e] != 0u ? 0x10000 : 0);
-            int x = mine;
+            for (int e = 0; e < PER; ++e) mine += (key[e] > last ? 1 : 0) + (key[e] == last && key[e] != 0u ? 0x10000 : 0);
+            int x = mine;                                   // two sums in one: a piece has at most 2^15 candidates
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
                 const int y = __shfl_up(x, d);
@@ -137,28 +137,28 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
             if (lane == 63) part[wave] = x;
             __syncthreads();
             int before = x - mine, total = 0;
-            for (int w = 0; w < EV_THREADS / 64; ++w) {
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
                 const int p = part[w];
                 if (w < wave) before += p;
                 total += p;
             }
-            int gt = seen_gt + (before & 0xffff), eq = seen_eq + (before >> 16);
+            int gt = seen_gt + (before & 0xffff), eq = seen_eq + (int)((unsigned)before >> 16);
 #pragma unroll
-            for (int e = 0; e < EV_PER; ++e) {
+            for (int e = 0; e < PER; ++e) {
                 const bool is_gt = key[e] > last, is_eq = key[e] == last && key[e] != 0u;
-                if (is_gt || (is_eq && eq < equal)) kept[a.n_sinks + gt + min(eq, equal)] = c0 + pc * EV_PIECE + tid * EV_PER + e;
+                if (is_gt || (is_eq && eq < equal)) kept[a.n_sinks + gt + min(eq, equal)] = c0 + pc * PIECE + tid * PER + e;
                 gt += is_gt ? 1 : 0;
                 eq += is_eq ? 1 : 0;
             }
             seen_gt += total & 0xffff;
-            seen_eq += total >> 16;
+            seen_eq += (int)((unsigned)total >> 16);
         }
     }
     __syncthreads();                                        // `kept` is written
     // the scores follow, from the last one down: a source lies at or below its target, so below every target of the pieces before
-    const int moved = a.keep - a.n_recent;
-    for (int top = moved; top > 0; top -= EV_THREADS) {
-        const int j = top - EV_THREADS + tid;
+    for (int top = a.keep - a.n_recent; top > 0; top -= THREADS) {
+        const int j = top - THREADS + tid;
         float x = 0.f;
         if (j >= 0) x = score[kept[j]];
         asm volatile("" : "+v"(x));
@@ -167,82 +167,163 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a) {
     }
 }
 
-// The contents follow: a wave takes a page of targets at a time, from the last one down, and a workgroup one of K and V of a (head, row, layer).  A source
-// lies at or below its target, so the pages of one turn have to be read before any of them is written, and those of later turns lie below.
-// Places of a page that no token moves to keep what they hold.
-enum { EV_WAVES = 8 };
-template <bool BF, int DH>
-__global__ __launch_bounds__(EV_WAVES * 64) void evict_move_kernel(EvictArgs a) {
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int h = blockIdx.x >> 1, is_v = blockIdx.x & 1, b = blockIdx.y, layer = blockIdx.z, H = gridDim.x >> 1, B = gridDim.y;
-    if (!a.evicted[b]) return;                              // uniform over the workgroup
-    const int L = a.seq_len[b], base = L - a.keep, moved = a.dst_table ? a.keep : a.keep - a.n_recent;
-    if (moved == 0) return;
-    const int32_t *kept = a.kept + (((size_t)layer * B + b) * H + h) * (size_t)a.keep;
-    const int32_t *pt = a.table + (size_t)b * a.max_pages, *dt = (a.dst_table ? a.dst_table : a.table) + (size_t)b * a.max_pages;
-    const int last = (base + moved - 1) >> 4, low = base >> 4;
-    typedef typename Act<BF>::type elem;
-    elem *pages = reinterpret_cast<elem *>(is_v ? a.v : a.k);
-    auto block = [&](int page) { return pages + kv_block_base(layer, a.n_pages, page, H, h, DH); };
-    constexpr int N = BF ? DH / 32 : DH / 16;               // 16-byte pieces of a page per lane
-    for (int p0 = last; p0 >= low; p0 -= EV_WAVES) {
-        const int lp = p0 - wave;
-        const bool live = lp >= low;                        // wave-uniform
-        const int to = dt[max(lp, low)];
-        u32x4_t x[N];
+// The contents follow.  A workgroup takes 64 dims of K or V of one (head, row, layer), a wave one page of targets at a time, from the last one down.  A source
+// lies at or below its target, so the pages of one turn have to be read before any of them is written, and those of later turns lie below: their loads
+// are under way while this turn's pages are stored.  Places of a page that no token moves to keep what they hold.
+enum { EV_WAVES = 8, EV_GROUP = 3, EV_PAGE_LDS = 2048 };
+struct EvictPlan { int to, slot, page; };                   // of a page of targets: its number, and for place lane % 16 the slot that moves there (-1: none) and its page
+struct EvictMove {
+    const int32_t *kept, *pt, *dt;
+    int base, moved, low;
+    __device__ __forceinline__ EvictPlan slots(int lp, int lane) const {
+        EvictPlan p;
+        const int j = lp * 16 + (lane & 15) - base;
+        p.to = dt[max(lp, low)];
+        p.slot = j >= 0 && j < moved ? kept[j] : -1;
+        p.page = 0;
+        return p;
+    }
+    __device__ __forceinline__ void look_up(EvictPlan &p) const { p.page = p.slot >= 0 ? pt[p.slot >> 4] : p.to; }
+};
+
+// fp32 rows, and 16-bit K (runs of 8 dims, [dim / 8][token]): they move as they lie, 16 bytes a lane.  block(page): the page's 64 dims
+template <bool BF, class Block>
+__device__ __forceinline__ void evict_move_rows(const EvictMove &m, int Dh, int last, int lane, int wave, Block block) {
+    constexpr int N = BF ? 2 : 4;
+    const int place = lane & 15, sub = lane >> 4;
+    auto at = [&](int page, int tok, int i) -> u32x4_t * {
+        if (BF) return reinterpret_cast<u32x4_t *>(block(page)) + (i * 4 + sub) * 16 + tok;                   // sub: the run of 8 dims
+        return reinterpret_cast<u32x4_t *>(block(page) + tok * Dh) + place;                                    // 16 lanes to the 64 dims of token 4 i + sub
+    };
+    auto load = [&](const EvictPlan &p, u32x4_t (&x)[N]) {
+        const int tok = p.slot >= 0 ? p.slot & 15 : place;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = BF ? *at(p.page, tok, i) : *at(__shfl(p.page, i * 4 + sub, 64), __shfl(tok, i * 4 + sub, 64), i);
+    };
+    EvictPlan now = m.slots(last - wave, lane), next = m.slots(last - wave - EV_WAVES, lane), after = m.slots(last - wave - 2 * EV_WAVES, lane);
+    m.look_up(now);
+    m.look_up(next);
+    u32x4_t x[N], y[N];
+    if (last - wave >= m.low) load(now, x);
+    for (int lp = last - wave; lp + wave >= m.low; lp -= EV_WAVES) {            // uniform over the workgroup
+        const bool live = lp >= m.low;                       // wave-uniform
+        const int to = now.to;
+        if (lp - EV_WAVES >= m.low) load(next, y);
+        now = next;
+        next = after;
+        m.look_up(next);
+        after = m.slots(lp - 3 * EV_WAVES, lane);
+#pragma unroll
+        for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));               // this turn's sources have arrived
+        __syncthreads();
         if (live) {
-            // lane t of the first 16 (and again of the others) knows where the token of place t comes from
-            const int place = lane & 15, j = lp * 16 + place - base;
-            const bool in = j >= 0 && j < moved;
-            const int src = in ? kept[j] : 0;
-            const int page = in ? pt[src >> 4] : to, tok = in ? src & 15 : place;
-            if (BF && !is_v) {                              // runs of 8 dims, [dim / 8][token]
-                const u32x4_t *from = reinterpret_cast<const u32x4_t *>(block(page)) + tok;
 #pragma unroll
-                for (int i = 0; i < N; ++i) x[i] = from[(i * 4 + (lane >> 4)) * 16];
-            } else if (BF) {                                // 2 bytes, [dim][place]
+            for (int i = 0; i < N; ++i) *at(to, BF ? place : i * 4 + sub, i) = x[i];
+        }
 #pragma unroll
-                for (int i = 0; i < N / 2; ++i) {
-                    uint32_t w[16];
+        for (int i = 0; i < N; ++i) x[i] = y[i];
+    }
+}
+
+// 16-bit V lies by dim: a lane holds the 16 tokens of one dim of a source page, which go to LDS as [dword][lane] (a dword: two tokens); since every lane moves the same tokens, one
+// is picked by an offset that the wave shares, without bank conflicts.  Picked from registers, by a register number that the wave shares, a page of targets took
+// twice as long as its loads and stores (7B, 8 layers, 2048 of 2560 tokens: 268 us).
+template <class Block>
+__device__ __forceinline__ void evict_move_v(const EvictMove &m, int last, int lane, int wave, char *lds, Block block) {
+    typedef uint16_t __attribute__((may_alias)) half_word;   // of what is written as dwords
+    const int place = lane & 15;
+    u32x4_t s[EV_GROUP][2];
+    uint32_t rest = 0;                                       // tokens that begin a source page which is not asked for yet
+    int pick = 0;                                            // of token `place`: the group of its page, and where it will lie in LDS
+    EvictPlan now;
+    auto fetch = [&] {
 #pragma unroll
-                    for (int t = 0; t < 16; ++t)
-                        w[v_perm(t)] = reinterpret_cast<const uint16_t *>(block(__builtin_amdgcn_readlane(page, t)))[(i * 64 + lane) * 16 + v_perm(__builtin_amdgcn_readlane(tok, t))];
+        for (int g = 0; g < EV_GROUP; ++g)
+            if (rest) {                                      // wave-uniform
+                const u32x4_t *from = reinterpret_cast<const u32x4_t *>(block(__builtin_amdgcn_readlane(now.page, __builtin_ctz(rest)))) + lane * 2;
+                s[g][0] = from[0];
+                s[g][1] = from[1];
+                rest &= rest - 1u;
+            }
+    };
+    auto begin = [&] {
+        const int tok = now.slot >= 0 ? now.slot & 15 : place, before = __shfl_up(now.page, 1, 64);
+        rest = (uint32_t)__ballot(lane < 16 && (lane == 0 || now.page != before));
+        const int nth = __popc(rest & ((2u << place) - 1u)) - 1, at = v_perm(tok);
+        pick = (nth / EV_GROUP) << 16 | (nth % EV_GROUP * EV_PAGE_LDS + (at >> 1) * 256 + (at & 1) * 2);
+        fetch();
+    };
+    now = m.slots(last - wave, lane);
+    EvictPlan next = m.slots(last - wave - EV_WAVES, lane), after = m.slots(last - wave - 2 * EV_WAVES, lane);
+    m.look_up(now);
+    m.look_up(next);
+    if (last - wave >= m.low) begin();
+    for (int lp = last - wave; lp + wave >= m.low; lp -= EV_WAVES) {            // uniform over the workgroup
+        const bool live = lp >= m.low;                       // wave-uniform
+        const int to = now.to;
+        uint32_t w[16];
+        if (live) {
 #pragma unroll
-                    for (int q = 0; q < 2; ++q)
+            for (int t = 0; t < 16; ++t) w[t] = 0u;
+            for (int group = 0;; ++group) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[2 * i + q][e] = w[8 * q + 2 * e] | (w[8 * q + 2 * e + 1] << 16);
+                for (int g = 0; g < EV_GROUP; ++g)
+#pragma unroll
+                    for (int d = 0; d < 8; ++d) *reinterpret_cast<uint32_t *>(lds + g * EV_PAGE_LDS + d * 256 + lane * 4) = s[g][d >> 2][d & 3];
+                const bool more = rest != 0;
+                if (more) fetch();
+#pragma unroll
+                for (int t = 0; t < 16; ++t) {
+                    const int o = __builtin_amdgcn_readlane(pick, t);
+                    if (o >> 16 == group) w[t] = *reinterpret_cast<const half_word *>(lds + (o & 0xffff) + lane * 4);
                 }
-            } else {                                        // a token's dims in a row
-                constexpr int PER = DH / 4;                 // lanes of a token
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int t = (i * 64 + lane) / PER;
-                    const int pg = __shfl(page, t, 64), tk = __shfl(tok, t, 64);
-                    x[i] = reinterpret_cast<const u32x4_t *>(block(pg))[tk * PER + lane % PER];
-                }
+                if (!more) break;
             }
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();                                    // every source of this turn has arrived
+        now = next;
+        next = after;
+        m.look_up(next);
+        after = m.slots(lp - 3 * EV_WAVES, lane);
+        if (lp - EV_WAVES >= m.low) begin();
+        u32x4_t x[2];
         if (live) {
-            u32x4_t *out = reinterpret_cast<u32x4_t *>(block(to));
-            if (BF && !is_v) {
+            uint32_t y[16];
 #pragma unroll
-                for (int i = 0; i < N; ++i) out[(i * 4 + (lane >> 4)) * 16 + (lane & 15)] = x[i];
-            } else if (BF) {
+            for (int t = 0; t < 16; ++t) y[v_perm(t)] = w[t];
 #pragma unroll
-                for (int i = 0; i < N; ++i) out[((i >> 1) * 64 + lane) * 2 + (i & 1)] = x[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) out[i * 64 + lane] = x[i];
-            }
+            for (int e = 0; e < 8; ++e) x[e >> 2][e & 3] = y[2 * e] | (y[2 * e + 1] << 16);
+        }
+        asm volatile("" : "+v"(x[0]), "+v"(x[1]));
+        __syncthreads();                                     // every wave's sources have gone through LDS
+        if (live) {
+            u32x4_t *out = reinterpret_cast<u32x4_t *>(block(to)) + lane * 2;
+            out[0] = x[0];
+            out[1] = x[1];
         }
     }
 }
 
-__global__ void evict_finish_kernel(const int32_t *seq_len, const int32_t *evicted, int32_t *first, int keep, int B) {
-    const int b = blockIdx.x * blockDim.x + threadIdx.x;
-    if (b < B && evicted[b]) first[b] = seq_len[b] - keep;
+template <bool BF>
+__global__ __launch_bounds__(EV_WAVES * 64) void evict_move_kernel(EvictArgs a, int Dh) {
+    __shared__ __attribute__((aligned(16))) char lds[BF ? EV_WAVES * EV_GROUP * EV_PAGE_LDS : 16];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int parts = Dh >> 6, h = (int)blockIdx.x / (2 * parts), part = (int)blockIdx.x % parts, is_v = (int)blockIdx.x / parts & 1;
+    const int b = blockIdx.y, layer = blockIdx.z, H = (int)gridDim.x / (2 * parts), B = gridDim.y;
+    if (!a.evicted[b]) return;                              // uniform over the workgroup
+    const int L = a.seq_len[b], base = L - a.keep, moved = a.dst_table ? a.keep : a.keep - a.n_recent;
+    if (tid == 0 && blockIdx.x == 0 && layer == 0) a.first[b] = base;         // nobody reads it here
+    if (moved == 0) return;
+    EvictMove m;
+    m.kept = a.kept + (((size_t)layer * B + b) * H + h) * (size_t)a.keep;
+    m.pt = a.table + (size_t)b * a.max_pages;
+    m.dt = (a.dst_table ? a.dst_table : a.table) + (size_t)b * a.max_pages;
+    m.base = base; m.moved = moved; m.low = base >> 4;
+    const int last = (base + moved - 1) >> 4;
+    typedef typename Act<BF>::type elem;
+    elem *pages = reinterpret_cast<elem *>(is_v ? a.v : a.k) + (BF ? part * 64 * 16 : part * 64);
+    auto block = [&](int page) { return pages + kv_block_base(layer, a.n_pages, page, H, h, Dh); };
+    if (BF && is_v) evict_move_v(m, last, lane, wave, lds + wave * EV_GROUP * EV_PAGE_LDS, block);
+    else            evict_move_rows<BF>(m, Dh, last, lane, wave, block);
 }
 
 // Scores of accepted nodes: one thread walks the path for one head, as kv_compact walks it.
@@ -304,19 +385,18 @@ int launch_kv_evict(hydra_ctx *c, hipStream_t s, int B, const int32_t *seq_len, 
     EvictArgs a = evict_args(c, seq_len, span);
     a.dst_table = dst_table; a.ref = ref; a.kept = kept; a.evicted = evicted; a.n_recent = n_recent; a.keep = keep; a.slack = slack;
     const int H = c->m.n_heads, NL = c->m.n_layers;
-    hipLaunchKernelGGL(evict_select_kernel, dim3(H, B, NL), dim3(EV_THREADS), 0, s, a);
+    const int64_t held = span->span_hint > 0 ? span->span_hint : span->kv.seq_len_hint > 0 ? span->kv.seq_len_hint : (int64_t)span->kv.max_pages * 16;
+    const int64_t n = held - span->n_sinks - n_recent;       // candidates, as far as the host knows
+    const dim3 sgrid(H, B, NL);
+    if (n <= 1024)       hipLaunchKernelGGL((evict_select_kernel<256, 4>), sgrid, dim3(256), 0, s, a);
+    else if (n <= 4096)  hipLaunchKernelGGL((evict_select_kernel<512, 8>), sgrid, dim3(512), 0, s, a);
+    else if (n <= 16384) hipLaunchKernelGGL((evict_select_kernel<1024, 16>), sgrid, dim3(1024), 0, s, a);
+    else                 hipLaunchKernelGGL((evict_select_kernel<1024, 32>), sgrid, dim3(1024), 0, s, a);
     HYDRA_LAUNCH_CHECK("evict_select_kernel");
-    const dim3 grid(2 * H, B, NL), block(EV_WAVES * 64);
-    if (c->bf16) {
-        if (c->m.head_dim == 128) hipLaunchKernelGGL((evict_move_kernel<true, 128>), grid, block, 0, s, a);
-        else                      hipLaunchKernelGGL((evict_move_kernel<true, 64>), grid, block, 0, s, a);
-    } else {
-        if (c->m.head_dim == 128) hipLaunchKernelGGL((evict_move_kernel<false, 128>), grid, block, 0, s, a);
-        else                      hipLaunchKernelGGL((evict_move_kernel<false, 64>), grid, block, 0, s, a);
-    }
+    const dim3 grid(2 * H * (c->m.head_dim / 64), B, NL), block(EV_WAVES * 64);
+    if (c->bf16) hipLaunchKernelGGL(evict_move_kernel<true>, grid, block, 0, s, a, c->m.head_dim);
+    else         hipLaunchKernelGGL(evict_move_kernel<false>, grid, block, 0, s, a, c->m.head_dim);
     HYDRA_LAUNCH_CHECK("evict_move_kernel");
-    hipLaunchKernelGGL(evict_finish_kernel, dim3(ceil_div(B, 256)), dim3(256), 0, s, seq_len, evicted, span->first, keep, B);
-    HYDRA_LAUNCH_CHECK("evict_finish_kernel");
     return HYDRA_OK;
 }
 
