@@ -29,14 +29,27 @@ __device__ __forceinline__ uint32_t score_key(float v) {
     return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
+// over the 64 lanes, the same in all of them
+__device__ __forceinline__ int wave_total(int v) {
+    const auto a = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = (int)(a[0] + a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = (int)(b[0] + b[1]);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, false);            // row_ror:8, 4, 2, 1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x124, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x122, 0xf, 0xf, false);
+    return v + __builtin_amdgcn_update_dpp(0, v, 0x121, 0xf, 0xf, false);
+}
+
 // One workgroup per (head, row, layer) finds what it keeps.  The key of the last token that is kept (`want` tokens have it or a larger one) is found from
-// its upper bits down, two at a time, by counting; tokens with that very key are taken from the lowest slot on.  Counting is scalar work (a comparison per candidate and
-// bound, its lanes counted by the scalar unit), a turn a barrier; it ends as soon as a bound has just `want` candidates, for distinct scores after log2(n) / 2 turns or
-// a little more.  A thread holds PER neighbouring candidates in registers; rows that have more than THREADS * PER are read again for every count.
+// its upper bits down, two at a time, by counting; tokens with that very key are taken from the lowest slot on.  Counting takes a comparison and an addition per
+// candidate and bound (with lanes counted by the scalar unit 13B took 39 us instead of 31), a turn a barrier; it ends as soon as a bound has just `want` candidates, for distinct scores once the bits tell its
+// neighbours apart.  A thread holds PER neighbouring candidates in registers; rows that have more than THREADS * PER are read again for every count.
 template <int THREADS, int PER>
 __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
     constexpr int WAVES = THREADS / 64, PIECE = THREADS * PER;
-    __shared__ int4 cnt[2][WAVES];
+    constexpr int BITS = 2, M = (1 << BITS) - 1;             // three bits at a time: fewer turns of more comparisons, 7B 24 us instead of 20
+    __shared__ int cnt[2][WAVES][4];
     __shared__ int part[WAVES];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int h = blockIdx.x, b = blockIdx.y, layer = blockIdx.z, H = gridDim.x, B = gridDim.y;
@@ -58,8 +71,18 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
     auto load = [&](int piece) {
         const int id = piece * PIECE + tid * PER;
         float x[PER];
+        typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
+        if (id + PER <= n) {
 #pragma unroll
-        for (int e = 0; e < PER; ++e) x[e] = score[c0 + min(id + e, n - 1)];
+            for (int e = 0; e < PER; e += 4) {
+                const f4u v = *reinterpret_cast<const f4u *>(score + c0 + id + e);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[e + q] = v[q];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < PER; ++e) x[e] = score[c0 + min(id + e, n - 1)];
+        }
 #pragma unroll
         for (int e = 0; e < PER; ++e) key[e] = id + e < n ? score_key(x[e]) : 0u;
     };
@@ -85,38 +108,49 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
     for (int j = tid; j < a.n_recent; j += THREADS) kept[a.keep - a.n_recent + j] = L - a.n_recent + j;
     if (want > 0) {
         int turn = 0;
-        // how many candidates have a key of at least t[0], t[1], t[2]
-        auto count = [&](const uint32_t (&t)[3], int (&c)[3]) {
-            c[0] = c[1] = c[2] = 0;
+        // how many candidates have a key of at least t[i]
+        auto count = [&](const uint32_t (&t)[M], int (&c)[M]) {
+#pragma unroll
+            for (int i = 0; i < M; ++i) c[i] = 0;
             for (int pc = 0; pc < pieces; ++pc) {
                 if (pieces > 1) load(pc);
 #pragma unroll
                 for (int e = 0; e < PER; ++e)
 #pragma unroll
-                    for (int i = 0; i < 3; ++i) c[i] += __popcll(__ballot(key[e] >= t[i]));
+                    for (int i = 0; i < M; ++i) c[i] += key[e] >= t[i] ? 1 : 0;
             }
-            if (lane == 0) cnt[turn][wave] = make_int4(c[0], c[1], c[2], 0);
-            __syncthreads();
-            c[0] = c[1] = c[2] = 0;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                const int4 v = cnt[turn][w];
-                c[0] += v.x; c[1] += v.y; c[2] += v.z;
-            }
+            for (int i = 0; i < M; ++i) c[i] = wave_total(c[i]);
+            if (lane == 0)
+#pragma unroll
+                for (int i = 0; i < M; ++i) cnt[turn][wave][i] = c[i];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < M; ++i) c[i] = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w)
+#pragma unroll
+                for (int i = 0; i < M; ++i) c[i] += cnt[turn][w][i];
             turn ^= 1;                                      // read by everybody before the next barrier, written again behind it
         };
-        uint32_t last = 0u;
-        for (int bit = 30; bit >= 0; bit -= 2) {
-            const uint32_t t[3] = {last | (1u << bit), last | (2u << bit), last | (3u << bit)};
-            int c[3];
+        uint32_t last = 0u, t[M];
+        int c[M];
+        for (int shift = 32 - BITS; shift > -BITS; shift -= BITS) {
+#pragma unroll
+            for (int i = 0; i < M; ++i) t[i] = last | ((uint32_t)(i + 1) << max(shift, 0));
             count(t, c);
-            last = c[2] >= want ? t[2] : c[1] >= want ? t[1] : c[0] >= want ? t[0] : last;
-            if (c[2] == want || c[1] == want || c[0] == want) break;        // nothing is left to tell apart: the largest such bound has just these
+            bool exact = false;                             // nothing is left to tell apart: the largest bound that enough candidates reach has just so many
+#pragma unroll
+            for (int i = 0; i < M; ++i) {
+                last = c[i] >= want ? t[i] : last;
+                exact |= c[i] == want;
+            }
+            if (exact) break;
         }
         int above = 0;
         if (last != 0xffffffffu) {
-            const uint32_t t[3] = {last + 1u, last + 1u, last + 1u};
-            int c[3];
+#pragma unroll
+            for (int i = 0; i < M; ++i) t[i] = last + 1u;
             count(t, c);
             above = c[0];
         }
@@ -170,7 +204,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
 // The contents follow.  A workgroup takes 64 dims of K or V of one (head, row, layer), a wave one page of targets at a time, from the last one down.  A source
 // lies at or below its target, so the pages of one turn have to be read before any of them is written, and those of later turns lie below: their loads
 // are under way while this turn's pages are stored.  Places of a page that no token moves to keep what they hold.
-enum { EV_WAVES = 8, EV_GROUP = 3, EV_PAGE_LDS = 2048 };
+enum { EV_WAVES = 16, EV_GROUP = 2, EV_PAGE_LDS = 2048 };
 struct EvictPlan { int to, slot, page; };                   // of a page of targets: its number, and for place lane % 16 the slot that moves there (-1: none) and its page
 struct EvictMove {
     const int32_t *kept, *pt, *dt;
@@ -304,7 +338,7 @@ __device__ __forceinline__ void evict_move_v(const EvictMove &m, int last, int l
 }
 
 template <bool BF>
-__global__ __launch_bounds__(EV_WAVES * 64) void evict_move_kernel(EvictArgs a, int Dh) {
+__global__ __launch_bounds__(EV_WAVES * 64, 8) void evict_move_kernel(EvictArgs a, int Dh) {
     __shared__ __attribute__((aligned(16))) char lds[BF ? EV_WAVES * EV_GROUP * EV_PAGE_LDS : 16];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int parts = Dh >> 6, h = (int)blockIdx.x / (2 * parts), part = (int)blockIdx.x % parts, is_v = (int)blockIdx.x / parts & 1;
