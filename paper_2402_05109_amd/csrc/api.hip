@@ -108,6 +108,11 @@ static int draft_rows_max(const hydra_ctx *c, int B) {
     return mx * B;
 }
 
+static size_t span_record_bytes(const hydra_ctx *c, int B) {
+    const size_t Tq = align_up(c->tree.T, 32);
+    return (size_t)B * c->m.n_heads * (Tq * c->m.head_dim + 2 * Tq) * 4;
+}
+
 WsLayout ws_layout(const hydra_ctx *c, int B) {
     WsLayout w;
     const size_t d = c->m.d, F = c->m.ffn, V = c->m.vocab, T = c->tree.T;
@@ -147,8 +152,16 @@ WsLayout ws_layout(const hydra_ctx *c, int B) {
     w.ss = off;    off += align_up((d / 32 + 1) * rows * 4, 256);
     w.topk = off;  off += align_up(topk_scratch_bytes(c, (int)std::max<size_t>(Md, 1)), 256);
     w.mega = off;  off += align_up(layers_mega_ws_bytes(c, B), 256);     // per-layer buffers of the persistent layer kernel (0 if the shape cannot take it)
-    w.stats = off; off += align_up((size_t)B * c->m.n_heads * Tq * 8, 256);
+    // of attention over part of a cache: 2 floats per query, or the root's scores for as many slots as positions can have (and the ends of two tiles), up to 64 k
+    w.z_slots = (int)align_up(std::min<size_t>((size_t)c->m.max_pos + 64, 65536), 64);
+    w.stats = off; off += align_up((size_t)B * c->m.n_heads * std::max(Tq * 8, (size_t)w.z_slots * 4), 256);
     w.logprob = off; off += align_up(logprob_scratch_bytes(c, (int)M), 256);
+    // fp32: records of workgroups that share a head's keys in attention over part of a cache, for 512 workgroups in all, where no other buffer has room for them
+    w.records = off;
+    if (!c->bf16) {
+        const size_t want = std::min<size_t>(16, 512 / std::min<size_t>(512, (size_t)B * c->m.n_heads * ceil_div((int)T, 32))) * span_record_bytes(c, B);
+        if (want > std::max(w.part - w.xb, w.qbuf - w.part)) off += align_up(want, 256);
+    }
     w.total = off;
     return w;
 }
@@ -206,12 +219,12 @@ static int check_span(hydra_ctx *c, int B, const hydra_kv_span *span) {
 }
 
 // Where attention over part of a cache leaves the records of workgroups that share a head's keys, and for how many there is room: in the fp32 family, whose
-// own attention has none, the larger of two buffers that are not in use then.
+// own attention has none, the largest of three buffers that are not in use then.
 static float *span_records(const hydra_ctx *c, int B, const WsLayout &w, char *W, int *units) {
     if (c->bf16) { *units = w.attn_units; return (float *)(W + w.apart); }
-    const size_t Tq = align_up(c->tree.T, 32), rec = (size_t)B * c->m.n_heads * (Tq * c->m.head_dim + 2 * Tq) * 4, xb = w.part - w.xb, part = w.qbuf - w.part;
-    *units = (int)std::min<size_t>(std::max(xb, part) / rec, 16);
-    return (float *)(W + (xb >= part ? w.xb : w.part));
+    const size_t xb = w.part - w.xb, part = w.qbuf - w.part, own = w.total - w.records, most = std::max({xb, part, own});
+    *units = (int)std::min<size_t>(most / span_record_bytes(c, B), 16);
+    return (float *)(W + (most == own ? w.records : most == xb ? w.xb : w.part));
 }
 
 static inline int32_t *flags_ptr(hydra_ctx *c) {
@@ -544,7 +557,7 @@ static int forward_layers(hydra_ctx *c, hipStream_t s, int B, void *ws, const Ro
             const LayerOff &o = c->layer[l];
             const float *next_gain = (const float *)(A + (l + 1 < c->m.n_layers ? c->layer[l + 1].attn_norm : c->off_final_norm));
             if ((rc = launch_gemm_qkv_rope(c, s, xa, A + o.wqkv, M, rs, l, seq_len, kv, qbuf, part, flags, !kv8 && !span))) return rc;
-            if (span) { if ((rc = launch_span_attention(c, s, B, l, qbuf, false, seq_len, span, apart, w.attn_units, stats, xb, flags))) return rc; }
+            if (span) { if ((rc = launch_span_attention(c, s, B, l, qbuf, false, seq_len, span, apart, w.attn_units, stats, w.z_slots, xb, flags))) return rc; }
             else if (kv8) { if ((rc = launch_kv8_attention(c, s, B, l, qbuf, false, seq_len, kv8, apart, w.attn_units, xb, flags))) return rc; }
             else     { if ((rc = launch_attention(c, s, B, l, qbuf, seq_len, kv, apart, w.attn_units, xb, nullptr, flags))) return rc; }
             if ((rc = launch_gemm_resid(c, s, xb, A + o.wo, M, d, d, x, (const float *)(A + o.ffn_norm), xa, ss, Mpad, part, &rs.nb))) return rc;
@@ -563,7 +576,7 @@ static int forward_layers(hydra_ctx *c, hipStream_t s, int B, void *ws, const Ro
         if (span) {
             int units;
             float *records = span_records(c, B, w, W, &units);
-            if ((rc = launch_span_attention(c, s, B, l, qbuf, true, seq_len, span, records, units, stats, xa, flags))) return rc;
+            if ((rc = launch_span_attention(c, s, B, l, qbuf, true, seq_len, span, records, units, stats, w.z_slots, xa, flags))) return rc;
         } else if ((rc = launch_attention(c, s, B, l, qbuf, seq_len, kv, apart, w.attn_units, xa, nullptr, flags))) return rc;
         if ((rc = launch_f32_add(c, s, (const float *)xa, weights(o.wo), x, M, d))) return rc;
         if ((rc = launch_f32_swiglu(c, s, x, weights(o.ffn_norm), weights(o.wgu), (float *)xb, M))) return rc;
@@ -690,7 +703,7 @@ int tree_attention_span(hydra_ctx *c, void *stream, int B, int layer, void *ws, 
     const WsLayout w = ws_layout(c, B);
     int units;
     float *records = span_records(c, B, w, (char *)ws, &units);
-    return launch_span_attention(c, (hipStream_t)stream, B, layer, q, true, seq_len, span, records, units, (float *)((char *)ws + w.stats), out, flags_ptr(c));
+    return launch_span_attention(c, (hipStream_t)stream, B, layer, q, true, seq_len, span, records, units, (float *)((char *)ws + w.stats), w.z_slots, out, flags_ptr(c));
 }
 
 // of calls that work on the scores of a span

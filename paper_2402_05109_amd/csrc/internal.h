@@ -98,7 +98,8 @@ inline int    ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // ---- workspace ------------------------------------------------------------
 struct WsLayout {
-    size_t flags, x, xa, xb, part, qbuf, apart, z, ss, topk, mega, stats, logprob, total;
+    size_t flags, x, xa, xb, part, qbuf, apart, z, ss, topk, mega, stats, logprob, records, total;
+    int z_slots;        // slots of a head whose scores `stats` has room for
     int attn_units;     // split-KV units per (row, head, query group)
 };
 WsLayout ws_layout(const hydra_ctx *c, int B);
@@ -209,9 +210,9 @@ int launch_kv8_seal(hydra_ctx *c, hipStream_t s, int B, const int32_t *seq_len, 
 int launch_kv8_read(hydra_ctx *c, hipStream_t s, int B, int layer, const hydra_kv8 *kv, int first_slot, int n_slots, float *plain);
 
 // part of a cache (span_attn.hip, span_f32.hip, span_evict.hip).  plain: queries and result are [B, T, H, Dh] in the cache's format; otherwise, in the 16-bit
-// family, qbuf and the next GEMM's input.  stats: 2 floats per query and head, where the span has scores
+// family, qbuf and the next GEMM's input.  stats, where the span has scores: 2 floats per query and head, or z_slots per head where the root alone is counted
 int launch_span_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const void *q, bool plain, const int32_t *seq_len, const hydra_kv_span *span,
-                          float *apart, int units_max, float *stats, void *out, int32_t *flags);
+                          float *apart, int units_max, float *stats, int z_slots, void *out, int32_t *flags);
 int span_max_dynamic_lds();
 int span_f32_max_dynamic_lds();
 int launch_kv_evict(hydra_ctx *c, hipStream_t s, int B, const int32_t *seq_len, const hydra_kv_span *span, int keep, int n_recent, int slack, const int32_t *dst_table,

@@ -25,6 +25,18 @@ __device__ __forceinline__ u32x4_t span_query_piece(const SpanArgs &p, int b, in
     if (query < p.T) v = *reinterpret_cast<const u32x4_t *>(reinterpret_cast<const a16_t *>(p.q) + ((size_t)(b * p.T + query) * p.H + h) * DH + d0);
     return v;
 }
+// the root's score for one slot
+template <int DH>
+__device__ __forceinline__ float span_root_dot(const SpanArgs &p, int b, int h, int slot, int page) {
+    const u32x4_t *kp = reinterpret_cast<const u32x4_t *>(reinterpret_cast<const a16_t *>(p.kpages) + kv_block_base(p.layer, p.n_pages, page, p.H, h, DH)) + (slot & 15);
+    float z = 0.f;
+    for (int d = 0; d < DH; d += 8) {
+        const a16x8_t k = __builtin_bit_cast(a16x8_t, kp[d * 2]), q = __builtin_bit_cast(a16x8_t, span_query_piece<DH>(p, b, h, 0, (p.T + 31) >> 5, 0, d));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z = fmaf((float)k[e], (float)q[e], z);
+    }
+    return z;
+}
 // four dims of a result
 template <int DH>
 __device__ __forceinline__ void span_store(const SpanArgs &p, int m, int h, int dim, f32x4_t v) {
@@ -112,6 +124,8 @@ __global__ __launch_bounds__(NW * 64, 2) void span_attn_kernel(SpanArgs p) {
 #pragma unroll
     for (int q = 0; q < QT; ++q) { m_run[q] = -INFINITY; l_run[q] = 0.f; }
     // these have arrived: nothing in the loop is to wait for an ordinary load, which would be a wait for the DMA as well
+    const bool root = p.z != nullptr && qg == 0;            // this workgroup holds the root, whose scores are wanted
+    float *z0 = p.z + ((size_t)b * H + h) * p.z_slots;
     asm volatile("" : "+v"(pgs));
 #pragma unroll
     for (int q = 0; q < QT; ++q) asm volatile("" : "+v"(sq[q].from), "+v"(sq[q].sinks), "+v"(sq[q].anc0), "+v"(sq[q].anc1));
@@ -140,12 +154,21 @@ __global__ __launch_bounds__(NW * 64, 2) void span_attn_kernel(SpanArgs p) {
             request_k();
         }
         u32x4_t pb[QT][2];
+        const bool kept = root && (unit + it * units) * 32 + 32 <= p.z_slots;
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
             if (!whole) {
                 const uint32_t seen = span_seen(r, sq[q], slot0) >> (4 * hl);
 #pragma unroll
                 for (int v = 0; v < 16; ++v) sc[q][v] = (seen >> (8 * (v >> 2) + (v & 3))) & 1u ? sc[q][v] : -INFINITY;
+            }
+            if (q == 0 && kept) {                            // wave-uniform; four stores, which the wait for V counts
+                if (col == 0) {
+                    float *to = z0 + (unit + it * units) * 32 + 4 * hl;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4_t *>(to + 8 * g) = f32x4_t{sc[0][4 * g], sc[0][4 * g + 1], sc[0][4 * g + 2], sc[0][4 * g + 3]};
+                }
+                asm volatile("" ::: "memory");
             }
             float cmax = -INFINITY;
 #pragma unroll
@@ -178,8 +201,10 @@ __global__ __launch_bounds__(NW * 64, 2) void span_attn_kernel(SpanArgs p) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) pb[q][g][w] = half_pack(sc[q][8 * g + 2 * w], sc[q][8 * g + 2 * w + 1]);
         }
-        if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KS) : "memory");       // V has landed: only the next K may be missing
-        else      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        // V has landed: only the next K, and the root's scores on their way out, may be missing
+        if (!more)     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        else if (kept) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KS + 4) : "memory");
+        else           asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KS) : "memory");
         if (!whole) {
             const uint32_t held = span_held(r, slot0);
             if (held != 0xffffffffu) {
@@ -265,19 +290,27 @@ __global__ __launch_bounds__(NW * 64, 2) void span_attn_kernel(SpanArgs p) {
                 p.stats[((size_t)b * H + h) * Tq + query] = SpanStat{m_tot, inv};
             }
         }
+        if (q == 0 && root && p.key_wgs == 1) {              // uniform: the root's weights, by the whole workgroup
+            if (tid == 0) *reinterpret_cast<SpanStat *>(ml) = SpanStat{m_tot, inv};          // the first maximum and sum are read
+            __syncthreads();                                 // (and every wave's scores are written)
+            const SpanStat st = *reinterpret_cast<const SpanStat *>(ml);
+            span_add_root<32>(p, r, b, h, st, tid, NW * 64, [&](int slot, int page) { return span_root_dot<DH>(p, b, h, slot, page); });
+        }
         if (q + 1 < QT) __syncthreads();                     // the next query tile's sums go where these were
     }
 }
 
 // out = sum_u 2^((m_u - m) c) O_u / sum_u 2^((m_u - m) c) l_u over the records of a head: one thread per (query, 4 dims), all its loads in one round trip.
-template <bool F32>
-__global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs p, int Dh) {
+// The workgroups behind the first `blocks` of a head add up the root's weights instead.
+template <bool F32, int DH>
+__global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs p, int blocks) {
     const int h = blockIdx.y, b = blockIdx.z, T = p.T, H = p.H;
-    const int per_q = Dh >> 2;
-    const int n = blockIdx.x * (256 / per_q) + threadIdx.x / per_q;
-    const int dim = (threadIdx.x % per_q) * 4;
+    constexpr int per_q = DH >> 2;
+    const bool slots = (int)blockIdx.x >= blocks;           // uniform
+    const int n = slots ? 0 : (int)blockIdx.x * (256 / per_q) + (int)threadIdx.x / per_q;
+    const int dim = (int)threadIdx.x % per_q * 4;
     const int Tq = ((T + 31) >> 5) * 32;
-    const size_t recsz = apart_record(Tq, Dh);
+    const size_t recsz = apart_record(Tq, DH);
     const float *base = p.apart + (((size_t)b * H + h) * p.key_wgs) * recsz;
     const bool live = n < T;
     float mu[SPAN_MERGE_MAX], lu[SPAN_MERGE_MAX];
@@ -287,12 +320,14 @@ __global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs p, int Dh) {
         mu[u] = -INFINITY; lu[u] = 0.f; ou[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         if (u < p.key_wgs && live) {
             const float *r = base + u * recsz;
-            mu[u] = r[(size_t)Tq * Dh + n];
-            lu[u] = r[(size_t)Tq * Dh + Tq + n];
-            ou[u] = *reinterpret_cast<const f32x4_t *>(r + (size_t)n * Dh + dim);
+            mu[u] = r[(size_t)Tq * DH + n];
+            lu[u] = r[(size_t)Tq * DH + Tq + n];
+            if (!slots) ou[u] = *reinterpret_cast<const f32x4_t *>(r + (size_t)n * DH + dim);
         }
     }
-    if (!live || !span_row<32>(p, b).ok) return;
+    constexpr int W = F32 ? 16 : 32;
+    const SpanRow row = span_row<W>(p, b);
+    if (!live || !row.ok) return;
     float mt = -INFINITY;
 #pragma unroll
     for (int u = 0; u < SPAN_MERGE_MAX; ++u) mt = fmaxf(mt, mu[u]);
@@ -306,24 +341,39 @@ __global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs p, int Dh) {
         acc += ou[u] * w;
     }
     const float inv = 1.0f / den;
-    if (F32) *reinterpret_cast<f32x4_t *>(reinterpret_cast<float *>(p.out) + ((size_t)(b * T + n) * H + h) * Dh + dim) = acc * inv;
-    else if (Dh == 128) span_store<128>(p, b * T + n, h, dim, acc * inv);
-    else           span_store<64>(p, b * T + n, h, dim, acc * inv);
+    if (slots) {
+        const int first = ((int)blockIdx.x - blocks) * 256 + (int)threadIdx.x, step = ((int)gridDim.x - blocks) * 256;
+        span_add_root<W>(p, row, b, h, SpanStat{mt, inv}, first, step, [&](int slot, int page) {
+            if constexpr (F32) {
+                const float *k = reinterpret_cast<const float *>(p.kpages) + kv_block_base(p.layer, p.n_pages, page, H, h, DH) + (slot & 15) * DH;
+                const float *q = reinterpret_cast<const float *>(p.q) + ((size_t)b * T * H + h) * DH;
+                float z = 0.f;
+                for (int d = 0; d < DH; ++d) z = fmaf(k[d], q[d], z);
+                return z;
+            } else {
+                return span_root_dot<DH>(p, b, h, slot, page);
+            }
+        });
+        return;
+    }
+    if (F32) *reinterpret_cast<f32x4_t *>(reinterpret_cast<float *>(p.out) + ((size_t)(b * T + n) * H + h) * DH + dim) = acc * inv;
+    else span_store<DH>(p, b * T + n, h, dim, acc * inv);
     if (p.stats && dim == 0) p.stats[((size_t)b * H + h) * Tq + n] = SpanStat{mt, inv};
 }
 
 // The weights that every slot receives from nodes 0 .. n_scored - 1, behind the attention that has left each query's maximum and sum:
-//     score[s] += sum_n 2^((z_ns - M_n) c) / l_n
-// Queries are the rows of S = Q K^T here, so that a lane holds one slot and adds over its registers.  A wave takes 32-key tiles in turn; no two waves
-// hold the same slot, so no sum depends on an order of arrival.
+//     score[s] += sum_n 2^((z_ns - M_n) c) / l_n = sum_n 2^((z_ns - M'_n) c),   M' = M + log2(l) / c
+// Queries are the rows of S = Q K^T here, so that a lane holds one slot and adds over its registers, and -M' is what the accumulators of the product begin with: a score costs a
+// multiplication, an exponential and an addition.  A wave takes 32-key tiles in turn, the next one's K under way; no two waves hold the same slot, so no sum depends
+// on an order of arrival.
 enum { SCORE_WAVES = 4 };
-template <int DH>
-__global__ __launch_bounds__(SCORE_WAVES * 64) void span_score_kernel(SpanArgs p) {
+template <int DH, int QS>
+__global__ __launch_bounds__(SCORE_WAVES * 64, 2) void span_score_kernel(SpanArgs p) {
     constexpr int KS = DH / 16, NW = SCORE_WAVES;
-    extern __shared__ float lds[];                          // queries [tiles][KS] of 1 KiB, then of each query its maximum, 1 / sum and what it sees
+    extern __shared__ float lds[];                          // queries [QS][KS] of 1 KiB, then what each sees
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hl = lane >> 5, col = lane & 31;
-    const int T = p.T, H = p.H, QTtot = (T + 31) >> 5, QS = (p.n_scored + 31) >> 5, Tq = QTtot * 32;
+    const int T = p.T, H = p.H, QTtot = (T + 31) >> 5, Tq = QTtot * 32;
     const int seq = (int)blockIdx.x >> 3;
     const int group = seq / p.key_wgs * 8 + ((int)blockIdx.x & 7), key_wg = seq % p.key_wgs;
     if (group >= p.groups) return;
@@ -332,48 +382,65 @@ __global__ __launch_bounds__(SCORE_WAVES * 64) void span_score_kernel(SpanArgs p
     if (!r.ok) return;                                      // reported by the attention
     const int units = p.key_wgs * NW, unit = key_wg * NW + wave;
     const int32_t *pt = p.table + (size_t)b * p.max_pages;
-    u32x4_t *qs = reinterpret_cast<u32x4_t *>(lds);
-    SpanStat *st = reinterpret_cast<SpanStat *>(qs + QS * KS * 64);
-    SpanQuery *sq = reinterpret_cast<SpanQuery *>(st + QS * 32);
-    for (int i = wave; i < QS * KS; i += NW) qs[i * 64 + lane] = span_query_piece<DH>(p, b, h, i / KS, QTtot, col, 16 * (i % KS) + 8 * hl);
-    for (int i = tid; i < QS * 32; i += NW * 64) {
-        const bool counts = i < p.n_scored;
-        const SpanStat s = p.stats[((size_t)b * H + h) * Tq + (counts ? i : 0)];
-        st[i] = counts ? s : SpanStat{0.f, 0.f};
-        sq[i] = span_query(p, r, i);
-    }
-    __syncthreads();
-    float *row = p.score + ((size_t)b * H + h) * ((size_t)p.max_pages * 16);
     const a16_t *kpages = reinterpret_cast<const a16_t *>(p.kpages);
-    for (int u = unit; u < r.n; u += units) {
-        const int t = r.tile(u), slot0 = t * 32;
-        const bool whole = span_whole<32>(p, r, slot0);
-        int lp = 2 * t + (col >> 4);
+    auto page_id = [&](int u) {                             // of the lane's slot in this wave's tile u; behind the last tile: the last one again
+        int lp = 2 * r.tile(min(u, r.n - 1)) + (col >> 4);
         if (!r.holds(lp)) lp ^= 1;
-        const int raw = pt[min(lp, p.max_pages - 1)], page = (unsigned)raw < (unsigned)p.n_pages ? raw : 0;      // reported by the attention
+        const int raw = pt[min(lp, p.max_pages - 1)];
+        return (unsigned)raw < (unsigned)p.n_pages ? raw : 0;                    // reported by the attention
+    };
+    auto load = [&](u32x4_t (&k)[KS], int page) {
         const u32x4_t *kp = reinterpret_cast<const u32x4_t *>(kpages + kv_block_base(p.layer, p.n_pages, page, H, h, DH)) + hl * 16 + (col & 15);
-        u32x4_t k[KS];
 #pragma unroll
         for (int s = 0; s < KS; ++s) k[s] = kp[s * 32];
+    };
+    u32x4_t k[KS];
+    load(k, page_id(unit));
+    int page = page_id(unit + units);
+    u32x4_t *qs = reinterpret_cast<u32x4_t *>(lds);
+    SpanQuery *sq = reinterpret_cast<SpanQuery *>(qs + QS * KS * 64);
+    for (int i = wave; i < QS * KS; i += NW) qs[i * 64 + lane] = span_query_piece<DH>(p, b, h, min(i / KS, QTtot - 1), QTtot, col, 16 * (i % KS) + 8 * hl);
+    for (int i = tid; i < QS * 32; i += NW * 64) sq[i] = span_query(p, r, i < p.n_scored ? i : p.T);
+    f32x16_t start[QS];                                     // -M' of the queries in the accumulators' rows; no weight at all: -infinity
+#pragma unroll
+    for (int q = 0; q < QS; ++q)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int query = q * 32 + 8 * (v >> 2) + 4 * hl + (v & 3);
+            const SpanStat s = p.stats[((size_t)b * H + h) * Tq + max(min(query, p.n_scored - 1), 0)];
+            start[q][v] = query < p.n_scored ? __builtin_amdgcn_logf(s.r) / p.c - s.m : -INFINITY;
+        }
+    __syncthreads();
+    float *row = p.score + ((size_t)b * H + h) * ((size_t)p.max_pages * 16);
+    for (int u = unit; u < r.n; u += units) {
+        const int slot0 = r.tile(u) * 32, slot = slot0 + col;
+        const bool whole = span_whole<32>(p, r, slot0), mine = hl == 0 && ((span_held(r, slot0) >> col) & 1u);
+        const float before = mine && slot < r.L ? row[slot] : 0.f;
+        u32x4_t next[KS];
+        load(next, page);
+        page = page_id(u + 2 * units);
         float sum = 0.f;
+        int at = lane;
+        asm volatile("" : "+v"(at));                         // keeps the reads of the queries inside the loop
+#pragma unroll
         for (int q = 0; q < QS; ++q) {
-            f32x16_t z;
+            f32x16_t z = start[q];
 #pragma unroll
-            for (int v = 0; v < 16; ++v) z[v] = 0.f;
+            for (int s = 0; s < KS; ++s) z = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, qs[at + (q * KS + s) * 64]), __builtin_bit_cast(a16x8_t, k[s]), z);
+            if (!whole) {
+                uint32_t sees = 0;                           // a bit for each of the lane's queries
+#pragma unroll 1
+                for (int v = 0; v < 16; ++v) sees |= ((span_seen(r, sq[q * 32 + 8 * (v >> 2) + 4 * hl + (v & 3)], slot0) >> col) & 1u) << v;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) z = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, qs[(q * KS + s) * 64 + lane]), __builtin_bit_cast(a16x8_t, k[s]), z);
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int query = q * 32 + 8 * (v >> 2) + 4 * hl + (v & 3);
-                const SpanStat s = st[query];
-                bool seen = query < p.n_scored;
-                if (!whole) seen = seen && ((span_seen(r, sq[query], slot0) >> col) & 1u);
-                sum += seen ? __builtin_amdgcn_exp2f((z[v] - s.m) * p.c) * s.r : 0.f;
+                for (int v = 0; v < 16; ++v) z[v] = (sees >> v) & 1u ? z[v] : -INFINITY;
             }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(z[v] * p.c);
         }
         const HalfWaves two = half_waves(sum);
-        const int slot = slot0 + col;
-        if (hl == 0 && ((span_held(r, slot0) >> col) & 1u)) row[slot] = (slot < r.L ? row[slot] : 0.f) + (two.lo + two.hi);
+        if (mine) row[slot] = before + (two.lo + two.hi);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) k[s] = next[s];
     }
 }
 
@@ -387,17 +454,16 @@ int span_max_dynamic_lds() {
     if (e == hipSuccess) e = hipFuncSetAttribute((const void *)span_attn_kernel<DHv, QTv, NWv, STv>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     SPAN_EACH(ATTR)
 #undef ATTR
-    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)span_score_kernel<128>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)span_score_kernel<64>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (e != hipSuccess) return hip_fail(e, "hipFuncSetAttribute(attention over part of a cache)");
     return HYDRA_OK;
 }
 
-int launch_span_merge(hydra_ctx *c, hipStream_t s, const SpanArgs &a) {
-    const int Dh = c->m.head_dim;
-    const dim3 grid(ceil_div(a.T, 256 / (Dh / 4)), a.H, a.groups / a.H);
-    if (c->bf16) hipLaunchKernelGGL(span_merge_kernel<false>, grid, dim3(256), 0, s, a, Dh);
-    else         hipLaunchKernelGGL(span_merge_kernel<true>, grid, dim3(256), 0, s, a, Dh);
+int launch_span_merge(hydra_ctx *c, hipStream_t s, const SpanArgs &a, int slots) {
+    const int Dh = c->m.head_dim, blocks = ceil_div(a.T, 256 / (Dh / 4)), adding = a.z ? std::min(ceil_div(slots, 512), std::max(1, 1024 / a.groups)) : 0;
+    const dim3 grid(blocks + adding, a.H, a.groups / a.H);
+#define LAUNCH(Fv, DHv) if (c->bf16 != Fv && Dh == DHv) hipLaunchKernelGGL((span_merge_kernel<Fv, DHv>), grid, dim3(256), 0, s, a, blocks);
+    LAUNCH(false, 128) LAUNCH(false, 64) LAUNCH(true, 128) LAUNCH(true, 64)
+#undef LAUNCH
     HYDRA_LAUNCH_CHECK("span_merge_kernel");
     return HYDRA_OK;
 }
@@ -409,7 +475,8 @@ static int span_slots(const hydra_ctx *c, const hydra_kv_span *span) {
     return (int)std::min<int64_t>(len + c->tree.T, INT_MAX / 2);
 }
 
-static SpanArgs span_args(hydra_ctx *c, int B, int layer, const void *q, bool plain, const int32_t *seq_len, const hydra_kv_span *span, float *apart, float *stats, void *out, int32_t *flags) {
+static SpanArgs span_args(hydra_ctx *c, int B, int layer, const void *q, bool plain, const int32_t *seq_len, const hydra_kv_span *span, float *apart, float *stats, int z_slots,
+                          void *out, int32_t *flags) {
     SpanArgs a;
     const int H = c->m.n_heads;
     a.q = q; a.kpages = span->kv.k_pages; a.vpages = span->kv.v_pages; a.table = span->kv.page_table; a.seq_len = seq_len; a.first = span->first;
@@ -417,21 +484,24 @@ static SpanArgs span_args(hydra_ctx *c, int B, int layer, const void *q, bool pl
     a.max_pages = span->kv.max_pages; a.n_pages = span->kv.n_pages; a.layer = layer; a.T = c->tree.T; a.H = H; a.groups = H * B; a.key_wgs = 1;
     a.n_sinks = span->n_sinks; a.window = span->window; a.plain = plain ? 1 : 0; a.c = LOG2E / sqrtf((float)c->m.head_dim);
     a.n_scored = span->score ? span->n_scored : 0;
-    a.stats = span->score ? reinterpret_cast<SpanStat *>(stats) : nullptr;
+    const bool root = a.n_scored == 1;
+    a.stats = span->score && !root ? reinterpret_cast<SpanStat *>(stats) : nullptr;
+    a.z = root ? stats : nullptr;
+    a.z_slots = z_slots;
     a.score = span->score ? span->score + (size_t)layer * span->score_rows * H * ((size_t)span->kv.max_pages * 16) : nullptr;
     return a;
 }
 
 int launch_span_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const void *q, bool plain, const int32_t *seq_len, const hydra_kv_span *span,
-                          float *apart, int units_max, float *stats, void *out, int32_t *flags) {
-    SpanArgs a = span_args(c, B, layer, q, plain, seq_len, span, apart, stats, out, flags);
+                          float *apart, int units_max, float *stats, int z_slots, void *out, int32_t *flags) {
+    SpanArgs a = span_args(c, B, layer, q, plain, seq_len, span, apart, stats, z_slots, out, flags);
     const int T = a.T, H = a.H, Dh = c->m.head_dim, QTtot = ceil_div(T, 32), slots = span_slots(c, span);
     if (!c->bf16) return launch_span_f32(c, s, a, slots, std::min(units_max, (int)SPAN_MERGE_MAX));
     const int tiles = ceil_div(slots, 32) + 2;
-    const int qt = QTtot > 1 && H * B * QTtot > 256 ? 2 : 1, qgroups = ceil_div(QTtot, qt), hb = H * B * qgroups;
+    const int qt = QTtot > 1 && (H * B * QTtot > 256 || tiles >= (QTtot == 2 ? 400 : 200)) ? 2 : 1, qgroups = ceil_div(QTtot, qt), hb = H * B * qgroups;
     const int nw = hb > 256 ? 4 : 8;
     const bool stream = qgroups == 1;
-    a.key_wgs = std::max(1, std::min({ceil_div(tiles, nw * 2), std::max(1, 256 / hb), units_max, (int)SPAN_MERGE_MAX}));
+    a.key_wgs = tiles <= 20 ? 1 : std::max(1, std::min({ceil_div(tiles, QTtot == 1 ? nw : nw * 2), std::max(1, 256 / hb), units_max, (int)SPAN_MERGE_MAX}));
     const dim3 grid(ceil_div(H * B, 8) * 8 * qgroups * a.key_wgs), block(nw * 64);
     const size_t lds = span_lds_bytes(Dh, qt, nw);
 #define LAUNCH(DHv, QTv, NWv, STv) \
@@ -440,14 +510,15 @@ int launch_span_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const v
 #undef LAUNCH
     HYDRA_LAUNCH_CHECK("span_attn_kernel");
     if (a.key_wgs > 1)
-        if (int rc = launch_span_merge(c, s, a)) return rc;
-    if (!a.score) return HYDRA_OK;
-    const int QS = ceil_div(a.n_scored, 32);
-    a.key_wgs = std::max(1, std::min(ceil_div(tiles, SCORE_WAVES), std::max(1, 1024 / (H * B))));
+        if (int rc = launch_span_merge(c, s, a, slots)) return rc;
+    if (!a.score || a.z) return HYDRA_OK;
+    const int QS = a.n_scored <= 32 ? 1 : a.n_scored <= 64 ? 2 : 4;
+    a.key_wgs = std::max(1, std::min(ceil_div(tiles, SCORE_WAVES), std::max(1, (QS == 1 ? 1024 : 512) / (H * B))));
     const dim3 sgrid(ceil_div(H * B, 8) * 8 * a.key_wgs), sblock(SCORE_WAVES * 64);
-    const size_t slds = (size_t)QS * ((Dh / 16) * 1024 + 32 * (sizeof(SpanStat) + sizeof(SpanQuery)));
-    if (Dh == 128) hipLaunchKernelGGL(span_score_kernel<128>, sgrid, sblock, slds, s, a);
-    else           hipLaunchKernelGGL(span_score_kernel<64>, sgrid, sblock, slds, s, a);
+    const size_t slds = (size_t)QS * ((Dh / 16) * 1024 + 32 * sizeof(SpanQuery));
+#define LAUNCH(DHv, QSv) if (Dh == DHv && QS == QSv) hipLaunchKernelGGL((span_score_kernel<DHv, QSv>), sgrid, sblock, slds, s, a);
+    LAUNCH(128, 1) LAUNCH(128, 2) LAUNCH(128, 4) LAUNCH(64, 1) LAUNCH(64, 2) LAUNCH(64, 4)
+#undef LAUNCH
     HYDRA_LAUNCH_CHECK("span_score_kernel");
     return HYDRA_OK;
 }

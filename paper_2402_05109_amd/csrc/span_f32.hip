@@ -90,18 +90,23 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
         }
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+            f32x4_t s = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < KS; ++i) {
+            for (int i = 0; i < KS; ++i) {                   // two chains: a product waits for the one before it in its own
                 const f32x4_t qv = qs[(t * KS + i) * 64 + lane];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s = SPAN_MFMA4(k[i][e], qv[e], s);
+                for (int e = 0; e < 4; e += 2) {
+                    s = SPAN_MFMA4(k[i][e], qv[e], s);
+                    s1 = SPAN_MFMA4(k[i][e + 1], qv[e + 1], s1);
+                }
             }
+            s += s1;
             if (!whole) {
                 const uint32_t seen = span_seen(r, sq[t], slot0) >> (4 * g);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[e] = (seen >> e) & 1u ? s[e] : -INFINITY;
             }
+            if (t == 0 && p.z && qg == 0 && col == 0 && u * 16 + 16 <= p.z_slots) *reinterpret_cast<f32x4_t *>(p.z + ((size_t)b * H + h) * p.z_slots + u * 16 + 4 * g) = s;
             const float top = over_keys(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), [](float a, float c) { return fmaxf(a, c); });
             const float m_new = fmaxf(m_run[t], top), ref = m_new == -INFINITY ? 0.f : m_new;
             const float alpha = __builtin_amdgcn_exp2f((m_run[t] - ref) * p.c);
@@ -183,15 +188,26 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
                 p.stats[((size_t)b * H + h) * Tq + query] = SpanStat{m_tot, inv};
             }
         }
+        if (t == 0 && p.z && qg == 0 && p.key_wgs == 1) {    // uniform: the root's weights, by the whole workgroup
+            if (tid == 0) *reinterpret_cast<SpanStat *>(ml) = SpanStat{m_tot, inv};
+            __syncthreads();                                 // (and every wave's scores are written; the first maximum and sum had been read)
+            const SpanStat st = *reinterpret_cast<const SpanStat *>(ml);
+            span_add_root<16>(p, r, b, h, st, tid, NW * 64, [&](int slot, int page) {
+                const float *kp = kpages + kv_block_base(p.layer, p.n_pages, page, H, h, DH) + (slot & 15) * DH, *q0 = q + ((size_t)b * T * H + h) * DH;
+                float z = 0.f;
+                for (int d = 0; d < DH; ++d) z = fmaf(kp[d], q0[d], z);
+                return z;
+            });
+        }
     }
 }
 
 // The weights that every slot receives from nodes 0 .. n_scored - 1, behind the attention (span_attn.hip): queries are the rows of S = Q K^T here, a lane
-// holds one slot.
+// holds one slot, and the accumulators begin with -M' of the queries.
 template <int DH>
 __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_score_f32_kernel(SpanArgs p) {
     constexpr int KS = DH / 16, NW = SPAN32_WAVES;
-    extern __shared__ float lds[];                          // queries [tiles][KS] of 1 KiB, then of each query its maximum, 1 / sum and what it sees
+    extern __shared__ float lds[];                          // queries [tiles][KS] of 1 KiB, then of each query what it sees and -M'
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, col = lane & 15;
     const int T = p.T, H = p.H, QS = (p.n_scored + 15) >> 4, Tq = ((T + 31) >> 5) * 32;
@@ -204,9 +220,21 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_score_f32_kernel(SpanA
     const int units = p.key_wgs * NW, unit = key_wg * NW + wave;
     const int32_t *pt = p.table + (size_t)b * p.max_pages;
     const float *q = reinterpret_cast<const float *>(p.q), *kpages = reinterpret_cast<const float *>(p.kpages);
+    auto page_id = [&](int u) {                             // behind the last tile: the last one again
+        const int raw = pt[r.tile(min(u, r.n - 1))];
+        return (unsigned)raw < (unsigned)p.n_pages ? raw : 0;                    // reported by the attention
+    };
+    auto load = [&](f32x4_t (&k)[KS], int page) {
+        const float *kp = kpages + kv_block_base(p.layer, p.n_pages, page, H, h, DH) + col * DH + 4 * g;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) k[i] = *reinterpret_cast<const f32x4_t *>(kp + 16 * i);
+    };
+    f32x4_t k[KS];
+    load(k, page_id(unit));
+    int page = page_id(unit + units);
     f32x4_t *qs = reinterpret_cast<f32x4_t *>(lds);
-    SpanStat *st = reinterpret_cast<SpanStat *>(qs + QS * KS * 64);
-    SpanQuery *sq = reinterpret_cast<SpanQuery *>(st + QS * 16);
+    SpanQuery *sq = reinterpret_cast<SpanQuery *>(qs + QS * KS * 64);
+    float *start = reinterpret_cast<float *>(sq + QS * 16);
     for (int i = wave; i < QS * KS; i += NW) {
         const int query = i / KS * 16 + col;
         f32x4_t v = {0.f, 0.f, 0.f, 0.f};
@@ -216,40 +244,42 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_score_f32_kernel(SpanA
     for (int i = tid; i < QS * 16; i += NW * 64) {
         const bool counts = i < p.n_scored;
         const SpanStat s = p.stats[((size_t)b * H + h) * Tq + (counts ? i : 0)];
-        st[i] = counts ? s : SpanStat{0.f, 0.f};
-        sq[i] = span_query(p, r, i);
+        start[i] = counts ? __builtin_amdgcn_logf(s.r) / p.c - s.m : -INFINITY;
+        sq[i] = span_query(p, r, counts ? i : T);
     }
     __syncthreads();
     float *row = p.score + ((size_t)b * H + h) * ((size_t)p.max_pages * 16);
     for (int u = unit; u < r.n; u += units) {
-        const int lp = r.tile(u), slot0 = lp * 16;
-        const bool whole = span_whole<16>(p, r, slot0);
-        const int raw = pt[lp], page = (unsigned)raw < (unsigned)p.n_pages ? raw : 0;            // reported by the attention
-        const float *kp = kpages + kv_block_base(p.layer, p.n_pages, page, H, h, DH) + col * DH + 4 * g;
-        f32x4_t k[KS];
-#pragma unroll
-        for (int i = 0; i < KS; ++i) k[i] = *reinterpret_cast<const f32x4_t *>(kp + 16 * i);
+        const int slot0 = r.tile(u) * 16, slot = slot0 + col;
+        const bool whole = span_whole<16>(p, r, slot0), mine = g == 0 && ((span_held(r, slot0) >> col) & 1u);
+        const float before = mine && slot < r.L ? row[slot] : 0.f;
+        f32x4_t next[KS];
+        load(next, page);
+        page = page_id(u + 2 * units);
         float sum = 0.f;
         for (int t = 0; t < QS; ++t) {
-            f32x4_t z = {0.f, 0.f, 0.f, 0.f};
+            f32x4_t z = *reinterpret_cast<const f32x4_t *>(start + t * 16 + 4 * g), z1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < KS; ++i) {
+            for (int i = 0; i < KS; ++i) {                   // two chains: a product waits for the one before it in its own
                 const f32x4_t qv = qs[(t * KS + i) * 64 + lane];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) z = SPAN_MFMA4(qv[e], k[i][e], z);
+                for (int e = 0; e < 4; e += 2) {
+                    z = SPAN_MFMA4(qv[e], k[i][e], z);
+                    z1 = SPAN_MFMA4(qv[e + 1], k[i][e + 1], z1);
+                }
+            }
+            z += z1;
+            if (!whole) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[e] = (span_seen(r, sq[t * 16 + 4 * g + e], slot0) >> col) & 1u ? z[e] : -INFINITY;
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int query = t * 16 + 4 * g + e;
-                const SpanStat s = st[query];
-                bool seen = query < p.n_scored;
-                if (!whole) seen = seen && ((span_seen(r, sq[query], slot0) >> col) & 1u);
-                sum += seen ? __builtin_amdgcn_exp2f((z[e] - s.m) * p.c) * s.r : 0.f;
-            }
+            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(z[e] * p.c);
         }
         sum = over_keys(sum, [](float a, float c) { return a + c; });
-        const int slot = slot0 + col;
-        if (g == 0 && ((span_held(r, slot0) >> col) & 1u)) row[slot] = (slot < r.L ? row[slot] : 0.f) + sum;
+        if (mine) row[slot] = before + sum;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) k[i] = next[i];
     }
 }
 
@@ -268,14 +298,14 @@ int launch_span_f32(hydra_ctx *c, hipStream_t s, SpanArgs a, int slots, int unit
     else           hipLaunchKernelGGL(span_f32_kernel<64>, grid, block, 0, s, a);
     HYDRA_LAUNCH_CHECK("span_f32_kernel");
     if (a.key_wgs > 1) {
-        int rc = launch_span_merge(c, s, a);
+        int rc = launch_span_merge(c, s, a, slots);
         if (rc) return rc;
     }
-    if (!a.score) return HYDRA_OK;
+    if (!a.score || a.z) return HYDRA_OK;
     const int QS = ceil_div(a.n_scored, 16);
     a.key_wgs = std::max(1, std::min(ceil_div(pages, SPAN32_WAVES), std::max(1, 1024 / a.groups)));
     const dim3 sgrid(ceil_div(a.groups, 8) * 8 * a.key_wgs);
-    const size_t lds = (size_t)QS * ((Dh / 16) * 1024 + 16 * (sizeof(SpanStat) + sizeof(SpanQuery)));
+    const size_t lds = (size_t)QS * ((Dh / 16) * 1024 + 16 * (sizeof(SpanQuery) + 4));
     if (Dh == 128) hipLaunchKernelGGL(span_score_f32_kernel<128>, sgrid, block, lds, s, a);
     else           hipLaunchKernelGGL(span_score_f32_kernel<64>, sgrid, block, lds, s, a);
     HYDRA_LAUNCH_CHECK("span_score_f32_kernel");

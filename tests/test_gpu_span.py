@@ -94,6 +94,27 @@ def test_results_do_not_depend_on_hints(f32):
 
 
 @pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("window, span_hint", [(0, 0), (0, 400), (300, 0)])
+def test_the_roots_weights_of_more_slots_than_the_workspace_has_room_for(f32, window, span_hint):
+    """max_pos sizes the workspace; this cache is longer."""
+    H, Dh, T = 2, 128, 40
+    parent, lens, firsts = tree_parent(T), [400, 30, 333], [0, 3, 150]
+    c = context(H, Dh, 3, parent, max_pos=48, f32=f32)
+    kv = torch.randn(1, 3, 400 + T, 2, H, Dh, generator=torch.Generator().manual_seed(1)).to(dtype_of(f32))
+    m = masks(parent, lens, firsts, 4, window, 400 + T)
+    kvd = cache(c, H, Dh, kv, m, f32)
+    q = torch.randn(3, T, H, Dh, generator=torch.Generator().manual_seed(2)).to(dtype_of(f32)).to(DEV)
+    out, score = torch.empty_like(q), torch.zeros(1, 3, H, kvd.max_pages * 16, device=DEV)
+    span = hb.KVSpan(kvd, first=torch.tensor(firsts, dtype=torch.int32, device=DEV), n_sinks=4, window=window, span_hint=span_hint, score=score, n_scored=1)
+    c.tree_attention_span(3, 0, c.ws, q, torch.tensor(lens, dtype=torch.int32, device=DEV), span, out)
+    ref, tol, add, add_tol = attention_reference(q, kv[0], m, f32, 1)
+    assert ((out.double() - ref).abs() <= tol).all() and c.read_flags() == 0
+    seen = m.any(dim=1)[:, None].to(DEV)
+    got = score[0, :, :, :400 + T].double()
+    assert ((got - torch.where(seen, add, 0.0)).abs() <= add_tol).all()
+
+
+@pytest.mark.parametrize("f32", [False, True])
 def test_sharp_rows(f32):
     """Scores of deviation 30: nearly all weight on one slot."""
     run(tree_parent(30), [500], [0], 4, 200, f32=f32, n_scored=30, scale=30.0, seed=11)
