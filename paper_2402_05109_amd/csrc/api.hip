@@ -203,16 +203,19 @@ static int check_kv8(hydra_ctx *c, const hydra_kv8 *kv) {
     return HYDRA_OK;
 }
 
-static int check_span(hydra_ctx *c, int B, const hydra_kv_span *span) {
+// attends: the call adds the context's tree behind seq_len; the others work on what a row holds
+static int check_span(hydra_ctx *c, int B, const hydra_kv_span *span, bool attends) {
     if (!span) return fail(HYDRA_E_INVALID_ARG, "span is NULL");
-    int rc = check_kv(c, &span->kv);
+    hydra_kv kv = span->kv;
+    if (!attends && kv.seq_len_hint > 0) kv.seq_len_hint = 0;
+    int rc = check_kv(c, &kv);
     if (rc) return rc;
     // slots are ints, and attention counts to the end of a tile of 32 behind the last one
     if (span->kv.max_pages > INT_MAX / HYDRA_PAGE - 1) return fail(HYDRA_E_CAPACITY, "span: a table of more than 2^31 - 32 slots");
     if (((uintptr_t)span->kv.k_pages | (uintptr_t)span->kv.v_pages) & 15) return fail(HYDRA_E_INVALID_ARG, "span: pages must be 16-byte aligned");
     if (span->n_sinks < 0 || span->window < 0 || span->span_hint < 0) return fail(HYDRA_E_INVALID_ARG, "span: n_sinks, window or span_hint is negative");
     if (span->score) {
-        if (span->n_scored < 0 || span->n_scored > c->tree.T) return fail(HYDRA_E_INVALID_ARG, "span: n_scored outside [0, T]");
+        if (attends && (span->n_scored < 0 || span->n_scored > c->tree.T)) return fail(HYDRA_E_INVALID_ARG, "span: n_scored outside [0, T]");
         if (span->score_rows < B) return fail(HYDRA_E_CAPACITY, "span: score has fewer rows than B");
     }
     return HYDRA_OK;
@@ -679,7 +682,7 @@ int tree_verify_forward_span(hydra_ctx *c, void *stream, int B, void *ws, const 
     int rc = check_common(c, B, ws);
     if (rc) return rc;
     if (!tree_tokens || !seq_len || !hidden || !argmax) return fail(HYDRA_E_INVALID_ARG, "tree_verify_forward_span: NULL argument");
-    if ((rc = check_span(c, B, span))) return rc;
+    if ((rc = check_span(c, B, span, true))) return rc;
     const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
     return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, &span->kv, nullptr, span, true, hidden, argmax, margin, logits);
 }
@@ -688,7 +691,7 @@ int hydra_prefill_chunk_span(hydra_ctx *c, void *stream, int B, void *ws, const 
     int rc = check_common(c, B, ws);
     if (rc) return rc;
     if (!tree_tokens || !seq_len) return fail(HYDRA_E_INVALID_ARG, "hydra_prefill_chunk_span: NULL argument");
-    if ((rc = check_span(c, B, span))) return rc;
+    if ((rc = check_span(c, B, span, true))) return rc;
     const RowSource src = {tree_tokens, nullptr, 0, nullptr, nullptr};
     return forward_layers(c, (hipStream_t)stream, B, ws, src, seq_len, &span->kv, nullptr, span, false, nullptr, nullptr, nullptr, nullptr);
 }
@@ -699,7 +702,7 @@ int tree_attention_span(hydra_ctx *c, void *stream, int B, int layer, void *ws, 
     if (!q || !seq_len || !out) return fail(HYDRA_E_INVALID_ARG, "tree_attention_span: NULL argument");
     if (((uintptr_t)q | (uintptr_t)out) & 15) return fail(HYDRA_E_INVALID_ARG, "tree_attention_span: q and out must be 16-byte aligned");
     if (layer < 0 || layer >= c->m.n_layers) return fail(HYDRA_E_INVALID_ARG, "layer out of range");
-    if ((rc = check_span(c, B, span))) return rc;
+    if ((rc = check_span(c, B, span, true))) return rc;
     const WsLayout w = ws_layout(c, B);
     int units;
     float *records = span_records(c, B, w, (char *)ws, &units);
@@ -711,7 +714,7 @@ static int check_scores(hydra_ctx *c, int B, const int32_t *seq_len, const hydra
     if (B < 1 || B > c->max_batch) return fail(HYDRA_E_CAPACITY, "B outside [1, max_batch]");
     if (!c->arena) return fail(HYDRA_E_STATE, "no weight arena bound");
     if (!seq_len) return fail(HYDRA_E_INVALID_ARG, "seq_len is NULL");
-    int rc = check_span(c, B, span);
+    int rc = check_span(c, B, span, false);
     if (rc) return rc;
     if (!span->score) return fail(HYDRA_E_INVALID_ARG, "span: score is NULL");
     return HYDRA_OK;

@@ -7,7 +7,7 @@ copy results into a log, and to provide the stream.
 """
 from __future__ import annotations
 
-from typing import Callable, Dict, List, Optional, Sequence
+from typing import Callable, Dict, List, Optional, Sequence, Tuple
 
 import torch
 
@@ -42,16 +42,30 @@ class Session:
     cache_format 'int8' or 'e4m3' (bf16 models): whole pages of the base cache are held in 8 bits; a row keeps the
     few 16-bit pages of its last, incomplete page and of a step's tree nodes.
     pool_pages: the cache has that many pages for all rows together (B * max_len tokens have not to fit), which rows take
-    as they grow, share after fork() and give back with free_rows(); defragment() moves the pages in use to the front."""
+    as they grow, share after fork() and give back with free_rows(); defragment() moves the pages in use to the front.
+
+    What a text of any length costs can be bounded (positions go on, up to max_len): window = W lets a token see the last W positions and the first
+    `sinks`; budget = (keep, recent, slack) keeps about `keep` tokens per layer and head, the first `sinks`, the last `recent` and those that drew most
+    attention so far; between steps and prompt chunks no row holds more than keep + slack.  A prompt's tokens all count, of a step its root, the one node that is sure to stay.
+    With pool_pages, pages that nobody sees any more go back to the pool."""
 
     def __init__(self, shape, parent: Sequence[int], B: int, max_len: int,
                  get_tensor: Callable[[str], torch.Tensor], device="cuda:0", prefill_chunk: int = 64,
                  page_perm_seed: Optional[int] = None, want_logits: bool = False, max_pos: Optional[int] = None,
-                 cache_format: Optional[str] = None, pool_pages: Optional[int] = None):
+                 cache_format: Optional[str] = None, pool_pages: Optional[int] = None, window: Optional[int] = None, sinks: int = 0,
+                 budget: Optional[Tuple[int, int, int]] = None):
         if cache_format not in (None, "int8", "e4m3"):
             raise ValueError(f"cache_format {cache_format!r}: None (16 bits), 'int8' or 'e4m3'")
         if cache_format and shape.dtype != "bf16":
             raise ValueError("an 8-bit cache needs a bf16 model")
+        if window is not None and budget is not None:
+            raise ValueError("a window or a budget, not both")
+        if (window is not None or budget is not None) and (cache_format or getattr(shape, "prefix", 0)):
+            raise ValueError("windows and budgets are for caches in the model's own format, and for models without a prefix layer")
+        if window is not None and window < 1 or sinks < 0 or (sinks and window is None and budget is None):
+            raise ValueError("a window of at least 1; sinks >= 0, with a window or a budget")
+        if budget is not None and (len(budget) != 3 or min(budget) < 0 or budget[0] < 1 or budget[1] + sinks > budget[0]):
+            raise ValueError("budget: (keep, recent, slack) with sinks + recent <= keep")
         self.shape, self.B, self.dev = shape, B, torch.device(device)
         self.parent = list(parent)
         self.dtype_code = hb.HYDRA_BF16 if shape.dtype == "bf16" else hb.HYDRA_F32
@@ -112,6 +126,22 @@ class Session:
         if self.pool:
             most = max(self.n_pages, self.kv.n_pages)
             self._pages_ws = torch.empty(hb.pages_workspace_bytes(B, most, self.max_pages), dtype=torch.uint8, device=self.dev)
+        # part of the cache
+        self.span: Optional[hb.KVSpan] = None
+        self.budget = budget
+        if window is not None or budget is not None:
+            first = score = None
+            if budget is not None:
+                first = torch.zeros(B, **i32)
+                score = torch.zeros(shape.NL, B, shape.H, 16 * self.max_pages, dtype=torch.float32, device=self.dev)
+                self._kept = torch.zeros(shape.NL, B, shape.H, budget[0], **i32)
+                self._evicted = torch.zeros(B, **i32)
+            self.span = hb.KVSpan(self.kv, first=first, n_sinks=sinks, window=window or 0, score=score)
+            self._growth = 0                          # tokens that a row can have taken since the last cut
+            self._shared = False                      # rows may share pages
+            if self.pool:
+                self._lo = torch.zeros(B, **i32)
+                self._dst = hb.Pages(torch.full((B, self.max_pages), -1, **i32), self.pages.ref)
         # state
         self.seq_len = torch.zeros(B, dtype=torch.int32, device=self.dev)
         self.h_last = torch.zeros(B, shape.d, dtype=torch.float32, device=self.dev)
@@ -249,6 +279,16 @@ class Session:
         if self.pool and self.host_len + T > min(self.max_pages * 16, self._max_pos):
             self.sync_len()                           # rows may have been freed since: only the real lengths are refused
         self.kv.seq_len_hint = self.host_len
+        if self.span is not None:
+            self.span.span_hint = self._most_held()
+
+    def _most_held(self) -> int:
+        """Host bound on the tokens that a row holds (0: nothing is known to hold any)."""
+        held = max(self.host_len, self._other_len)
+        if self.budget is not None:
+            keep, _, slack = self.budget
+            held = min(held, keep + slack // 2 + self._growth)
+        return held
 
     def reset(self) -> None:
         self.seq_len.zero_(); self.h_last.zero_(); self.root.zero_()
@@ -256,6 +296,11 @@ class Session:
             self.pseq_len.zero_()
         if self.kv8 is not None:
             self.kv8.n_sealed.zero_()
+        if self.budget is not None:
+            self.span.first.zero_()
+            self.span.score.zero_()
+        if self.span is not None:
+            self._growth, self._shared = 0, False
         if self.pool:
             for p in self._pools():
                 p.page_table.fill_(-1)
@@ -264,18 +309,50 @@ class Session:
         self._len_event = None
 
     # ---- the cache behind a forward pass, in 16 or 8 bits ------------------------
-    def _forward(self, c: hb.Hydra, o: _Outputs, B: int) -> None:
+    def _forward(self, c: hb.Hydra, o: _Outputs, B: int, prompt: bool = False) -> None:
         args = (o.tree_tokens, self.seq_len[:B])
         out = (o.hidden, o.argmax, o.margin, o.logits)
-        if self.kv8 is None:
+        if self.span is not None:
+            self.span.n_scored = c.T if prompt else 1
+            c.tree_verify_forward_span(B, self.ws, *args, self.span, *out)
+        elif self.kv8 is None:
             c.tree_verify_forward(B, self.ws, *args, self.kv, *out)
         else:
             c.tree_verify_forward_kv8(B, self.ws, *args, self.kv8, *out)
 
     def _keep_accepted(self, c: hb.Hydra, o: _Outputs, B: int, h_last: torch.Tensor, root: torch.Tensor) -> None:
+        # (no hydra_score_compact: a prompt's path is the identity, and the root of a step sees no other node, so their sums all begin at 0)
         c.kv_compact(B, o.n_acc, o.path, o.next_root, o.last_node, o.hidden, self.kv, self.seq_len, h_last, root, o.kv_index)
         if self.kv8 is not None:
             c.hydra_kv8_seal(B, self.seq_len, self.kv8)
+
+    def _trim(self, grown: int) -> None:
+        """Rows over the budget are cut, once in a while: a cut leaves at most keep + slack / 2 tokens, and the next one comes before a row can have taken
+        the other half."""
+        if self.budget is None:
+            return
+        keep, recent, slack = self.budget
+        self._growth += grown
+        if self._growth <= slack - slack // 2 or max(self.host_len, self._other_len) <= keep + slack // 2:
+            return
+        m, B, spare = self.main, self.B, slack // 2
+        self.span.span_hint = 0 if self.host_len == 0 else max(self.host_len, self._other_len)
+        if not (self.pool and self._shared):
+            m.hydra_kv_evict(B, self.seq_len, self.span, keep, recent, spare, self._kept, self._evicted)
+        else:
+            # rows that may share pages go to pages of their own; what they held goes back, where no other row has it
+            cut = (self.seq_len - self.span.first) > keep + spare
+            zero = torch.zeros_like(self.seq_len)
+            m.hydra_pages_reserve(B, self._pages_ws, self._dst, torch.where(cut, self.seq_len - keep, zero), torch.where(cut, self.seq_len, zero), 0, self._lists[4])
+            if not bool(self._lists[4][:B].all()):
+                m.hydra_pages_release(B, self._dst, None, zero)
+                raise RuntimeError(f"the pool of {self.n_pages} pages is exhausted: no room for the kept tokens of rows that share pages")
+            m.hydra_kv_evict(B, self.seq_len, self.span, keep, recent, spare, self._kept, self._evicted, dst_table=self._dst.page_table)
+            done = self._evicted[:, None] > 0
+            m.hydra_pages_release(B, self.pages, None, torch.where(self._evicted > 0, zero, zero + 16 * self.max_pages))
+            self.page_table.copy_(torch.where(done, self._dst.page_table, self.page_table))
+            self._dst.page_table.fill_(-1)
+        self._growth = 0
 
     def _incomplete(self) -> torch.Tensor:
         """The 16-bit page of every row that its next token goes to (any page where the row holds none there)."""
@@ -317,6 +394,9 @@ class Session:
 
     def _drop_scratch(self) -> None:
         """The pages behind every row's text go back."""
+        if self.span is not None:
+            self.main.hydra_pages_release_span(self.B, self.pages, self.seq_len, self.span)
+            return
         for p in self._pools():
             self.main.hydra_pages_release(self.B, p, None, self.seq_len)
 
@@ -326,7 +406,11 @@ class Session:
         if not self.pool:
             return
         ok = self._lists[4]
-        self.main.hydra_pages_reserve(B, self._pages_ws, self.pages, None, self.seq_len, T, ok)
+        lo = None
+        if self.span is not None:                     # what no node sees any more goes back first, and stays without pages
+            lo = self._lo
+            self.main.hydra_pages_release_span(B, self.pages, self.seq_len, self.span, lo)
+        self.main.hydra_pages_reserve(B, self._pages_ws, self.pages, lo, self.seq_len, T, ok)
         if self.kv8 is not None:
             # never short of pages: no tree has more than _T_max nodes (_check_nodes), so a row holds at most a ring of them, and fork() takes
             # one more for each row
@@ -334,8 +418,10 @@ class Session:
             self.main.hydra_pages_release(B, self.tail_pages, lo, self.seq_len)
             self.main.hydra_pages_reserve(B, self._pages_ws, self.tail_pages, lo, self.seq_len, T)
         # a row may hold pages that the nodes of a larger tree than this one needed
-        most = max(c.T for c in self._ctx.values())
-        if self.B * ((max(self.host_len, self._other_len) + most + 15) // 16) > self.n_pages and not bool(ok[:B].all()):
+        most, held = max(c.T for c in self._ctx.values()), max(self.host_len, self._other_len)
+        if self.span is not None:                     # with the ends of two stretches, sinks and the rest, inside pages
+            held = min(held, self.span.window + self.span.n_sinks if self.span.window else self._most_held()) + 45
+        if self.B * ((held + most + 15) // 16) > self.n_pages and not bool(ok[:B].all()):
             raise RuntimeError(f"the pool of {self.n_pages} pages is exhausted")
 
     def fork(self, src_rows: Sequence[int]) -> None:
@@ -366,6 +452,12 @@ class Session:
             m.hydra_pages_fork(B, self._pages_ws, self.tail_pages, rows, self.seq_len, src, dst, self._lists[3])
             m.hydra_kv_copy_pages(self.kv, B, src, dst)
         state = [self.seq_len, self.h_last, self.root] + ([self.pseq_len] if self.prefix else []) + ([self.kv8.n_sealed] if self.kv8 is not None else [])
+        if self.span is not None:
+            self._shared = True
+        if self.budget is not None:
+            state.append(self.span.first)
+            for layer in self.span.score:
+                layer.copy_(layer[rows.long()])
         for t in state:
             t.copy_(t[rows.long()])
         self._len_event = None                        # a length on its way to the host may be another row's
@@ -379,6 +471,9 @@ class Session:
         at = torch.tensor(list(rows), dtype=torch.int64, device=self.dev)
         for t in [self.seq_len, self.h_last, self.root] + ([self.pseq_len] if self.prefix else []) + ([self.kv8.n_sealed] if self.kv8 is not None else []):
             t.index_fill_(0, at, 0)
+        if self.budget is not None:
+            self.span.first.index_fill_(0, at, 0)
+            self.span.score.index_fill_(1, at, 0)
         self._drop_scratch()
 
     def defragment(self) -> int:
@@ -395,11 +490,12 @@ class Session:
             self.prefix_ctx(m.depth + 1).hydra_kv_copy_pages(self.pkv, self.n_pages, src, dst, counts)
         return int(counts[1])
 
-    def prefill(self, prompts: torch.Tensor) -> None:
+    def prefill(self, prompts: torch.Tensor, behind_chunk: Optional[Callable[[str, int, int], None]] = None) -> None:
         """prompts: int32 [B, L] (same length for every row; with pool_pages also fewer rows, the first ones).  Causal chunks through
         tree_verify_forward with a chain tree; the state update is kv_compact with the
         identity path.  Where an exception breaks the prompt off, seq_len, h_last and root are those behind the last chunk that was
-        computed whole (behind the text in front of the prompt if there is none)."""
+        computed whole (behind the text in front of the prompt if there is none).  behind_chunk(context, position, tokens) is called when a chunk's outputs are
+        there, which then all chunks have."""
         B, L = prompts.shape
         assert B == self.B or (self.pool and B < self.B)
         prompts = prompts.to(self.dev, torch.int32)
@@ -412,7 +508,8 @@ class Session:
             lens = self.seq_len.tolist()
             self._other_len = max(lens[B:], default=0)
             self._set_len(max(lens[:B]))
-        layers_only = not self.prefix and self.host_len + L <= room
+        # Nor where a broken prompt could not go back, because what was cut or given back meanwhile is gone.
+        layers_only = not self.prefix and self.host_len + L <= room and behind_chunk is None and self.budget is None and not (self.span is not None and self.pool)
         last = {n: i for i, n in enumerate(chunks)}
         pos = 0
         behind = None                                 # the text behind the last chunk that h_last and root know of, if others followed
@@ -433,13 +530,17 @@ class Session:
                     if behind is None:
                         behind = self._mark()
                     h_last, root = torch.empty_like(h_last), torch.empty_like(root)       # of outputs that are not written
-                    if self.kv8 is None:
+                    if self.span is not None:
+                        c.hydra_prefill_chunk_span(B, self.ws, o.tree_tokens, self.seq_len, self.span)
+                    elif self.kv8 is None:
                         c.hydra_prefill_chunk(B, self.ws, o.tree_tokens, self.seq_len, self.kv)
                     else:
                         c.hydra_prefill_chunk_kv8(B, self.ws, o.tree_tokens, self.seq_len, self.kv8)
                 else:
-                    self._forward(c, o, B)
+                    self._forward(c, o, B, prompt=True)
                     o.next_root.copy_(o.argmax[:, n - 1])
+                    if behind_chunk is not None:
+                        behind_chunk(name, pos, n)
                 self._keep_accepted(c, o, B, h_last, root)
                 if h_last is self.h_last:
                     behind = None
@@ -448,6 +549,7 @@ class Session:
                 pos += n
                 self.host_len += n
                 self._growth_since_copy += n          # a length on its way to the host was read before these
+                self._trim(n)
         except BaseException:
             if behind is not None:                    # broken off: back to the text that h_last and root belong to
                 self._back_to(behind)
@@ -481,12 +583,41 @@ class Session:
             raise ValueError("typical acceptance needs the logits: create the Session with want_logits=True")
         c.accept_typical(self.B, self.ws, o.tree_tokens, o.logits, tau, eps, alpha, u, o.n_acc, o.path, o.next_root, o.last_node)
 
+    def logprobs(self, tokens: Optional[torch.Tensor] = None, tau: float = 1.0, k: int = 0, name: str = "main", rows: Optional[int] = None) -> Dict[str, torch.Tensor]:
+        """Of the last forward pass through context `name` (a session that keeps logits): the entropy of every node's distribution, the log probability and rank of
+        tokens [B, T] int32 (-1: none), and the k most likely tokens with theirs.  The first `rows` rows."""
+        c, o = self.ctx(name), self._out[name]
+        if o.logits is None:
+            raise ValueError("log probabilities need the logits: create the Session with want_logits=True")
+        B = rows or self.B
+        f32, i32 = dict(dtype=torch.float32, device=self.dev), dict(dtype=torch.int32, device=self.dev)
+        out = {"entropy": torch.empty(B, c.T, **f32)}
+        if tokens is not None:
+            if tuple(tokens.shape) != (B, c.T):
+                raise ValueError(f"tokens: expected [{B}, {c.T}], got {tuple(tokens.shape)}")
+            tokens = tokens.to(self.dev, torch.int32).contiguous()
+            out |= {"logprob": torch.empty(B, c.T, **f32), "rank": torch.empty(B, c.T, **i32)}
+        if k:
+            out |= {"top_ids": torch.empty(B, c.T, k, **i32), "top_logprobs": torch.empty(B, c.T, k, **f32)}
+        c.hydra_token_logprobs(B, self.ws, o.logits, tokens, tau, k, **out)
+        return out
+
+    def prompt_logprobs(self, prompts: torch.Tensor, tau: float = 1.0, k: int = 0) -> Dict[str, torch.Tensor]:
+        """prefill(prompts), and what the model thought of them: entry i of a row is about the token behind prompt token i (behind the last one: none given).
+        The mean of -logprob over a text says what a window, a budget or an 8-bit cache costs."""
+        B, L = prompts.shape
+        parts: List[Dict[str, torch.Tensor]] = []
+        given = torch.cat([prompts[:, 1:].to(self.dev, torch.int32), torch.full((B, 1), -1, dtype=torch.int32, device=self.dev)], dim=1)
+        self.prefill(prompts, lambda name, pos, n: parts.append(self.logprobs(given[:, pos:pos + n], tau, k, name, B)))
+        return {key: torch.cat([p[key] for p in parts], dim=1) for key in parts[0]}
+
     def compact(self, name: str = "main") -> None:
         c, o = self.ctx(name), self._out[name]
         self._hint(c.T)
         self._keep_accepted(c, o, self.B, self.h_last, self.root)
         self.host_len += c.depth + 1          # upper bound; the device holds the exact value
         self._growth_since_copy += c.depth + 1
+        self._trim(c.depth + 1)
 
     def step(self, name: str = "main", hook=None, typical=None) -> None:
         """One speculative step of every row.  `hook(outputs)` may edit tree_tokens between
