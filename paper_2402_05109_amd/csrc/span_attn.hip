@@ -370,7 +370,7 @@ enum { SCORE_WAVES = 4 };
 template <int DH, int QS>
 __global__ __launch_bounds__(SCORE_WAVES * 64, 2) void span_score_kernel(SpanArgs p) {
     constexpr int KS = DH / 16, NW = SCORE_WAVES;
-    extern __shared__ float lds[];                          // queries [QS][KS] of 1 KiB, then what each sees
+    extern __shared__ float lds[];                          // queries [QS][KS] of 1 KiB, then -M' of each, a bit row per query for each wave, and what each query sees
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hl = lane >> 5, col = lane & 31;
     const int T = p.T, H = p.H, QTtot = (T + 31) >> 5, Tq = QTtot * 32;
@@ -398,19 +398,30 @@ __global__ __launch_bounds__(SCORE_WAVES * 64, 2) void span_score_kernel(SpanArg
     load(k, page_id(unit));
     int page = page_id(unit + units);
     u32x4_t *qs = reinterpret_cast<u32x4_t *>(lds);
-    SpanQuery *sq = reinterpret_cast<SpanQuery *>(qs + QS * KS * 64);
+    float *begin = reinterpret_cast<float *>(qs + QS * KS * 64);          // -M' of the queries; no weight at all: -infinity
+    uint32_t *sees = reinterpret_cast<uint32_t *>(begin + QS * 32) + wave * 32;
+    SpanQuery *sq = reinterpret_cast<SpanQuery *>(begin + QS * 32 + NW * 32);
+    for (int i = tid; i < QS * 32; i += NW * 64) {
+        const bool counts = i < p.n_scored;
+        const SpanStat s = p.stats[((size_t)b * H + h) * Tq + (counts ? i : 0)];
+        begin[i] = counts ? __builtin_amdgcn_logf(s.r) / p.c - s.m : -INFINITY;
+        sq[i] = span_query(p, r, counts ? i : p.T);
+    }
     for (int i = wave; i < QS * KS; i += NW) qs[i * 64 + lane] = span_query_piece<DH>(p, b, h, min(i / KS, QTtot - 1), QTtot, col, 16 * (i % KS) + 8 * hl);
-    for (int i = tid; i < QS * 32; i += NW * 64) sq[i] = span_query(p, r, i < p.n_scored ? i : p.T);
-    f32x16_t start[QS];                                     // -M' of the queries in the accumulators' rows; no weight at all: -infinity
-#pragma unroll
-    for (int q = 0; q < QS; ++q)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int query = q * 32 + 8 * (v >> 2) + 4 * hl + (v & 3);
-            const SpanStat s = p.stats[((size_t)b * H + h) * Tq + max(min(query, p.n_scored - 1), 0)];
-            start[q][v] = query < p.n_scored ? __builtin_amdgcn_logf(s.r) / p.c - s.m : -INFINITY;
-        }
     __syncthreads();
+    auto begins = [&](int q) {                              // in the accumulators' rows
+        f32x16_t z;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4_t v = *reinterpret_cast<const f32x4_t *>(begin + q * 32 + 8 * g + 4 * hl);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[4 * g + e] = v[e];
+        }
+        return z;
+    };
+    f32x16_t start[QS];
+#pragma unroll
+    for (int q = 0; q < QS; ++q) start[q] = begins(q);
     float *row = p.score + ((size_t)b * H + h) * ((size_t)p.max_pages * 16);
     for (int u = unit; u < r.n; u += units) {
         const int slot0 = r.tile(u) * 32, slot = slot0 + col;
@@ -422,20 +433,36 @@ __global__ __launch_bounds__(SCORE_WAVES * 64, 2) void span_score_kernel(SpanArg
         float sum = 0.f;
         int at = lane;
         asm volatile("" : "+v"(at));                         // keeps the reads of the queries inside the loop
+        auto product = [&](int from, f32x16_t z) {
 #pragma unroll
-        for (int q = 0; q < QS; ++q) {
-            f32x16_t z = start[q];
+            for (int s = 0; s < KS; ++s) z = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, qs[from + s * 64]), __builtin_bit_cast(a16x8_t, k[s]), z);
+            return z;
+        };
+        if (whole) {                                         // no branch between the products: one query tile's reads and products go beside the other's exponentials
 #pragma unroll
-            for (int s = 0; s < KS; ++s) z = HYDRA_MFMA16(__builtin_bit_cast(a16x8_t, qs[at + (q * KS + s) * 64]), __builtin_bit_cast(a16x8_t, k[s]), z);
-            if (!whole) {
-                uint32_t sees = 0;                           // a bit for each of the lane's queries
-#pragma unroll 1
-                for (int v = 0; v < 16; ++v) sees |= ((span_seen(r, sq[q * 32 + 8 * (v >> 2) + 4 * hl + (v & 3)], slot0) >> col) & 1u) << v;
+            for (int q = 0; q < QS; ++q) {
+                const f32x16_t z = product(at + q * KS * 64, start[q]);
+                float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int v = 0; v < 16; ++v) z[v] = (sees >> v) & 1u ? z[v] : -INFINITY;
+                for (int v = 0; v < 16; ++v) part[v & 3] += __builtin_amdgcn_exp2f(z[v] * p.c);
+                sum += (part[0] + part[1]) + (part[2] + part[3]);
+                if (q & 1) __builtin_amdgcn_sched_barrier(0);          // four tiles at once do not fit the registers
             }
+        } else {
+#pragma unroll 1
+            for (int q = 0; q < QS; ++q) {
+                const f32x16_t z = product(at + q * KS * 64, begins(q));
+                // what each query sees is worked out once, by the lane of its number, and read by all through LDS, which is in order within a wave
+                asm volatile("" ::: "memory");
+                if (hl == 0) sees[col] = span_seen(r, sq[q * 32 + col], slot0);
+                asm volatile("" ::: "memory");
 #pragma unroll
-            for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(z[v] * p.c);
+                for (int g = 0; g < 4; ++g) {
+                    const u32x4_t w = *reinterpret_cast<const u32x4_t *>(sees + 8 * g + 4 * hl);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum += (w[e] >> col) & 1u ? __builtin_amdgcn_exp2f(z[4 * g + e] * p.c) : 0.f;
+                }
+            }
         }
         const HalfWaves two = half_waves(sum);
         if (mine) row[slot] = before + (two.lo + two.hi);
@@ -515,7 +542,7 @@ int launch_span_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const v
     const int QS = a.n_scored <= 32 ? 1 : a.n_scored <= 64 ? 2 : 4;
     a.key_wgs = std::max(1, std::min(ceil_div(tiles, SCORE_WAVES), std::max(1, (QS == 1 ? 1024 : 512) / (H * B))));
     const dim3 sgrid(ceil_div(H * B, 8) * 8 * a.key_wgs), sblock(SCORE_WAVES * 64);
-    const size_t slds = (size_t)QS * ((Dh / 16) * 1024 + 32 * sizeof(SpanQuery));
+    const size_t slds = (size_t)QS * ((Dh / 16) * 1024 + 32 * (4 + sizeof(SpanQuery))) + SCORE_WAVES * 128;
 #define LAUNCH(DHv, QSv) if (Dh == DHv && QS == QSv) hipLaunchKernelGGL((span_score_kernel<DHv, QSv>), sgrid, sblock, slds, s, a);
     LAUNCH(128, 1) LAUNCH(128, 2) LAUNCH(128, 4) LAUNCH(64, 1) LAUNCH(64, 2) LAUNCH(64, 4)
 #undef LAUNCH
