@@ -366,7 +366,7 @@ __global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs p, int blocks)
 // Queries are the rows of S = Q K^T here, so that a lane holds one slot and adds over its registers, and -M' is what the accumulators of the product begin with: a score costs a
 // multiplication, an exponential and an addition.  A wave takes 32-key tiles in turn, the next one's K under way; no two waves hold the same slot, so no sum depends
 // on an order of arrival.
-enum { SCORE_WAVES = 4 };
+enum { SCORE_WAVES = 8 };
 template <int DH, int QS>
 __global__ __launch_bounds__(SCORE_WAVES * 64, 2) void span_score_kernel(SpanArgs p) {
     constexpr int KS = DH / 16, NW = SCORE_WAVES;
@@ -540,7 +540,7 @@ int launch_span_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const v
         if (int rc = launch_span_merge(c, s, a, slots)) return rc;
     if (!a.score || a.z) return HYDRA_OK;
     const int QS = a.n_scored <= 32 ? 1 : a.n_scored <= 64 ? 2 : 4;
-    a.key_wgs = std::max(1, std::min(ceil_div(tiles, SCORE_WAVES), std::max(1, (QS == 1 ? 1024 : 512) / (H * B))));
+    a.key_wgs = std::max(1, std::min(ceil_div(tiles, SCORE_WAVES), std::max(1, (QS == 1 ? 512 : 256) / (H * B))));
     const dim3 sgrid(ceil_div(H * B, 8) * 8 * a.key_wgs), sblock(SCORE_WAVES * 64);
     const size_t slds = (size_t)QS * ((Dh / 16) * 1024 + 32 * (4 + sizeof(SpanQuery))) + SCORE_WAVES * 128;
 #define LAUNCH(DHv, QSv) if (Dh == DHv && QS == QSv) hipLaunchKernelGGL((span_score_kernel<DHv, QSv>), sgrid, sblock, slds, s, a);
