@@ -22,7 +22,7 @@ __device__ __forceinline__ float over_keys(float v, Op op) {
     return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-enum { SPAN32_WAVES = 4, SPAN32_QT = 2 };
+enum { SPAN32_WAVES = 8, SPAN32_QT = 2 };
 template <int DH>
 __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p) {
     constexpr int KS = DH / 16, J = DH / 64, NW = SPAN32_WAVES, QT = SPAN32_QT;
@@ -64,17 +64,49 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
     float m_run[QT], l_run[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) { m_run[t] = -INFINITY; l_run[t] = 0.f; }
-    for (int u = unit; u < r.n; u += units) {
-        const int lp = r.tile(u), slot0 = lp * 16;
-        const bool whole = span_whole<16>(p, r, slot0);     // uniform
-        const size_t base = kv_block_base(p.layer, p.n_pages, checked_page(pt[lp], p.n_pages, p.flags), H, h, DH);
-        f32x4_t k[KS], v[4][J];
+    // K of the next tile is asked for behind this one's first product, V behind the second, page numbers a tile ahead; behind the last tile: the last one again
+    auto tile_page = [&](int u) { return pt[r.tile(min(u, r.n - 1))]; };
+    f32x4_t k[KS], v[4][J];
+    auto load_k = [&](size_t base) {
 #pragma unroll
         for (int i = 0; i < KS; ++i) k[i] = *reinterpret_cast<const f32x4_t *>(kpages + base + col * DH + 16 * i + 4 * g);
+    };
+    auto load_v = [&](size_t base) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int jj = 0; jj < J; ++jj) v[e][jj] = *reinterpret_cast<const f32x4_t *>(vpages + base + (4 * g + e) * DH + 64 * jj + 4 * col);
+    };
+    auto base_of = [&](int page) { return kv_block_base(p.layer, p.n_pages, checked_page(page, p.n_pages, p.flags), H, h, DH); };
+    size_t base = 0;
+    int page = 0;
+    if (unit < r.n) {
+        base = base_of(tile_page(unit));
+        page = tile_page(unit + units);
+        load_k(base);
+        load_v(base);
+    }
+    for (int u = unit; u < r.n; u += units) {
+        const int slot0 = r.tile(u) * 16;
+        const bool whole = span_whole<16>(p, r, slot0);     // uniform
+        f32x4_t st[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            f32x4_t s = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {                   // two chains: a product waits for the one before it in its own
+                const f32x4_t qv = qs[(t * KS + i) * 64 + lane];
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    s = SPAN_MFMA4(k[i][e], qv[e], s);
+                    s1 = SPAN_MFMA4(k[i][e + 1], qv[e + 1], s1);
+                }
+            }
+            st[t] = s + s1;
+        }
+        const size_t next = base_of(page);
+        page = tile_page(u + 2 * units);
+        load_k(next);
         bool odd = false;                                   // something that is not finite in a tile that not every query sees whole
         if (!whole) {
             const uint32_t held = span_held(r, slot0);
@@ -90,17 +122,7 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
         }
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            f32x4_t s = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < KS; ++i) {                   // two chains: a product waits for the one before it in its own
-                const f32x4_t qv = qs[(t * KS + i) * 64 + lane];
-#pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    s = SPAN_MFMA4(k[i][e], qv[e], s);
-                    s1 = SPAN_MFMA4(k[i][e + 1], qv[e + 1], s1);
-                }
-            }
-            s += s1;
+            f32x4_t s = st[t];
             if (!whole) {
                 const uint32_t seen = span_seen(r, sq[t], slot0) >> (4 * g);
 #pragma unroll
@@ -141,6 +163,8 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
                     }
             }
         }
+        base = next;
+        load_v(base);
     }
     // ---- merge the waves through LDS, one query tile after the other
     if (g == 0) {
@@ -292,7 +316,9 @@ int span_f32_max_dynamic_lds() {
 
 int launch_span_f32(hydra_ctx *c, hipStream_t s, SpanArgs a, int slots, int units_max) {
     const int T = a.T, Dh = c->m.head_dim, pages = ceil_div(slots, 16) + 2, hb = a.groups * ceil_div(T, 16 * SPAN32_QT);
-    a.key_wgs = std::max(1, std::min({ceil_div(pages, SPAN32_WAVES * 2), std::max(1, 512 / hb), units_max}));
+    // two pages of a wave cost less than a second kernel: 200 tokens 10.0 us against 10.2, 400 tokens with a kernel more 10.3 against 13.9.  Twice the workgroups leave
+    // twice the records (2 rows of 64 nodes behind 2000 tokens, 16 heads of 128: 49 us instead of 40, of which half the waves to a workgroup are a part)
+    a.key_wgs = pages <= 2 * SPAN32_WAVES ? 1 : std::max(1, std::min({ceil_div(pages, SPAN32_WAVES), std::max(1, 256 / hb), units_max}));
     const dim3 grid(ceil_div(a.groups, 8) * 8 * ceil_div(T, 16 * SPAN32_QT) * a.key_wgs), block(SPAN32_WAVES * 64);
     if (Dh == 128) hipLaunchKernelGGL(span_f32_kernel<128>, grid, block, 0, s, a);
     else           hipLaunchKernelGGL(span_f32_kernel<64>, grid, block, 0, s, a);
@@ -303,7 +329,7 @@ int launch_span_f32(hydra_ctx *c, hipStream_t s, SpanArgs a, int slots, int unit
     }
     if (!a.score || a.z) return HYDRA_OK;
     const int QS = ceil_div(a.n_scored, 16);
-    a.key_wgs = std::max(1, std::min(ceil_div(pages, SPAN32_WAVES), std::max(1, 1024 / a.groups)));
+    a.key_wgs = std::max(1, std::min(ceil_div(pages, SPAN32_WAVES), std::max(1, 256 / a.groups)));
     const dim3 sgrid(ceil_div(a.groups, 8) * 8 * a.key_wgs);
     const size_t lds = (size_t)QS * ((Dh / 16) * 1024 + 16 * (sizeof(SpanQuery) + 4));
     if (Dh == 128) hipLaunchKernelGGL(span_score_f32_kernel<128>, sgrid, block, lds, s, a);
