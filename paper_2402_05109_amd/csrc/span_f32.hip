@@ -89,13 +89,15 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
     for (int u = unit; u < r.n; u += units) {
         const int slot0 = r.tile(u) * 16;
         const bool whole = span_whole<16>(p, r, slot0);     // uniform
+        int at = lane;
+        asm volatile("" : "+v"(at));                         // keeps the reads of the queries inside the loop
         f32x4_t st[QT];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             f32x4_t s = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < KS; ++i) {                   // two chains: a product waits for the one before it in its own
-                const f32x4_t qv = qs[(t * KS + i) * 64 + lane];
+                const f32x4_t qv = qs[(t * KS + i) * 64 + at];
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) {
                     s = SPAN_MFMA4(k[i][e], qv[e], s);
@@ -316,8 +318,8 @@ int span_f32_max_dynamic_lds() {
 
 int launch_span_f32(hydra_ctx *c, hipStream_t s, SpanArgs a, int slots, int units_max) {
     const int T = a.T, Dh = c->m.head_dim, pages = ceil_div(slots, 16) + 2, hb = a.groups * ceil_div(T, 16 * SPAN32_QT);
-    // two pages of a wave cost less than a second kernel: 200 tokens 10.0 us against 10.2, 400 tokens with a kernel more 10.3 against 13.9.  Twice the workgroups leave
-    // twice the records (2 rows of 64 nodes behind 2000 tokens, 16 heads of 128: 49 us instead of 40, of which half the waves to a workgroup are a part)
+    // two pages of a wave cost about what a second kernel does (16 nodes, 4 heads of 64: a window of 100 9.5 us against 10.3; 400 tokens 9.8, with four pages of a wave
+    // 13.7).  More workgroups than compute units leave more records only (2 rows of 64 nodes behind 2000 tokens, 16 heads of 128: 43 us instead of 37)
     a.key_wgs = pages <= 2 * SPAN32_WAVES ? 1 : std::max(1, std::min({ceil_div(pages, SPAN32_WAVES), std::max(1, 256 / hb), units_max}));
     const dim3 grid(ceil_div(a.groups, 8) * 8 * ceil_div(T, 16 * SPAN32_QT) * a.key_wgs), block(SPAN32_WAVES * 64);
     if (Dh == 128) hipLaunchKernelGGL(span_f32_kernel<128>, grid, block, 0, s, a);
