@@ -29,28 +29,42 @@ __device__ __forceinline__ uint32_t score_key(float v) {
     return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
-// over the 64 lanes, the same in all of them
-__device__ __forceinline__ int wave_total(int v) {
-    const auto a = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
-    v = (int)(a[0] + a[1]);
-    const auto b = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
-    v = (int)(b[0] + b[1]);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, false);            // row_ror:8, 4, 2, 1
-    v += __builtin_amdgcn_update_dpp(0, v, 0x124, 0xf, 0xf, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x122, 0xf, 0xf, false);
-    return v + __builtin_amdgcn_update_dpp(0, v, 0x121, 0xf, 0xf, false);
+// the largest over the 64 lanes, the same in all of them
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(b[0], b[1]);
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, false));            // row_ror:8, 4, 2, 1
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xf, 0xf, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, false));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, false));
+}
+// sums over the lanes up to this one
+__device__ __forceinline__ int wave_prefix(int v, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(v, d);
+        if (lane >= d) v += y;
+    }
+    return v;
 }
 
-// One workgroup per (head, row, layer) finds what it keeps.  The key of the last token that is kept (`want` tokens have it or a larger one) is found from
-// its upper bits down, two at a time, by counting; tokens with that very key are taken from the lowest slot on.  Counting takes a comparison and an addition per
-// candidate and bound (with lanes counted by the scalar unit 13B took 39 us instead of 31), a turn a barrier; it ends as soon as a bound has just `want` candidates, for distinct scores once the bits tell its
-// neighbours apart.  A thread holds PER neighbouring candidates in registers; rows that have more than THREADS * PER are read again for every count.
+// One workgroup per (head, row, layer) finds what it keeps.  Between the smallest and the largest key, the bracket, lies the key of the last token that is kept
+// (`want` tokens have it or a larger one): candidates are counted in BINS parts of the bracket, which then becomes the part that this key lies in, until all that
+// is in it stays or it is one key; tokens with that very key are taken from the lowest slot on.  Keys are in the order of the scores but spread like their
+// logarithms, so a second turn nearly always ends it (two bits of the key a turn, counted by comparisons with each candidate, took 38 us where this takes 19: 4 layers of 40 heads,
+// 15487 candidates).  A thread holds PER neighbouring candidates in registers; rows that have more than THREADS * PER are read again in every turn.
 template <int THREADS, int PER>
 __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
     constexpr int WAVES = THREADS / 64, PIECE = THREADS * PER;
-    constexpr int BITS = 2, M = (1 << BITS) - 1;             // three bits at a time: fewer turns of more comparisons, 7B 24 us instead of 20
-    __shared__ int cnt[2][WAVES][4];
+    constexpr int BINS = THREADS * 4, LOG = THREADS == 256 ? 10 : THREADS == 512 ? 11 : 12;
+    static_assert(1 << LOG == BINS, "");
+    typedef __attribute__((ext_vector_type(4), may_alias)) int i32x4_t;
+    __shared__ i32x4_t bins[THREADS];                        // of thread tid: the 4 from bin 4 * (THREADS - 1 - tid) on
     __shared__ int part[WAVES];
+    __shared__ uint32_t ends[2][WAVES];
+    __shared__ int found[3];                                 // a bin, how many candidates lie above it, how many in it
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int h = blockIdx.x, b = blockIdx.y, layer = blockIdx.z, H = gridDim.x, B = gridDim.y;
     const bool speaks = tid == 0 && h == 0 && layer == 0;
@@ -87,6 +101,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
         for (int e = 0; e < PER; ++e) key[e] = id + e < n ? score_key(x[e]) : 0u;
     };
     load(0);
+    bins[tid] = i32x4_t{0, 0, 0, 0};
     const int32_t *pt = a.table + (size_t)b * a.max_pages;
     int bad = 0;                                            // 1: an entry that names no page, 2: a page that is shared
     for (int lp = (F >> 4) + tid; lp <= (L - 1) >> 4; lp += THREADS) {
@@ -97,6 +112,18 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
     if (a.dst_table)
         for (int lp = ((L - a.keep) >> 4) + tid; lp <= (L - 1) >> 4; lp += THREADS)
             if ((unsigned)a.dst_table[(size_t)b * a.max_pages + lp] >= (unsigned)a.n_pages) bad |= 1;
+    uint32_t top = 0u, low = 0u;                            // the largest key, and the complement of the smallest
+    for (int pc = 0; pc < pieces; ++pc) {
+        if (pc > 0) load(pc);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            top = max(top, key[e]);
+            low = max(low, key[e] ? ~key[e] : 0u);
+        }
+    }
+    top = wave_max(top);
+    low = wave_max(low);
+    if (lane == 0) { ends[0][wave] = top; ends[1][wave] = low; }
     const int none = __syncthreads_or(bad & 1), shared = __syncthreads_or(bad & 2);
     if (none || shared) {
         if (speaks) { atomicOr(a.flags, (none ? FLAG_BAD_PAGE : 0) | (shared ? FLAG_CAPACITY : 0)); a.evicted[b] = 0; }
@@ -107,66 +134,58 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
     for (int j = tid; j < a.n_sinks; j += THREADS) kept[j] = F + j;
     for (int j = tid; j < a.n_recent; j += THREADS) kept[a.keep - a.n_recent + j] = L - a.n_recent + j;
     if (want > 0) {
-        int turn = 0;
-        // how many candidates have a key of at least t[i]
-        auto count = [&](const uint32_t (&t)[M], int (&c)[M]) {
 #pragma unroll
-            for (int i = 0; i < M; ++i) c[i] = 0;
+        for (int w = 0; w < WAVES; ++w) {
+            top = max(top, ends[0][w]);
+            low = max(low, ends[1][w]);
+        }
+        uint32_t lo = ~low;                                 // the bracket: lo .. lo + 2^width - 1
+        int width = 32 - __clz((int)(top - lo));
+        int stay = want, inside = n;                        // of the bracket's candidates
+        while (width > 0 && stay < inside) {                // uniform over the workgroup
+            const int shift = max(width - LOG, 0);
+            const uint32_t most = width == 32 ? 0xffffffffu : (1u << width) - 1u;
             for (int pc = 0; pc < pieces; ++pc) {
                 if (pieces > 1) load(pc);
 #pragma unroll
-                for (int e = 0; e < PER; ++e)
-#pragma unroll
-                    for (int i = 0; i < M; ++i) c[i] += key[e] >= t[i] ? 1 : 0;
+                for (int e = 0; e < PER; ++e) {
+                    const uint32_t bin = (key[e] - lo) >> shift;
+                    if (key[e] >= lo && key[e] - lo <= most) atomicAdd(reinterpret_cast<int *>(bins) + (bin ^ (BINS - 4)), 1);
+                }
             }
-#pragma unroll
-            for (int i = 0; i < M; ++i) c[i] = wave_total(c[i]);
-            if (lane == 0)
-#pragma unroll
-                for (int i = 0; i < M; ++i) cnt[turn][wave][i] = c[i];
             __syncthreads();
+            const i32x4_t c = bins[tid];
+            bins[tid] = i32x4_t{0, 0, 0, 0};
+            const int sum = (c[0] + c[1]) + (c[2] + c[3]), upto = wave_prefix(sum, lane);
+            if (lane == 63) part[wave] = upto;
+            __syncthreads();
+            int above = upto - sum;
 #pragma unroll
-            for (int i = 0; i < M; ++i) c[i] = 0;
+            for (int w = 0; w < WAVES; ++w) above += w < wave ? part[w] : 0;
+            if (above < stay && above + sum >= stay) {       // one thread's
+                int i = 3;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w)
-#pragma unroll
-                for (int i = 0; i < M; ++i) c[i] += cnt[turn][w][i];
-            turn ^= 1;                                      // read by everybody before the next barrier, written again behind it
-        };
-        uint32_t last = 0u, t[M];
-        int c[M];
-        for (int shift = 32 - BITS; shift > -BITS; shift -= BITS) {
-#pragma unroll
-            for (int i = 0; i < M; ++i) t[i] = last | ((uint32_t)(i + 1) << max(shift, 0));
-            count(t, c);
-            bool exact = false;                             // nothing is left to tell apart: the largest bound that enough candidates reach has just so many
-#pragma unroll
-            for (int i = 0; i < M; ++i) {
-                last = c[i] >= want ? t[i] : last;
-                exact |= c[i] == want;
+                for (int q = 3; q > 0; --q)
+                    if (i == q && above + c[q] < stay) { above += c[q]; i = q - 1; }
+                found[0] = 4 * (THREADS - 1 - tid) + i;
+                found[1] = above;
+                found[2] = i == 3 ? c[3] : i == 2 ? c[2] : i == 1 ? c[1] : c[0];
             }
-            if (exact) break;
+            __syncthreads();
+            lo += (uint32_t)found[0] << shift;
+            stay -= found[1];
+            inside = found[2];
+            width = shift;
         }
-        int above = 0;
-        if (last != 0xffffffffu) {
-#pragma unroll
-            for (int i = 0; i < M; ++i) t[i] = last + 1u;
-            count(t, c);
-            above = c[0];
-        }
-        const int equal = want - above;                     // of those with the key `last`, the lowest slots
+        const uint32_t last = stay == inside ? lo - 1u : lo;         // the smallest key is above 0
+        const int equal = stay == inside ? 0 : stay;        // of those with the key `last`, the lowest slots
         int seen_gt = 0, seen_eq = 0;
         for (int pc = 0; pc < pieces; ++pc) {
             if (pieces > 1) load(pc);
             int mine = 0;
 #pragma unroll
             for (int e = 0; e < PER; ++e) mine += (key[e] > last ? 1 : 0) + (key[e] == last && key[e] != 0u ? 0x10000 : 0);
-            int x = mine;                                   // two sums in one: a piece has at most 2^15 candidates
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int y = __shfl_up(x, d);
-                if (lane >= d) x += y;
-            }
+            const int x = wave_prefix(mine, lane);          // two sums in one: a piece has at most 2^15 candidates
             __syncthreads();                                // `part` may still be read from the piece before
             if (lane == 63) part[wave] = x;
             __syncthreads();

@@ -85,6 +85,29 @@ def test_in_place(case, kind, f32):
     check(c, kv, kvd, lens, firsts, score0, score, first, kept, evicted, sinks, recent, keep, slack, f32)
 
 
+@pytest.mark.parametrize("kind", ["plain", "odd", "close", "wide", "two"])
+@pytest.mark.parametrize("L, hint", [(40000, 0), (3000, 20), (6000, 1500), (9000, 5000), (1000, 0), (4000, 0)])
+def test_choice_among_many(L, hint, kind):
+    """More candidates than a workgroup holds in registers; scores that differ in their last bits, that fill the type's range, or that have two values."""
+    NL, H, Dh, sinks, recent, keep = 1, 2, 64, 3, 20, L // 3
+    c, kv, kvd, n, first = setup([L], [5], NL, H, Dh, False, 3)
+    shape = (NL, 1, H, kvd.max_pages * 16)
+    if kind == "close":
+        score0 = scores("ties", shape, 5) * 0 + 1 + torch.randint(0, 300, shape, generator=torch.Generator().manual_seed(5)).to(DEV) * 2.0 ** -23
+    elif kind == "wide":
+        bits = torch.randint(-2 ** 31, 2 ** 31, shape, generator=torch.Generator().manual_seed(5)).to(torch.int32)
+        score0 = bits.view(torch.float32).to(DEV)
+    elif kind == "two":
+        score0 = (scores("plain", shape, 5) > 0.05).float()
+    else:
+        score0 = scores(kind, shape, 5)
+    score = score0.clone()
+    kept = torch.full((NL, 1, H, keep), -7, dtype=torch.int32, device=DEV)
+    evicted = torch.full((1,), -7, dtype=torch.int32, device=DEV)
+    c.hydra_kv_evict(1, n, hb.KVSpan(kvd, first=first, n_sinks=sinks, score=score, span_hint=hint), keep, recent, 0, kept, evicted)
+    check(c, kv, kvd, [L], [5], score0, score, first, kept, evicted, sinks, recent, keep, 0, False)
+
+
 @pytest.mark.parametrize("f32", [False, True])
 @pytest.mark.parametrize("case", [1, 3, 6, 7, 8, 9, 13])
 def test_into_other_pages(case, f32):
