@@ -361,29 +361,35 @@ class Hydra:
         _check(_lib.hydra_kv8_read(self._h, _stream(), B, layer, C.byref(d), first_slot, n_slots, _ptr(plain, torch.float32, "kv_plain")))
 
     # ---- part of a cache
+    def _span_desc(self, span: KVSpan) -> KVSpanDesc:
+        want = (self.model.n_layers, self.model.n_heads)
+        if span.score is not None and ((span.score.shape[0], span.score.shape[2]) != want or span.score.numel() == 0):
+            raise ValueError(f"score: expected {want[0]} layers of {want[1]} heads and rows of slots, got {tuple(span.score.shape)}")
+        return span.desc()
+
     def tree_verify_forward_span(self, B, ws, tree_tokens, seq_len, span: KVSpan, hidden, argmax, margin=None, logits=None) -> None:
-        d = span.desc()
+        d = self._span_desc(span)
         _check(_lib.tree_verify_forward_span(self._h, _stream(), B, _ptr(ws, torch.uint8, "ws"), _ptr(tree_tokens, torch.int32, "tree_tokens"),
                                              _ptr(seq_len, torch.int32, "seq_len"), C.byref(d), _ptr(hidden, torch.float32, "hidden"),
                                              _ptr(argmax, torch.int32, "argmax"), _ptr(margin, torch.float32, "margin"), _ptr(logits, torch.float32, "logits")))
 
     def hydra_prefill_chunk_span(self, B, ws, tree_tokens, seq_len, span: KVSpan) -> None:
-        d = span.desc()
+        d = self._span_desc(span)
         _check(_lib.hydra_prefill_chunk_span(self._h, _stream(), B, _ptr(ws, torch.uint8, "ws"), _ptr(tree_tokens, torch.int32, "tree_tokens"),
                                              _ptr(seq_len, torch.int32, "seq_len"), C.byref(d)))
 
     def tree_attention_span(self, B, layer, ws, q, seq_len, span: KVSpan, out) -> None:
-        d = span.desc()
+        d = self._span_desc(span)
         _check(_lib.tree_attention_span(self._h, _stream(), B, layer, _ptr(ws, torch.uint8, "ws"), _ptr(q, self._cache_dtype, "q"),
                                         _ptr(seq_len, torch.int32, "seq_len"), C.byref(d), _ptr(out, self._cache_dtype, "out")))
 
     def hydra_score_compact(self, B, n_acc, path, seq_len, span: KVSpan) -> None:
-        d = span.desc()
+        d = self._span_desc(span)
         _check(_lib.hydra_score_compact(self._h, _stream(), B, _ptr(n_acc, torch.int32, "n_acc"), _ptr(path, torch.int32, "path"),
                                         _ptr(seq_len, torch.int32, "seq_len"), C.byref(d)))
 
     def hydra_kv_evict(self, B, seq_len, span: KVSpan, keep, n_recent, slack, kept, evicted, dst_table=None, ref=None) -> None:
-        d = span.desc()
+        d = self._span_desc(span)
         _check(_lib.hydra_kv_evict(self._h, _stream(), B, _ptr(seq_len, torch.int32, "seq_len"), C.byref(d), int(keep), int(n_recent), int(slack),
                                    _ptr(dst_table, torch.int32, "dst_table"), _ptr(ref, torch.int32, "ref"), _ptr(kept, torch.int32, "kept"),
                                    _ptr(evicted, torch.int32, "evicted")))

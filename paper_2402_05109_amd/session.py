@@ -495,7 +495,7 @@ class Session:
         tree_verify_forward with a chain tree; the state update is kv_compact with the
         identity path.  Where an exception breaks the prompt off, seq_len, h_last and root are those behind the last chunk that was
         computed whole (behind the text in front of the prompt if there is none).  behind_chunk(context, position, tokens) is called when a chunk's outputs are
-        there, which then all chunks have."""
+        there, which then all chunks have.  With a budget, what a chunk that was broken off added to the weights of the tokens in front of it stays."""
         B, L = prompts.shape
         assert B == self.B or (self.pool and B < self.B)
         prompts = prompts.to(self.dev, torch.int32)
@@ -606,6 +606,8 @@ class Session:
         """prefill(prompts), and what the model thought of them: entry i of a row is about the token behind prompt token i (behind the last one: none given).
         The mean of -logprob over a text says what a window, a budget or an 8-bit cache costs."""
         B, L = prompts.shape
+        if not L or not self.want_logits:
+            raise ValueError("log probabilities need a prompt, and the logits: create the Session with want_logits=True")
         parts: List[Dict[str, torch.Tensor]] = []
         given = torch.cat([prompts[:, 1:].to(self.dev, torch.int32), torch.full((B, 1), -1, dtype=torch.int32, device=self.dev)], dim=1)
         self.prefill(prompts, lambda name, pos, n: parts.append(self.logprobs(given[:, pos:pos + n], tau, k, name, B)))

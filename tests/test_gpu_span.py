@@ -229,6 +229,22 @@ def test_another_layer_another_stream_and_a_graph(f32):
     assert c.read_flags() == 0
 
 
+@pytest.mark.parametrize("shape", [(1, 1, 2), (3, 1, 2), (2, 1, 1), (2, 1, 4), (2, 0, 2)])
+def test_scores_of_another_model_are_refused(shape):
+    c = context(2, 64, 1, [-1], NL=2, max_pos=64)
+    kv = torch.zeros(2, 1, 33, 2, 2, 64, dtype=torch.float16)
+    kvd = cache(c, 2, 64, kv, torch.ones(1, 1, 33, dtype=torch.bool), False, NL=2)
+    score = torch.zeros(*shape, 16 * kvd.max_pages, device=DEV)
+    n, q = torch.tensor([32], dtype=torch.int32, device=DEV), torch.zeros(1, 1, 2, 64, dtype=torch.float16, device=DEV)
+    span = hb.KVSpan(kvd, first=torch.zeros_like(n), score=score, n_scored=1)
+    ids = torch.zeros(1, 8, dtype=torch.int32, device=DEV)
+    for call in (lambda: c.tree_attention_span(1, 0, c.ws, q, n, span, torch.empty_like(q)), lambda: c.hydra_score_compact(1, n, ids, n, span),
+                 lambda: c.hydra_kv_evict(1, n, span, 8, 2, 0, torch.zeros(2, 1, 2, 8, dtype=torch.int32, device=DEV), ids[0])):
+        with pytest.raises((ValueError, hb.HydraError)):
+            call()
+    assert (score == 0).all()
+
+
 def test_slots_beyond_two_gigabytes_of_scores_and_pages():
     """Offsets that pass 32 bits: pages behind 4 GiB of others, scores of a late row."""
     H, Dh, T, L = 16, 128, 3, 70

@@ -276,6 +276,12 @@ def test_log_probabilities_behind_a_step():
     plain = gpu_session(HALF, TREE, 1, 64, weights)
     with pytest.raises(ValueError):
         plain.logprobs()
+    prompt = torch.ones(1, 8, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        plain.prompt_logprobs(prompt)
+    assert plain.seq_len.tolist() == [0]
+    with pytest.raises(ValueError):
+        s.prompt_logprobs(prompt.expand(2, 8)[:, :0])
 
 
 @pytest.mark.parametrize("kw", [dict(window=0), dict(window=8, budget=(8, 2, 0)), dict(sinks=4), dict(window=8, sinks=-1), dict(budget=(0, 0, 0)), dict(budget=(8, 6, 0), sinks=3),
