@@ -201,7 +201,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LogprobArgs a) {
     const int tok = lp_token(a, row, given);
     uint2 *list = lists + (TOP ? wave * LP_LIST : 0);
     int count = 0;                                          // of the wave's list; beyond LP_LIST: so many would have gone there
-    float best = -INFINITY;
+    float best = -INFINITY, thr = -INFINITY;                // the largest of the lane's logits so far, and what k of the wave's reach
     LpSums s = {-INFINITY, 0.f, 0.f, 0.f};
     int above = 0;
     for (int at0 = 0; at0 < n; at0 += PORTION) {
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LogprobArgs a) {
             }
         if constexpr (TOP) {
             best = fmaxf(best, cm);
-            const float thr = lp_bound(logit_key(best), a.k);
+            thr = lp_bound(logit_key(best), a.k);
 #pragma unroll
             for (int i = 0; i < LP_PER / 4; ++i)
                 if (__any(gm[i] >= thr)) {
@@ -275,9 +275,8 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LogprobArgs a) {
     if (lane == 0) { sums[wave] = s; larger[wave] = above; }
     if constexpr (TOP) {
         // a bound for the whole piece: k logits reach that of any wave, and a WAVES-th of k in every wave the lowest of theirs
-        const uint32_t key = logit_key(best);
-        const float mine = lp_bound(key, a.k), quarter = lp_bound(key, (a.k + WAVES - 1) / WAVES);
-        if (lane == 0) { bounds[0][wave] = mine; bounds[1][wave] = quarter; counts[wave] = count; }
+        const float quarter = lp_bound(logit_key(best), (a.k + WAVES - 1) / WAVES);
+        if (lane == 0) { bounds[0][wave] = thr; bounds[1][wave] = quarter; counts[wave] = count; }
     }
     __syncthreads();
     // every wave joins the waves' sums
