@@ -106,11 +106,11 @@ template <int W, class Dot>
 __device__ __forceinline__ void span_add_root(const SpanArgs &p, const SpanRow &r, int b, int h, SpanStat st, int tid, int step, Dot dot) {
     const float *z = p.z + ((size_t)b * p.H + h) * p.z_slots;
     float *row = p.score + ((size_t)b * p.H + h) * ((size_t)p.max_pages * 16);
-    for (int i = tid; i < r.n * W; i += step) {
-        const int slot0 = r.tile(i / W) * W, k = i % W, slot = slot0 + k;
+    for (uint32_t i = tid; i < (uint32_t)(r.n * W); i += step) {         // (the step behind the last slot may pass 2^31)
+        const int slot0 = r.tile((int)(i / W)) * W, k = (int)(i % W), slot = slot0 + k;
         if (!((span_held(r, slot0) >> k) & 1u)) continue;
         float x;
-        if (i < p.z_slots) {
+        if (i < (uint32_t)p.z_slots) {
             x = z[i];
         } else {
             const SpanQuery q = span_query(p, r, 0);

@@ -80,13 +80,13 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
     float *score = a.score + (((size_t)layer * a.score_rows + b) * H + h) * ((size_t)a.max_pages * 16);
     int32_t *kept = a.kept + (((size_t)layer * B + b) * H + h) * (size_t)a.keep;
     const int c0 = F + a.n_sinks, n = L - a.n_recent - c0, want = a.keep - a.n_sinks - a.n_recent;      // candidates, and how many of them stay: want < n
-    const int pieces = (n + PIECE - 1) / PIECE;
+    const int pieces = (n - 1) / PIECE + 1;
     uint32_t key[PER];
     auto load = [&](int piece) {
-        const int id = piece * PIECE + tid * PER;
+        const uint32_t id = (uint32_t)piece * PIECE + tid * PER, end = (uint32_t)n;    // may pass 2^31 behind the last candidate
         float x[PER];
         typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
-        if (id + PER <= n) {
+        if (id + PER <= end) {
 #pragma unroll
             for (int e = 0; e < PER; e += 4) {
                 const f4u v = *reinterpret_cast<const f4u *>(score + c0 + id + e);
@@ -95,10 +95,10 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < PER; ++e) x[e] = score[c0 + min(id + e, n - 1)];
+            for (int e = 0; e < PER; ++e) x[e] = score[c0 + min(id + e, end - 1u)];
         }
 #pragma unroll
-        for (int e = 0; e < PER; ++e) key[e] = id + e < n ? score_key(x[e]) : 0u;
+        for (int e = 0; e < PER; ++e) key[e] = id + e < end ? score_key(x[e]) : 0u;
     };
     load(0);
     bins[tid] = i32x4_t{0, 0, 0, 0};
@@ -131,8 +131,8 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
     }
     if (speaks) a.evicted[b] = 1;
 
-    for (int j = tid; j < a.n_sinks; j += THREADS) kept[j] = F + j;
-    for (int j = tid; j < a.n_recent; j += THREADS) kept[a.keep - a.n_recent + j] = L - a.n_recent + j;
+    for (uint32_t j = tid; j < (uint32_t)a.n_sinks; j += THREADS) kept[j] = F + (int)j;
+    for (uint32_t j = tid; j < (uint32_t)a.n_recent; j += THREADS) kept[a.keep - a.n_recent + (int)j] = L - a.n_recent + (int)j;
     if (want > 0) {
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
