@@ -367,8 +367,8 @@ __global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs p, int blocks)
 //     score[s] += sum_n 2^((z_ns - M_n) c) / l_n = sum_n 2^((z_ns - M'_n) c),   M' = M + log2(l) / c
 // Queries are the rows of S = Q K^T here, so that a lane holds one slot and adds over its registers, and -M' is what the accumulators of the product begin with: a score costs a
 // multiplication, an exponential and an addition.  A wave takes 32-key tiles in turn, the next one's K under way; no two waves hold the same slot, so no sum depends
-// on an order of arrival.  Matrix and exponential units bound it: 40 heads x 128 queries x 16128 slots 44 us, of which the products are 18 at the matrix units' rate and
-// K's bytes 26 at 6.4 TB/s.
+// on an order of arrival.  K's bytes bound it: 40 heads x 128 queries x 16128 slots 44 us, 32 without the products and 35 without the exponentials, of which a tile per
+// wave takes 9 and the bytes 26 at 6.4 TB/s; a second tile ahead, and queries read from LDS ahead of the products, change nothing.
 enum { SCORE_WAVES = 8 };
 template <int DH, int QS>
 __global__ __launch_bounds__(SCORE_WAVES * 64, 2) void span_score_kernel(SpanArgs p) {
