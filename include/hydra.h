@@ -339,8 +339,8 @@ int accept_typical_static(hydra_ctx *ctx, void *stream, int B,
  *   logits device [B, T, V] fp32: tree_verify_forward's optional output       tokens device [B, T] int32
  *   logprob, entropy device [B, T] fp32 (out)       rank device [B, T] int32 (out)       each NULL where not wanted (tokens too, if neither logprob nor rank is)
  *   top_ids [B, T, k] int32, top_logprobs [B, T, k] fp32 (out): NULL if k == 0
- * Sums are fp32 and taken relative to the largest logit, so small entropies and log probabilities near 0 keep their digits.  k <= HYDRA_MAX_TOPK and <= V;
- * tau and 1 / tau positive and finite. */
+ * Sums are fp32 and taken relative to the largest logit, so small entropies and log probabilities near 0 keep their digits (a weight below 2^-126 of
+ * the largest counts as 0).  k <= HYDRA_MAX_TOPK and <= V; tau and 1 / tau positive and finite. */
 int hydra_token_logprobs(hydra_ctx *ctx, void *stream, int B, void *ws, const float *logits, const int32_t *tokens, float tau, int k,
                          float *logprob, int32_t *rank, float *entropy, int32_t *top_ids, float *top_logprobs);
 
