@@ -205,8 +205,9 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
 #pragma unroll
             for (int w = 1; w < NW; ++w) acc += ob[(w * J * 4 + id) * 64 + lane];
             const int dim = 64 * (id >> 2) + 16 * g + 4 * (id & 3);
+            if (query >= T) continue;                        // columns behind the last node go nowhere
             if (p.key_wgs > 1) *reinterpret_cast<f32x4_t *>(rec + (size_t)query * DH + dim) = acc;
-            else if (query < T) *reinterpret_cast<f32x4_t *>(reinterpret_cast<float *>(p.out) + ((size_t)(b * T + query) * H + h) * DH + dim) = acc * inv;
+            else *reinterpret_cast<f32x4_t *>(reinterpret_cast<float *>(p.out) + ((size_t)(b * T + query) * H + h) * DH + dim) = acc * inv;
         }
         if (wave == 0 && g == 0) {
             if (p.key_wgs > 1) {
