@@ -537,13 +537,14 @@ int launch_span_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const v
     //   48.6 against 50.3; with fewer workgroups eight: a row of 64 (4100) 22 against 27
     // - K and V pass the caches by where one workgroup reads them: a node (32000), 40 heads 107 against 122, 16 rows of 64 79 against 89; not where several query tiles read
     //   them: a row of 128 (4100) 31 against 35
-    // - one workgroup per head up to 20 tiles: a node (300) 8.2 against 9.6 with more of them and a second kernel, a row of 64 (600) 11.7 against 13.3; a node (570) 10.1 either way,
-    //   (1028) 12.4 against 16.2.  Behind several nodes a wave takes two tiles, which is worth as much as one behind a single node (there 14.2 against 12.4)
+    // - one workgroup per head up to 20 tiles, 36 behind more than 32 nodes: a node (300) 8.4 against 9.7 with more of them and a second kernel, (570) 9.8 against 10.3, (640) 12.0
+    //   against 10.5; a row of 64 (640) 11.9 against 13.5, (900) 13.8 against 14.4, (1200) 15.6 against 14.6.  Behind several nodes a wave takes two tiles, which is worth as
+    //   much as one behind a single node (a node (1028) then 14.2 against 12.4)
     // - as many workgroups as compute units: twice as many leave twice the records, a row of 64 (4100) 28 against 22
     const int qt = QTtot > 1 && (H * B * QTtot > 256 || tiles >= (QTtot == 2 ? 400 : 200)) ? 2 : 1, qgroups = ceil_div(QTtot, qt), hb = H * B * qgroups;
     const int nw = hb > 256 ? 4 : 8;
     const bool stream = qgroups == 1;
-    a.key_wgs = tiles <= 20 ? 1 : std::max(1, std::min({ceil_div(tiles, QTtot == 1 ? nw : nw * 2), std::max(1, 256 / hb), units_max, (int)SPAN_MERGE_MAX}));
+    a.key_wgs = tiles <= (QTtot == 1 ? 20 : 36) ? 1 : std::max(1, std::min({ceil_div(tiles, QTtot == 1 ? nw : nw * 2), std::max(1, 256 / hb), units_max, (int)SPAN_MERGE_MAX}));
     const dim3 grid(ceil_div(H * B, 8) * 8 * qgroups * a.key_wgs), block(nw * 64);
     const size_t lds = span_lds_bytes(Dh, qt, nw);
 #define LAUNCH(DHv, QTv, NWv, STv) \
