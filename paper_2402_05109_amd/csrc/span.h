@@ -55,12 +55,17 @@ __device__ __forceinline__ SpanRow span_row(const SpanArgs &p, int b) {
 
 // What one query sees: cached slots from `from` on or below `sinks` (never below F), and the tree slots that its ancestor mask names.
 struct SpanQuery { int from, sinks; uint64_t anc0, anc1; };
-__device__ __forceinline__ SpanQuery span_query(const SpanArgs &p, const SpanRow &r, int query) {
+struct SpanNode { int depth; uint64_t anc0, anc1; };                     // what the tree says of a query (behind the last node: of that one)
+__device__ __forceinline__ SpanNode span_node(const SpanArgs &p, int query) {
+    const int n = min(query, p.T - 1);
+    return {p.tree->depth[n], p.tree->anc[n][0], p.tree->anc[n][1]};
+}
+__device__ __forceinline__ SpanQuery span_query(const SpanArgs &p, const SpanRow &r, int query, const SpanNode &node) {
     SpanQuery s = {0x7fffffff, 0, 0ull, 0ull};                            // behind the last node: nothing
     if (query >= p.T) return s;
-    const int depth = p.tree->depth[query];
-    s.anc0 = p.tree->anc[query][0];
-    s.anc1 = p.tree->anc[query][1];
+    const int depth = node.depth;
+    s.anc0 = node.anc0;
+    s.anc1 = node.anc1;
     s.from = p.window > 0 ? max(r.F, r.L + depth + 1 - p.window) : r.F;
     s.sinks = r.F + min(p.n_sinks, r.total - r.F);
     if (p.window > 0 && p.window <= depth)                                // ancestors that are out of the window
@@ -73,6 +78,7 @@ __device__ __forceinline__ SpanQuery span_query(const SpanArgs &p, const SpanRow
         }
     return s;
 }
+__device__ __forceinline__ SpanQuery span_query(const SpanArgs &p, const SpanRow &r, int query) { return span_query(p, r, query, span_node(p, query)); }
 // the low n bits, n clamped to [0, 32]
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 

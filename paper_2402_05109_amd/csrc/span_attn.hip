@@ -15,15 +15,13 @@ namespace hydra {
 
 static constexpr float LOG2E = 1.44269504f;
 
-// 16 bytes of a query: dims d0 .. d0 + 7 of column `col` of a query tile (queries past the last one: zeros, or whatever the packed buffer holds; nobody
+// 16 bytes of a query: dims d0 .. d0 + 7 of column `col` of a query tile (queries past the last one: that one, or whatever the packed buffer holds; nobody
 // stores their result)
 template <int DH>
 __device__ __forceinline__ u32x4_t span_query_piece(const SpanArgs &p, int b, int h, int qtile, int QTtot, int col, int d0) {
-    if (!p.plain) return reinterpret_cast<const u32x4_t *>(p.q)[((((size_t)b * p.H + h) * QTtot + qtile) * (DH / 16) + (d0 >> 4)) * 64 + ((d0 >> 3) & 1) * 32 + col];
-    const int query = qtile * 32 + col;
-    u32x4_t v = {0u, 0u, 0u, 0u};
-    if (query < p.T) v = *reinterpret_cast<const u32x4_t *>(reinterpret_cast<const a16_t *>(p.q) + ((size_t)(b * p.T + query) * p.H + h) * DH + d0);
-    return v;
+    const size_t packed = ((((size_t)b * p.H + h) * QTtot + qtile) * (DH / 16) + (d0 >> 4)) * 64 + ((d0 >> 3) & 1) * 32 + col;
+    const size_t plain = ((size_t)(b * p.T + min(qtile * 32 + col, p.T - 1)) * p.H + h) * (DH / 8) + (d0 >> 3);
+    return reinterpret_cast<const u32x4_t *>(p.q)[p.plain ? plain : packed];
 }
 // the root's score for one slot
 template <int DH>
@@ -64,6 +62,17 @@ __global__ __launch_bounds__(NW * 64, 2) void span_attn_kernel(SpanArgs p) {
     const int group = seq / per * 8 + ((int)blockIdx.x & 7), j = seq % per;
     if (group >= p.groups) return;
     const int b = group / H, h = group - b * H, qg = j % QG, key_wg = j / QG;
+    // what does not depend on the row's length, beside the load of that (a row of 64 nodes behind 1028 tokens 13.3 us; behind it 14.1)
+    constexpr int PIECES = (QT * KS + NW - 1) / NW;
+    u32x4_t piece[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int at = min(wave + i * NW, QT * KS - 1), qtile = min(qg * QT + at / KS, QTtot - 1);       // a second tile behind the last query: the first one again, which nobody stores
+        piece[i] = span_query_piece<DH>(p, b, h, qtile, QTtot, col, 16 * (at % KS) + 8 * hl);
+    }
+    SpanNode node[QT];
+#pragma unroll
+    for (int q = 0; q < QT; ++q) node[q] = span_node(p, (qg * QT + q) * 32 + col);
     const int units = p.key_wgs * NW, unit = key_wg * NW + wave;
     const SpanRow r = span_row<32>(p, b);
     if (!r.ok) {                                            // uniform over the workgroup
@@ -80,13 +89,12 @@ __global__ __launch_bounds__(NW * 64, 2) void span_attn_kernel(SpanArgs p) {
     };
     int pgs = page_ids(0);
     u32x4_t *qs = reinterpret_cast<u32x4_t *>(lds);
-    for (int i = wave; i < QT * KS; i += NW) {
-        const int qtile = min(qg * QT + i / KS, QTtot - 1);  // a second tile behind the last query: the first one again, which nobody stores
-        qs[i * 64 + lane] = span_query_piece<DH>(p, b, h, qtile, QTtot, col, 16 * (i % KS) + 8 * hl);
-    }
     SpanQuery sq[QT];
 #pragma unroll
-    for (int q = 0; q < QT; ++q) sq[q] = span_query(p, r, (qg * QT + q) * 32 + col);
+    for (int q = 0; q < QT; ++q) sq[q] = span_query(p, r, (qg * QT + q) * 32 + col, node[q]);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+        if (wave + i * NW < QT * KS) qs[(wave + i * NW) * 64 + lane] = piece[i];
     __syncthreads();
 
     u32x4_t *mine = qs + (QT * KS + wave * TILE) * 64;      // this wave's tile: K blocks, then V blocks [page][dims / 32]
@@ -125,9 +133,9 @@ __global__ __launch_bounds__(NW * 64, 2) void span_attn_kernel(SpanArgs p) {
     float m_run[QT], l_run[QT];
 #pragma unroll
     for (int q = 0; q < QT; ++q) { m_run[q] = -INFINITY; l_run[q] = 0.f; }
-    // these have arrived: nothing in the loop is to wait for an ordinary load, which would be a wait for the DMA as well
     const bool root = p.z != nullptr && qg == 0;            // this workgroup holds the root, whose scores are wanted
     float *z0 = p.z + ((size_t)b * H + h) * p.z_slots;
+    // these have arrived: nothing in the loop is to wait for an ordinary load, which would be a wait for the DMA as well
     asm volatile("" : "+v"(pgs));
 #pragma unroll
     for (int q = 0; q < QT; ++q) asm volatile("" : "+v"(sq[q].from), "+v"(sq[q].sinks), "+v"(sq[q].anc0), "+v"(sq[q].anc1));
@@ -383,6 +391,18 @@ __global__ __launch_bounds__(SCORE_WAVES * 64, 2) void span_score_kernel(SpanArg
     const int group = seq / p.key_wgs * 8 + ((int)blockIdx.x & 7), key_wg = seq % p.key_wgs;
     if (group >= p.groups) return;
     const int b = group / H, h = group - b * H;
+    // what does not depend on the row's length, beside the load of that
+    constexpr int PIECES = (QS * KS + NW - 1) / NW;
+    static_assert(QS * 32 <= NW * 64, "a thread per query");
+    u32x4_t piece[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int at = min(wave + i * NW, QS * KS - 1);
+        piece[i] = span_query_piece<DH>(p, b, h, min(at / KS, QTtot - 1), QTtot, col, 16 * (at % KS) + 8 * hl);
+    }
+    const bool counts = tid < p.n_scored;
+    const SpanStat stat = p.stats[((size_t)b * H + h) * Tq + min(tid, Tq - 1)];
+    const SpanNode node = span_node(p, tid);
     const SpanRow r = span_row<32>(p, b);
     if (!r.ok) return;                                      // reported by the attention
     const int units = p.key_wgs * NW, unit = key_wg * NW + wave;
@@ -406,13 +426,13 @@ __global__ __launch_bounds__(SCORE_WAVES * 64, 2) void span_score_kernel(SpanArg
     float *begin = reinterpret_cast<float *>(qs + QS * KS * 64);          // -M' of the queries; no weight at all: -infinity
     uint32_t *sees = reinterpret_cast<uint32_t *>(begin + QS * 32) + wave * 32;
     SpanQuery *sq = reinterpret_cast<SpanQuery *>(begin + QS * 32 + NW * 32);
-    for (int i = tid; i < QS * 32; i += NW * 64) {
-        const bool counts = i < p.n_scored;
-        const SpanStat s = p.stats[((size_t)b * H + h) * Tq + (counts ? i : 0)];
-        begin[i] = counts ? __builtin_amdgcn_logf(s.r) / p.c - s.m : -INFINITY;
-        sq[i] = span_query(p, r, counts ? i : p.T);
+    if (tid < QS * 32) {
+        begin[tid] = counts ? __builtin_amdgcn_logf(stat.r) / p.c - stat.m : -INFINITY;
+        sq[tid] = span_query(p, r, counts ? tid : T, node);
     }
-    for (int i = wave; i < QS * KS; i += NW) qs[i * 64 + lane] = span_query_piece<DH>(p, b, h, min(i / KS, QTtot - 1), QTtot, col, 16 * (i % KS) + 8 * hl);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+        if (wave + i * NW < QS * KS) qs[(wave + i * NW) * 64 + lane] = piece[i];
     __syncthreads();
     auto begins = [&](int q) {                              // in the accumulators' rows
         f32x16_t z;
