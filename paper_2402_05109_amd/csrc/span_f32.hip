@@ -38,6 +38,18 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
     const int group = seq / per * 8 + ((int)blockIdx.x & 7), j = seq % per;
     if (group >= p.groups) return;
     const int b = group / H, h = group - b * H, qg = j % QG, key_wg = j / QG;
+    // what does not depend on the row's length, beside the load of that
+    const float *q = reinterpret_cast<const float *>(p.q);
+    constexpr int PIECES = (QT * KS + NW - 1) / NW;
+    f32x4_t piece[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {                       // queries behind the last one: that one again, which nobody stores
+        const int at = min(wave + i * NW, QT * KS - 1), query = min((qg * QT + at / KS) * 16 + col, T - 1);
+        piece[i] = *reinterpret_cast<const f32x4_t *>(q + ((size_t)(b * T + query) * H + h) * DH + 16 * (at % KS) + 4 * g);
+    }
+    SpanNode node[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) node[t] = span_node(p, (qg * QT + t) * 16 + col);
     const int units = p.key_wgs * NW, unit = key_wg * NW + wave;
     const SpanRow r = span_row<16>(p, b);
     if (!r.ok) {                                            // uniform over the workgroup
@@ -45,18 +57,13 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
         return;
     }
     const int32_t *pt = p.table + (size_t)b * p.max_pages;
-    const float *q = reinterpret_cast<const float *>(p.q), *kpages = reinterpret_cast<const float *>(p.kpages), *vpages = reinterpret_cast<const float *>(p.vpages);
+    const float *kpages = reinterpret_cast<const float *>(p.kpages), *vpages = reinterpret_cast<const float *>(p.vpages);
     SpanQuery sq[QT];
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        const int query = (qg * QT + t) * 16 + col;
-        sq[t] = span_query(p, r, query);
-        for (int i = wave; i < KS; i += NW) {
-            f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-            if (query < T) v = *reinterpret_cast<const f32x4_t *>(q + ((size_t)(b * T + query) * H + h) * DH + 16 * i + 4 * g);
-            qs[(t * KS + i) * 64 + lane] = v;
-        }
-    }
+    for (int t = 0; t < QT; ++t) sq[t] = span_query(p, r, (qg * QT + t) * 16 + col, node[t]);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+        if (wave + i * NW < QT * KS) qs[(wave + i * NW) * 64 + lane] = piece[i];
     __syncthreads();
     f32x4_t o[QT][J * 4];                                   // [4 jj + e]: dims 64 jj + 16 g + 4 rr + e, rr the place in the vector
 #pragma unroll
