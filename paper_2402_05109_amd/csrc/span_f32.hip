@@ -70,6 +70,7 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
     for (int t = 0; t < QT; ++t)
 #pragma unroll
         for (int i = 0; i < J * 4; ++i) o[t][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const int tiles = min(QT, (T - qg * QT * 16 + 15) >> 4);
     float m_run[QT], l_run[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) { m_run[t] = -INFINITY; l_run[t] = 0.f; }
@@ -103,6 +104,7 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
         f32x4_t st[QT];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
+            if (t >= tiles) break;                           // uniform over the workgroup: no node in it
             f32x4_t s = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < KS; ++i) {                   // two chains: a product waits for the one before it in its own
@@ -133,6 +135,7 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
         }
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
+            if (t >= tiles) break;
             f32x4_t s = st[t];
             if (!whole) {
                 const uint32_t seen = span_seen(r, sq[t], slot0) >> (4 * g);
@@ -190,7 +193,7 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_f32_kernel(SpanArgs p)
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const int query = (qg * QT + t) * 16 + col;
-        if ((qg * QT + t) * 16 >= T) break;                  // uniform over the workgroup
+        if (t >= tiles) break;
         __syncthreads();                                     // maxima and sums are there; the tile before this one is stored
         float m_tot = -INFINITY;
 #pragma unroll
