@@ -49,7 +49,7 @@ static size_t span_lds_bytes(int Dh, int qt, int nw) {        // queries and til
 // Masked slots leave a weight of 0, and V of slots that no node of the row may see is replaced by 0: those hold what was never written or has been
 // evicted.  (Values that are held are finite: whatever writes the cache clamps them.)
 // The bytes of K and V bound it where rows or heads are many (16 rows of 64 nodes, 32 heads, 1570 slots: 411 MB in 75 us, 5.5 TB/s); where they are few, the way from a
-// length to a page number to K to a result (a node behind 1028 tokens: 9 us and 3 for the records, of which the bytes would be 2.6).
+// length to a page number to K to a result (a node behind 1028 tokens: 8 us and 3 for the records, of which the bytes would be 2.6).
 template <int DH, int QT, int NW, bool STREAM>
 __global__ __launch_bounds__(NW * 64, 2) void span_attn_kernel(SpanArgs p) {
     constexpr int KS = DH / 16, DT = DH / 32, TILE = KS + 2 * DT;    // KiB of a K and V tile

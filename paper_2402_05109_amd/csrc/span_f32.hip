@@ -331,8 +331,8 @@ int span_f32_max_dynamic_lds() {
 
 int launch_span_f32(hydra_ctx *c, hipStream_t s, SpanArgs a, int slots, int units_max) {
     const int T = a.T, Dh = c->m.head_dim, pages = ceil_div(slots, 16) + 2, hb = a.groups * ceil_div(T, 16 * SPAN32_QT);
-    // two pages of a wave cost about what a second kernel does (16 nodes, 4 heads of 64: a window of 100 9.5 us against 10.3; 400 tokens 9.8, with four pages of a wave
-    // 13.7).  More workgroups than compute units leave more records only (2 rows of 64 nodes behind 2000 tokens, 16 heads of 128: 43 us instead of 37)
+    // two pages of a wave cost less than a second kernel (16 nodes, 4 heads of 64: a window of 100 7.8 us against 9.2; 330 tokens 8.8, by one workgroup with three pages of a
+    // wave 9.9).  More workgroups than compute units leave more records only (2 rows of 64 nodes behind 2000 tokens, 16 heads of 128: 43 us instead of 37)
     a.key_wgs = pages <= 2 * SPAN32_WAVES ? 1 : std::max(1, std::min({ceil_div(pages, SPAN32_WAVES), std::max(1, 256 / hb), units_max}));
     const dim3 grid(ceil_div(a.groups, 8) * 8 * ceil_div(T, 16 * SPAN32_QT) * a.key_wgs), block(SPAN32_WAVES * 64);
     if (Dh == 128) hipLaunchKernelGGL(span_f32_kernel<128>, grid, block, 0, s, a);
