@@ -229,6 +229,46 @@ def test_another_layer_another_stream_and_a_graph(f32):
     assert c.read_flags() == 0
 
 
+@pytest.mark.parametrize("f32", [False, True])
+def test_two_calls_at_once(f32):
+    """Two streams, one context and cache, a workspace each: attention with scores beside attention without and log probabilities."""
+    H, Dh, T, L, V = 4, 128, 40, 3000, 5000
+    parent = tree_parent(T)
+    c = context(H, Dh, 1, parent, max_pos=L + T + 1, f32=f32, vocab=V)
+    g = torch.Generator().manual_seed(9)
+    kv = torch.randn(1, 1, L + T, 2, H, Dh, generator=g).to(dtype_of(f32))
+    kvd = cache(c, H, Dh, kv, masks(parent, [L], [0], 0, 0, L + T), f32)
+    q = torch.randn(1, T, H, Dh, generator=g).to(dtype_of(f32)).to(DEV)
+    n, x = torch.tensor([L], dtype=torch.int32, device=DEV), torch.randn(1, T, V, generator=g).to(DEV)
+    ws = [torch.empty(c.workspace_bytes(1), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    span = [hb.KVSpan(kvd, n_sinks=3, window=1500), hb.KVSpan(kvd)]
+
+    def first(out, score):
+        span[0].score, span[0].n_scored = score, 7
+        c.tree_attention_span(1, 0, ws[0], q, n, span[0], out)
+
+    def second(out, lps, ids):
+        c.tree_attention_span(1, 0, ws[1], q, n, span[1], out)
+        c.hydra_token_logprobs(1, ws[1], x, None, 1.0, 3, top_ids=ids, top_logprobs=lps)
+
+    def outputs():
+        return (torch.empty_like(q), torch.zeros(1, 1, H, 16 * kvd.max_pages, device=DEV)), (torch.empty_like(q), torch.empty(1, T, 3, device=DEV), torch.empty(1, T, 3, dtype=torch.int32, device=DEV))
+    want = outputs()
+    first(*want[0]); second(*want[1])
+    got = [outputs() for _ in range(5)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for a, b in got:
+        with torch.cuda.stream(streams[0]):
+            first(*a)
+        with torch.cuda.stream(streams[1]):
+            second(*b)
+    torch.cuda.synchronize()
+    for a, b in got:
+        assert all(torch.equal(u, v) for u, v in zip(a + b, want[0] + want[1]))
+    assert c.read_flags() == 0
+
+
 @pytest.mark.parametrize("shape", [(1, 1, 2), (3, 1, 2), (2, 1, 1), (2, 1, 4), (2, 0, 2)])
 def test_scores_of_another_model_are_refused(shape):
     c = context(2, 64, 1, [-1], NL=2, max_pos=64)
