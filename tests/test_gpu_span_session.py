@@ -312,3 +312,35 @@ def test_a_prompt_that_is_broken_off_under_a_bound():
         t.prefill(p[:, :64], lambda *a: None)
         assert torch.equal(s.h_last, t.h_last) and torch.equal(s.root, t.root)
         assert s.generate(12)[0] == t.generate(12)[0] and s.main.read_flags() == 0
+
+
+@pytest.mark.parametrize("cfg", [F32, HALF])
+def test_a_windowed_step_replays_from_a_graph(cfg):
+    """Replay by replay the text of an eager session, with eager work between the replays.  The hint sizes grids, so sums may be taken in another order: in 16 bits a result of attention
+    then rounds to its neighbour (2^-11 of it) in each of two layers, and what follows carries it on (twice that); in fp32 sums of up to 24 + 3 + 16 terms by 2^-24 each, twice."""
+    weights = make_weights(cfg)
+    p = torch.stack([uniform_tokens(cfg.seed + i, 0, 40, cfg.V) for i in range(2)]).to(torch.int32)
+    a, b = (gpu_session(cfg, TREE, 2, 256, weights, window=24, sinks=3, want_logits=True) for _ in range(2))
+    a.prefill(p)
+    b.prefill(p)
+    b.host_len += 120                                                        # frozen into the graph: a bound for every replay
+    hint, state = b.host_len, [t.clone() for t in (b.seq_len, b.h_last, b.root)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b.step()
+    torch.cuda.current_stream().wait_stream(side)
+    for t, s in zip((b.seq_len, b.h_last, b.root), state):
+        t.copy_(s)
+    b.host_len = hint
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.step()
+    for _ in range(6):
+        graph.replay()
+        a.step()
+        assert torch.equal(a.seq_len, b.seq_len) and torch.equal(a.root, b.root) and torch.equal(a.out().n_acc, b.out().n_acc)
+        assert max_rel(to_np(b.h_last), to_np(a.h_last)) <= (1e-5 if cfg is F32 else 2e-3)
+        b.logprobs(k=2)
+        torch.cuda.synchronize()
+    assert a.main.read_flags() == 0 and b.main.read_flags() == 0
