@@ -179,8 +179,8 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LogprobArgs a) {
     const int row = (int)blockIdx.x / a.pieces, pc = (int)blockIdx.x - row * a.pieces, from = pc * a.piece, n = min(a.piece, a.V - from);
     const float *x0 = a.logits + (size_t)row * a.V + from;
     const float k2 = a.inv_tau * 1.44269504f;
-    // No load is behind a condition: a group behind the last one reads the last four logits and holds none of them, the group that the end cuts reads them too
-    // and leaves out those that the one before it has.
+    // Logits pass the caches by (1024 rows x 32000, k = 0 / 5 / 32: 25.8 / 29.4 / 35.5 us; through them 28.5 / 32.3 / 37.4).  No load is behind a condition: a group
+    // behind the last one reads the last four logits and holds none of them, the group that the end cuts reads them too and leaves out those that the one before it has.
     auto place = [&](int at0, int i) { return at0 + (i * LP_THREADS + tid) * 4; };
     auto load = [&](float (&x)[LP_PER], int at0) {
         if (n < 4) {                                         // uniform: a vocabulary of two or three tokens, or what is left of one
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LogprobArgs a) {
         }
 #pragma unroll
         for (int i = 0; i < LP_PER / 4; ++i) {
-            const f4u v = *reinterpret_cast<const f4u *>(x0 + min(place(at0, i), n - 4));
+            const f4u v = __builtin_nontemporal_load(reinterpret_cast<const f4u *>(x0 + min(place(at0, i), n - 4)));
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[4 * i + e] = v[e];
         }
