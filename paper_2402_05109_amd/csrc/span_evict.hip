@@ -223,9 +223,9 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
 // The contents follow.  A workgroup takes 64 dims of K or V of one (head, row, layer), a wave one page of targets at a time, from the last one down.  A source
 // lies at or below its target, so the pages of one turn have to be read before any of them is written, and those of later turns lie below: their loads
 // are under way while this turn's pages are stored.  Places of a page that no token moves to keep what they hold.
-// Bytes bound it: 8 layers of 32 heads of 128, 2048 of 2560 tokens: 0.6 GB in 133 us, 4.5 TB/s.  Of 16003 tokens (4 layers of 40 heads) the 2048 that stay are an eighth, but
-// a page's K holds 16 bytes of each token beside each other, and V two: with whole lines of 128 bytes that is 1.1 GB, in 253 us.
-enum { EV_WAVES = 16, EV_GROUP = 2, EV_PAGE_LDS = 2048 };
+// Bytes bound it: 8 layers of 32 heads of 128, 2048 of 2560 tokens: 0.6 GB in 124 us, 4.9 TB/s.  Of 16003 tokens (4 layers of 40 heads) the 2048 that stay are an eighth, but
+// a page's K holds 16 bytes of each token beside each other, and V two: with whole lines of 128 bytes that is 1.1 GB, in 242 us.
+enum { EV_WAVES = 16, EV_GROUP = 2, EV_ROW_LDS = 272, EV_PAGE_LDS = 8 * EV_ROW_LDS };
 struct EvictPlan { int to, slot, page; };                   // of a page of targets: its number, and for place lane % 16 the slot that moves there (-1: none) and its page
 struct EvictMove {
     const int32_t *kept, *pt, *dt;
@@ -241,7 +241,8 @@ struct EvictMove {
     __device__ __forceinline__ void look_up(EvictPlan &p) const { p.page = p.slot >= 0 ? pt[p.slot >> 4] : p.to; }
 };
 
-// fp32 rows, and 16-bit K (runs of 8 dims, [dim / 8][token]): they move as they lie, 16 bytes a lane.  block(page): the page's 64 dims
+// fp32 rows, and 16-bit K (runs of 8 dims, [dim / 8][token]): they move as they lie, 16 bytes a lane.  block(page): the page's 64 dims.  They pass the caches by
+// (13B, 2048 of 16003 tokens 277 -> 267 us in all, fp32 132 -> 126).
 template <bool BF, class Block>
 __device__ __forceinline__ void evict_move_rows(const EvictMove &m, int Dh, int last, int lane, int wave, Block block) {
     constexpr int N = BF ? 2 : 4;
@@ -253,7 +254,7 @@ __device__ __forceinline__ void evict_move_rows(const EvictMove &m, int Dh, int 
     auto load = [&](const EvictPlan &p, u32x4_t (&x)[N]) {
         const int tok = p.slot >= 0 ? p.slot & 15 : place;
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = BF ? *at(p.page, tok, i) : *at(__shfl(p.page, i * 4 + sub, 64), __shfl(tok, i * 4 + sub, 64), i);
+        for (int i = 0; i < N; ++i) x[i] = __builtin_nontemporal_load(BF ? at(p.page, tok, i) : at(__shfl(p.page, i * 4 + sub, 64), __shfl(tok, i * 4 + sub, 64), i));
     };
     EvictPlan now = m.slots(last - wave, lane), next = m.slots(last - wave - EV_WAVES, lane), after = m.slots(last - wave - 2 * EV_WAVES, lane);
     m.look_up(now);
@@ -273,15 +274,16 @@ __device__ __forceinline__ void evict_move_rows(const EvictMove &m, int Dh, int 
         __syncthreads();
         if (live) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) *at(to, BF ? place : i * 4 + sub, i) = x[i];
+            for (int i = 0; i < N; ++i) __builtin_nontemporal_store(x[i], at(to, BF ? place : i * 4 + sub, i));
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = y[i];
     }
 }
 
-// 16-bit V lies by dim: a lane holds the 16 tokens of one dim of a source page, which go to LDS as [dword][lane] (a dword: two tokens); since every lane moves the same tokens, one
-// is picked by an offset that the wave shares, without bank conflicts.  Picked from registers, by a register number that the wave shares, a page of targets took
+// 16-bit V lies by dim: the 16 tokens of the 64 dims of a source page go to LDS as [dword][dim] (a dword: two tokens), loaded as whole lines, half a dim a lane; since every lane moves
+// the same tokens, of one dim, one is picked by an offset that the wave shares, without bank conflicts.  (Neighbouring waves read the pages at their ends twice: through the caches;
+// past them 7B took 165 us instead of 154 in all.)  Picked from registers, by a register number that the wave shares, a page of targets took
 // twice as long as its loads and stores (7B, 8 layers, 2048 of 2560 tokens: 268 us).
 template <class Block>
 __device__ __forceinline__ void evict_move_v(const EvictMove &m, int last, int lane, int wave, char *lds, Block block) {
@@ -295,9 +297,9 @@ __device__ __forceinline__ void evict_move_v(const EvictMove &m, int last, int l
 #pragma unroll
         for (int g = 0; g < EV_GROUP; ++g)
             if (rest) {                                      // wave-uniform
-                const u32x4_t *from = reinterpret_cast<const u32x4_t *>(block(__builtin_amdgcn_readlane(now.page, __builtin_ctz(rest)))) + lane * 2;
+                const u32x4_t *from = reinterpret_cast<const u32x4_t *>(block(__builtin_amdgcn_readlane(now.page, __builtin_ctz(rest)))) + lane;
                 s[g][0] = from[0];
-                s[g][1] = from[1];
+                s[g][1] = from[64];
                 rest &= rest - 1u;
             }
     };
@@ -305,7 +307,7 @@ __device__ __forceinline__ void evict_move_v(const EvictMove &m, int last, int l
         const int tok = now.slot >= 0 ? now.slot & 15 : place, before = __shfl_up(now.page, 1, 64);
         rest = (uint32_t)__ballot(lane < 16 && (lane == 0 || now.page != before));
         const int nth = __popc(rest & ((2u << place) - 1u)) - 1, at = v_perm(tok);
-        pick = (nth / EV_GROUP) << 16 | (nth % EV_GROUP * EV_PAGE_LDS + (at >> 1) * 256 + (at & 1) * 2);
+        pick = (nth / EV_GROUP) << 16 | (nth % EV_GROUP * EV_PAGE_LDS + (at >> 1) * EV_ROW_LDS + (at & 1) * 2);
         fetch();
     };
     now = m.slots(last - wave, lane);
@@ -324,7 +326,8 @@ __device__ __forceinline__ void evict_move_v(const EvictMove &m, int last, int l
 #pragma unroll
                 for (int g = 0; g < EV_GROUP; ++g)
 #pragma unroll
-                    for (int d = 0; d < 8; ++d) *reinterpret_cast<uint32_t *>(lds + g * EV_PAGE_LDS + d * 256 + lane * 4) = s[g][d >> 2][d & 3];
+                    for (int d = 0; d < 8; ++d)
+                        *reinterpret_cast<uint32_t *>(lds + g * EV_PAGE_LDS + ((lane & 1) * 4 + (d & 3)) * EV_ROW_LDS + ((lane >> 1) + (d >> 2) * 32) * 4) = s[g][d >> 2][d & 3];
                 const bool more = rest != 0;
                 if (more) fetch();
 #pragma unroll
