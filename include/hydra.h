@@ -236,8 +236,8 @@ int hydra_bind_weights(hydra_ctx *ctx, void *stream, void *arena, int table_slot
 int hydra_load_tensor(hydra_ctx *ctx, void *stream, int kind, int index, int sub,
                       const void *src);
 
-/* Workspace bytes needed by any call with batch B (256-byte aligned device
- * memory, contents irrelevant between calls). */
+/* Workspace bytes needed by any call with a batch of up to B (256-byte aligned
+ * device memory, contents irrelevant between calls). */
 size_t hydra_workspace_bytes(const hydra_ctx *ctx, int B);
 
 /* Device-side flags raised by kernels of this context since the last call of

@@ -309,7 +309,9 @@ size_t hydra_weights_bytes(const hydra_ctx *c) { return c ? c->arena_bytes : 0; 
 int hydra_tree_depth(const hydra_ctx *c) { return c ? c->tree.max_depth : -1; }
 size_t hydra_workspace_bytes(const hydra_ctx *c, int B) {
     if (!c || B < 1 || B > c->max_batch) return 0;
-    return ws_layout(c, B).total;
+    size_t most = 0;                                        // split plans and records of fewer rows can take more
+    for (int b = 1; b <= B; ++b) most = std::max(most, ws_layout(c, b).total);
+    return most;
 }
 
 int hydra_bind_weights(hydra_ctx *c, void *stream, void *arena, int table_slot) {

@@ -73,6 +73,15 @@ def test_workspace_has_room_for_records_and_statistics():
     assert h.workspace_bytes(16) >= 16 * 128 * 100003 * 4 + 16 * 2 * 128 * 8
 
 
+@pytest.mark.parametrize("dtype", [hb.HYDRA_BF16, hb.HYDRA_F32])
+@pytest.mark.parametrize("heads, T, vocab", [(2, 1, 64), (2, 59, 262147), (4, 16, 100003), (8, 128, 32000)])
+def test_a_workspace_serves_fewer_rows(heads, T, vocab, dtype):
+    """Plans differ by the number of rows; a session prefills some of its rows in the workspace of all."""
+    h = hb.Hydra(d=64 * heads, n_layers=1, n_heads=heads, head_dim=64, ffn=128, vocab=vocab, max_pos=256, dtype=dtype, max_batch=200, parent=[-1] + list(range(T - 1)))
+    sizes = [h.workspace_bytes(B) for B in range(1, 201)]
+    assert sizes == sorted(sizes)
+
+
 # ---- what is checked behind the weights: on a device, with a bare context, still before anything is launched
 BAD_SPANS = [
     (dict(n_sinks=-1), hb.E_INVALID_ARG), (dict(window=-1), hb.E_INVALID_ARG), (dict(span_hint=-1), hb.E_INVALID_ARG), (dict(n_scored=-1), hb.E_INVALID_ARG),
