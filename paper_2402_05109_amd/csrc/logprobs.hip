@@ -367,13 +367,13 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LogprobArgs a)
     }
 }
 
-// Portions of a row that a workgroup takes: one while those are up to 768 in all, then as many as that needs.  A workgroup's fixed part (bounds, lists, ranks) is worth
-// about a portion where tokens are wanted, and four of them fit a compute unit.  us, k = 0 / 5 / 32: 128 rows x 100003 15.8 / 26.0 / 36.9 with a portion, 16.2 / 23.2 / 31.1
-// with two; 1024 rows x 32000 30.4 / 39.9 / 50.7 with two, 28.4 / 32.5 / 37.6 with all four; 256 rows x 131072 29.9 / 45.5 / 61.9 with one, 31.9 / 38.2 / 44.3 with four.  One row x 32000
-// takes 6.5 / 12 / 16 with pieces of 8192, 4096, 2048 or 1024.
+// Portions of a row that a workgroup takes: one while those are up to 768 in all, then as many as that needs; from 384 rows on all of a row, which then needs no second
+// kernel.  A workgroup's fixed part (bounds, lists, ranks) is worth about a portion where tokens are wanted, and four of them fit a compute unit.  us, k = 0 / 5 / 32:
+// 128 rows x 100003 15.3 / 24.6 / 35.5 with a portion, 16.2 / 21.9 / 29.8 with two; 256 rows x 131072 28.0 / 42.1 / 58.9 with one, 27.9 / 33.3 / 41.5 with four; 512 rows x 32000
+// 18.1 / 23.1 / 29.9 with two, 15.5 / 20.7 / 27.3 with all four.  One row x 32000 takes 6.6 / 12 / 16 with pieces of 8192, 4096, 2048 or 1024.
 static int logprob_pieces(int V, int rows) {
     const int portions = ceil_div(V, LP_THREADS * LP_PER);
-    const int64_t per = std::max<int64_t>({1, ceil_div(portions, LP_MAX_PIECES), (int64_t)portions * rows / 768});
+    const int64_t per = rows >= 384 ? portions : std::max<int64_t>({1, ceil_div(portions, LP_MAX_PIECES), (int64_t)portions * rows / 768});
     return ceil_div(portions, (int)std::min<int64_t>(per, portions));
 }
 size_t logprob_scratch_bytes(const hydra_ctx *c, int rows) { return (size_t)rows * logprob_pieces(c->m.vocab, rows) * lp_record_floats(HYDRA_MAX_TOPK) * 4; }
