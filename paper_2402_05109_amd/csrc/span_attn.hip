@@ -15,8 +15,8 @@ namespace hydra {
 
 static constexpr float LOG2E = 1.44269504f;
 
-// 16 bytes of a query: dims d0 .. d0 + 7 of column `col` of a query tile (queries past the last one: that one, or whatever the packed buffer holds; nobody
-// stores their result)
+// 16 bytes of a query: dims d0 .. d0 + 7 of column `col` of a query tile.  Queries past the last one: that one, or whatever the packed buffer holds, of which nobody writes those:
+// they may be no numbers, and whoever adds over queries leaves them out by a select.
 template <int DH>
 __device__ __forceinline__ u32x4_t span_query_piece(const SpanArgs &p, int b, int h, int qtile, int QTtot, int col, int d0) {
     const size_t packed = ((((size_t)b * p.H + h) * QTtot + qtile) * (DH / 16) + (d0 >> 4)) * 64 + ((d0 >> 3) & 1) * 32 + col;
@@ -374,6 +374,7 @@ __global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs p, int blocks)
 
 // The weights that every slot receives from nodes 0 .. n_scored - 1, behind the attention that has left each query's maximum and sum:
 //     score[s] += sum_n 2^((z_ns - M_n) c) / l_n = sum_n 2^((z_ns - M'_n) c),   M' = M + log2(l) / c
+// A query that does not count begins with -infinity, which alone is no guard (-infinity + NaN): its weights are left out of the sum.
 // Queries are the rows of S = Q K^T here, so that a lane holds one slot and adds over its registers, and -M' is what the accumulators of the product begin with: a score costs a
 // multiplication, an exponential and an addition.  A wave takes 32-key tiles in turn, the next one's K under way, from the last tile down: those are what the attention has
 // read last, and the masked ones are then no wave's last (a row of 64 behind 4000 tokens, 32 heads 30.5 us against 32.2 the other way round); no two waves hold the same slot, so no sum depends
@@ -469,7 +470,10 @@ __global__ __launch_bounds__(SCORE_WAVES * 64, 2) void span_score_kernel(SpanArg
                 const f32x16_t z = product(at + q * KS * 64, start[q]);
                 float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int v = 0; v < 16; ++v) part[v & 3] += __builtin_amdgcn_exp2f(z[v] * p.c);
+                for (int v = 0; v < 16; ++v) {
+                    const float w = __builtin_amdgcn_exp2f(z[v] * p.c);
+                    part[v & 3] += q + 1 == QS && start[q][v] == -INFINITY ? 0.f : w;        // the last tile alone has queries that do not count
+                }
                 sum += (part[0] + part[1]) + (part[2] + part[3]);
                 if (q & 1) __builtin_amdgcn_sched_barrier(0);          // four tiles at once do not fit the registers
             }
@@ -575,13 +579,13 @@ int launch_span_attention(hydra_ctx *c, hipStream_t s, int B, int layer, const v
     if (a.key_wgs > 1)
         if (int rc = launch_span_merge(c, s, a, slots)) return rc;
     if (!a.score || a.z) return HYDRA_OK;
-    const int QS = a.n_scored <= 32 ? 1 : a.n_scored <= 64 ? 2 : 4;
+    const int QS = std::max(1, ceil_div(a.n_scored, 32));
     // (twice as many workgroups, with the queries in LDS once more each: a row of 128, 40 heads (16000) 141 us against 134)
     a.key_wgs = std::max(1, std::min(ceil_div(tiles, SCORE_WAVES), std::max(1, 256 / (H * B))));
     const dim3 sgrid(ceil_div(H * B, 8) * 8 * a.key_wgs), sblock(SCORE_WAVES * 64);
     const size_t slds = (size_t)QS * ((Dh / 16) * 1024 + 32 * (4 + sizeof(SpanQuery))) + SCORE_WAVES * 128;
 #define LAUNCH(DHv, QSv) if (Dh == DHv && QS == QSv) hipLaunchKernelGGL((span_score_kernel<DHv, QSv>), sgrid, sblock, slds, s, a);
-    LAUNCH(128, 1) LAUNCH(128, 2) LAUNCH(128, 4) LAUNCH(64, 1) LAUNCH(64, 2) LAUNCH(64, 4)
+    LAUNCH(128, 1) LAUNCH(128, 2) LAUNCH(128, 3) LAUNCH(128, 4) LAUNCH(64, 1) LAUNCH(64, 2) LAUNCH(64, 3) LAUNCH(64, 4)
 #undef LAUNCH
     HYDRA_LAUNCH_CHECK("span_score_kernel");
     return HYDRA_OK;
