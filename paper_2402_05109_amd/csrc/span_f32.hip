@@ -297,7 +297,8 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_score_f32_kernel(SpanA
         page = page_id(u + 2 * units);
         float sum = 0.f;
         for (int t = 0; t < QS; ++t) {
-            f32x4_t z = *reinterpret_cast<const f32x4_t *>(start + t * 16 + 4 * g), z1 = {0.f, 0.f, 0.f, 0.f};
+            const f32x4_t begin = *reinterpret_cast<const f32x4_t *>(start + t * 16 + 4 * g);
+            f32x4_t z = begin, z1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < KS; ++i) {                   // two chains: a product waits for the one before it in its own
                 const f32x4_t qv = qs[(t * KS + i) * 64 + lane];
@@ -313,7 +314,10 @@ __global__ __launch_bounds__(SPAN32_WAVES * 64) void span_score_f32_kernel(SpanA
                 for (int e = 0; e < 4; ++e) z[e] = (span_seen(r, sq[t * 16 + 4 * g + e], slot0) >> col) & 1u ? z[e] : -INFINITY;
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(z[e] * p.c);
+            for (int e = 0; e < 4; ++e) {
+                const float w = __builtin_amdgcn_exp2f(z[e] * p.c);
+                sum += begin[e] == -INFINITY ? 0.f : w;      // of a query that does not count, whose products may be infinite or no numbers
+            }
         }
         sum = over_keys(sum, [](float a, float c) { return a + c; });
         if (mine) row[slot] = before + sum;

@@ -8,6 +8,8 @@ import torch
 
 from gpu_util import gpu_session, to_np
 from helpers import make_weights
+from paper_2402_05109_amd import binding as hb
+from span_util import DEV, attention_reference, cache, context, dtype_of, masks, tree_parent
 from synth import uniform_tokens
 from test_gpu_span_session import F32, HALF, TREE, Decoder
 
@@ -72,6 +74,40 @@ def test_whatever_the_workspace_held(T, chunk, cfg):
     s.seq_len.fill_(L + T)
     check_scores(cfg, s, decs)
     assert s.main.read_flags() == 0
+
+
+@pytest.mark.parametrize("f32, key", [(False, False), (True, False), (True, True)])     # (what writes a 16-bit cache clamps infinities)
+@pytest.mark.parametrize("T, n_scored", [(5, 3), (16, 15), (40, 33), (64, 50), (128, 96), (100, 70)])
+def test_nodes_that_do_not_count_stay_out_of_the_sums(T, n_scored, key, f32):
+    """Queries behind the counted ones that are no numbers; or (fp32) a K of -infinity, which gives the counted nodes' scores of -infinity, so weights of 0, and the others +infinity: every
+    slot's sum is that of the counted nodes alone."""
+    H, Dh, L, at, dim = 2, 64, 100, 40, 7
+    parent = tree_parent(T)
+    g = torch.Generator().manual_seed(T)
+    c = context(H, Dh, 1, parent, max_pos=300, f32=f32)
+    kv = torch.randn(1, 1, L + T, 2, H, Dh, generator=g).to(dtype_of(f32))
+    q = torch.randn(1, T, H, Dh, generator=g).to(dtype_of(f32))
+    m = masks(parent, [L], [0], 0, 0, L + T)
+    seen = m.clone()
+    if key:
+        q[:, :n_scored, :, dim] = q[:, :n_scored, :, dim].abs() + 0.1
+        q[:, n_scored:, :, dim] = -q[:, n_scored:, :, dim].abs() - 0.1
+        kv[0, 0, at, 0, :, dim] = -math.inf
+        seen[:, :, at] = False                                               # a weight of 0
+    kvd = cache(c, H, Dh, kv, m, f32)
+    given = q.clone()
+    if not key:
+        given[:, n_scored:] = math.nan
+    score0 = torch.rand(1, 1, H, kvd.max_pages * 16, generator=g).to(DEV)
+    score, out = score0.clone(), torch.empty(1, T, H, Dh, dtype=dtype_of(f32), device=DEV)
+    c.tree_attention_span(1, 0, c.ws, given.to(DEV), torch.tensor([L], dtype=torch.int32, device=DEV), hb.KVSpan(kvd, score=score, n_scored=n_scored), out)
+    plain = kv[0].clone()
+    plain[:, at, 0, :, dim] = 0.0
+    ref, tol, add, add_tol = attention_reference(q, plain if key else kv[0], seen, f32, n_scored)
+    assert ((out.double() - ref).abs() <= tol)[:, :n_scored].all()
+    want = torch.where(torch.arange(L + T, device=DEV) < L, score0[0, :, :, :L + T].double(), 0.0) + add
+    assert ((score[0, :, :, :L + T].double() - want).abs() <= add_tol + 2.0 ** -24 * want).all()
+    assert c.read_flags() == 0
 
 
 def choose(score, first, L, sinks, recent, keep):
