@@ -74,11 +74,13 @@ __device__ __forceinline__ float lp_finish(const LogprobArgs &a, int row, const 
     if (a.rank) a.rank[row] = tok < 0 ? -1 : above;
     return lnz;
 }
-// the row's token and its logit: -1 = none, others outside the vocabulary are reported and taken as 0
+// the row's token and its logit (a NaN: -infinity, as in every order; the row's sums are no numbers then, nor is the log probability): -1 = none, others outside the vocabulary are
+// reported and taken as 0
 __device__ __forceinline__ int lp_token(const LogprobArgs &a, int row, float &given) {
     int tok = a.tokens ? a.tokens[row] : -1;
     if (tok != -1 && (tok < 0 || tok >= a.V)) { atomicOr(a.flags, FLAG_BAD_TOKEN); tok = 0; }
     given = tok >= 0 ? a.logits[(size_t)row * a.V + tok] : INFINITY;
+    if (__builtin_isnan(given)) given = -INFINITY;
     return tok;
 }
 

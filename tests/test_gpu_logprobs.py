@@ -183,3 +183,21 @@ def test_on_another_stream_and_in_a_graph():
         assert all((a - b).abs().max() <= 1e-4 for a, b in zip((outs[0], outs[2], outs[4]), (want[0], want[2], want[4])))
         x.copy_(x2)
     assert c.read_flags() == 0
+
+
+@pytest.mark.parametrize("V", [3, 900, 40000])
+@pytest.mark.parametrize("k", [0, 3])
+def test_a_given_token_whose_logit_is_no_number(V, k):
+    """It ranks as one of -infinity does, whatever the sign of the NaN: behind every token over that."""
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn(4, 2, V, generator=g)
+    tok = torch.randint(0, V, (4, 2), generator=g)
+    tok[0], tok[1] = 0, V - 1
+    x.scatter_(2, tok[..., None], math.nan)
+    x[1] = torch.where(torch.isnan(x[1]), -x[1], x[1])
+    x[2, :, ::2] = torch.where(torch.isnan(x[2, :, ::2]), x[2, :, ::2], -math.inf)
+    x[3, 1] = math.nan                                                        # nothing over -infinity: all rank first
+    o = call(x, tok, k=k)
+    want = (x.nan_to_num(nan=-math.inf, posinf=math.inf, neginf=-math.inf) > -math.inf).sum(dim=-1)
+    assert torch.equal(o["rank"].cpu().long(), want) and want[3, 1] == 0
+    assert torch.isnan(o["logprob"]).all() and torch.isnan(o["entropy"]).all() and o["flags"] == 0
