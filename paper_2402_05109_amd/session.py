@@ -408,8 +408,8 @@ class Session:
         ok = self._lists[4]
         lo = None
         if self.span is not None:                     # what no node sees any more goes back first, and stays without pages
-            lo = self._lo
-            self.main.hydra_pages_release_span(B, self.pages, self.seq_len, self.span, lo)
+            lo = self._lo                             # (of every row: a cut empties pages of those too that take no part in a prompt)
+            self.main.hydra_pages_release_span(self.B, self.pages, self.seq_len, self.span, lo)
         self.main.hydra_pages_reserve(B, self._pages_ws, self.pages, lo, self.seq_len, T, ok)
         if self.kv8 is not None:
             # never short of pages: no tree has more than _T_max nodes (_check_nodes), so a row holds at most a ring of them, and fork() takes
