@@ -349,7 +349,9 @@ class Session:
                 raise RuntimeError(f"the pool of {self.n_pages} pages is exhausted: no room for the kept tokens of rows that share pages")
             m.hydra_kv_evict(B, self.seq_len, self.span, keep, recent, spare, self._kept, self._evicted, dst_table=self._dst.page_table)
             done = self._evicted[:, None] > 0
-            m.hydra_pages_release(B, self.pages, None, torch.where(self._evicted > 0, zero, zero + 16 * self.max_pages))
+            whole = zero + 16 * self.max_pages
+            m.hydra_pages_release(B, self.pages, None, torch.where(self._evicted > 0, zero, whole))
+            m.hydra_pages_release(B, self._dst, None, torch.where(self._evicted > 0, whole, zero))        # of rows that had to stay whole
             self.page_table.copy_(torch.where(done, self._dst.page_table, self.page_table))
             self._dst.page_table.fill_(-1)
         self._growth = 0

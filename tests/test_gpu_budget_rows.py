@@ -48,3 +48,31 @@ def test_a_prompt_beside_rows_that_are_cut():
     assert torch.equal(s.root[0], alone.root[0]) and (s.h_last[0] - alone.h_last[0]).abs().max() <= 1e-4 * alone.h_last[0].abs().max()
     s._drop_scratch()
     assert [int((s.page_table[b] >= 0).sum()) for b in range(4)] == [16, 4, 4, 4]
+
+
+def test_a_row_that_cannot_be_cut_gives_back_the_pages_reserved_for_it():
+    """Rows that share pages are due to be cut; one has an entry that names no page: it stays whole and is flagged, and no page is left that no row names."""
+    weights = make_weights(F32)
+    s = gpu_session(F32, TREE, 4, 400, weights, budget=(64, 24, 0), prefill_chunk=32, pool_pages=80)
+    s.prefill(text(0, 64).reshape(1, 64))
+    s.fork([0, 0, 0, 0])
+    for _ in range(2):
+        s.step()
+    assert s.main.read_flags() == 0 and s._shared
+    s._drop_scratch()
+    keep, s._trim = s._trim, lambda grown: None
+    s.step()
+    s._drop_scratch()
+    lens = (s.seq_len - s.span.first).tolist()
+    assert min(lens) > 64
+    bad = int(s.span.first[2]) // 16 + 1
+    page = int(s.page_table[2, bad])
+    s.page_table[2, bad] = s.n_pages + 3
+    s.pages.ref[page] -= 1
+    s.fork([0, 1, 2, 0])                                                     # rows 0 and 3 share pages
+    s.main.read_flags()
+    assert rows_and_counts_agree(s)
+    keep(1)
+    assert s.main.read_flags() == 64 and (s.seq_len - s.span.first).tolist() == [64, 64, lens[2], 64]
+    assert rows_and_counts_agree(s)
+    assert (s._dst.page_table == -1).all()
