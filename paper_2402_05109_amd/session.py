@@ -335,26 +335,48 @@ class Session:
         self._growth += grown
         if self._growth <= slack - slack // 2 or max(self.host_len, self._other_len) <= keep + slack // 2:
             return
-        m, B, spare = self.main, self.B, slack // 2
         self.span.span_hint = 0 if self.host_len == 0 else max(self.host_len, self._other_len)
-        if not (self.pool and self._shared):
-            m.hydra_kv_evict(B, self.seq_len, self.span, keep, recent, spare, self._kept, self._evicted)
+        if self.pool and self._shared:
+            self._cut_shared(keep, recent, slack // 2)
         else:
-            # rows that may share pages go to pages of their own; what they held goes back, where no other row has it
-            cut = (self.seq_len - self.span.first) > keep + spare
-            zero = torch.zeros_like(self.seq_len)
-            m.hydra_pages_reserve(B, self._pages_ws, self._dst, torch.where(cut, self.seq_len - keep, zero), torch.where(cut, self.seq_len, zero), 0, self._lists[4])
-            if not bool(self._lists[4][:B].all()):
-                m.hydra_pages_release(B, self._dst, None, zero)
-                raise RuntimeError(f"the pool of {self.n_pages} pages is exhausted: no room for the kept tokens of rows that share pages")
-            m.hydra_kv_evict(B, self.seq_len, self.span, keep, recent, spare, self._kept, self._evicted, dst_table=self._dst.page_table)
-            done = self._evicted[:, None] > 0
-            whole = zero + 16 * self.max_pages
-            m.hydra_pages_release(B, self.pages, None, torch.where(self._evicted > 0, zero, whole))
-            m.hydra_pages_release(B, self._dst, None, torch.where(self._evicted > 0, whole, zero))        # of rows that had to stay whole
-            self.page_table.copy_(torch.where(done, self._dst.page_table, self.page_table))
-            self._dst.page_table.fill_(-1)
+            self.main.hydra_kv_evict(self.B, self.seq_len, self.span, keep, recent, slack // 2, self._kept, self._evicted)
         self._growth = 0
+
+    def _cut_shared(self, keep: int, recent: int, spare: int) -> None:
+        """The cut of rows that may share pages (waits for the device): those that do go to pages of their own, and what they held goes back where no other row has it; the others
+        are cut where they lie.  A row that a call must leave alone is shown to it with no tokens (first = seq_len)."""
+        m, B, span, first = self.main, self.B, self.span, self.span.first
+        at = torch.arange(0, 16 * self.max_pages, 16, dtype=torch.int32, device=self.dev)
+        held = (self.page_table >= 0) & (at + 16 > first[:, None]) & (at < self.seq_len[:, None])
+        refs = self.pages.ref[self.page_table.clamp(0, self.n_pages - 1).long()]
+        moves = (self.seq_len - first > keep + spare) & (held & (refs > 1)).any(dim=1)
+        some, self._shared = torch.stack([moves.any(), (self.pages.ref > 1).any()]).tolist()
+        own = torch.where(moves, self.seq_len, first)
+
+        def cut(of: torch.Tensor, dst: Optional[torch.Tensor]) -> None:
+            m.hydra_kv_evict(B, self.seq_len, hb.KVSpan(span.kv, of, span.n_sinks, 0, span.span_hint, span.score), keep, recent, spare, self._kept, self._evicted, dst_table=dst)
+
+        cut(own, None)
+        first.copy_(torch.where(moves, first, own))
+        if not some:
+            return
+        here = self._evicted.clone()
+        self._drop_scratch()                          # with what those rows have left
+        zero = torch.zeros_like(self.seq_len)
+        whole = zero + 16 * self.max_pages
+        m.hydra_pages_reserve(B, self._pages_ws, self._dst, torch.where(moves, self.seq_len - keep, zero), torch.where(moves, self.seq_len, zero), 0, self._lists[4])
+        if not bool(self._lists[4][:B].all()):
+            m.hydra_pages_release(B, self._dst, None, zero)
+            raise RuntimeError(f"the pool of {self.n_pages} pages is exhausted: no room for the kept tokens of rows that share pages")
+        own = torch.where(moves, first, self.seq_len)
+        cut(own, self._dst.page_table)
+        done = self._evicted > 0
+        first.copy_(torch.where(done, own, first))
+        m.hydra_pages_release(B, self.pages, None, torch.where(done, zero, whole))
+        m.hydra_pages_release(B, self._dst, None, torch.where(done, whole, zero))        # of rows that had to stay whole
+        self.page_table.copy_(torch.where(done[:, None], self._dst.page_table, self.page_table))
+        self._dst.page_table.fill_(-1)
+        self._evicted += here
 
     def _incomplete(self) -> torch.Tensor:
         """The 16-bit page of every row that its next token goes to (any page where the row holds none there)."""

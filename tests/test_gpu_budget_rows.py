@@ -58,21 +58,72 @@ def test_a_row_that_cannot_be_cut_gives_back_the_pages_reserved_for_it():
     s.fork([0, 0, 0, 0])
     for _ in range(2):
         s.step()
-    assert s.main.read_flags() == 0 and s._shared
+    assert s.main.read_flags() == 0
     s._drop_scratch()
     keep, s._trim = s._trim, lambda grown: None
     s.step()
     s._drop_scratch()
     lens = (s.seq_len - s.span.first).tolist()
     assert min(lens) > 64
+    s.fork([0, 1, 2, 2])
+    assert s.main.read_flags() == 0
+    lens[3] = lens[2]
     bad = int(s.span.first[2]) // 16 + 1
     page = int(s.page_table[2, bad])
     s.page_table[2, bad] = s.n_pages + 3
     s.pages.ref[page] -= 1
-    s.fork([0, 1, 2, 0])                                                     # rows 0 and 3 share pages
-    s.main.read_flags()
     assert rows_and_counts_agree(s)
     keep(1)
     assert s.main.read_flags() == 64 and (s.seq_len - s.span.first).tolist() == [64, 64, lens[2], 64]
     assert rows_and_counts_agree(s)
     assert (s._dst.page_table == -1).all()
+
+
+def test_rows_that_share_no_longer_are_cut_where_they_lie():
+    """A fork whose other row ended: a pool of 12 pages holds two rows of 64 tokens and a tree each, and not what a cut to other pages takes besides."""
+    weights = make_weights(F32)
+    kw = dict(budget=(64, 24, 0), prefill_chunk=32)
+    s = gpu_session(F32, TREE, 2, 400, weights, pool_pages=12, **kw)
+    alone = gpu_session(F32, TREE, 1, 400, weights, **kw)
+    prompt = text(0, 64).reshape(1, 64)
+    s.prefill(prompt)
+    alone.prefill(prompt)
+    s.fork([0, 0])
+    s.free_rows([1])
+    for _ in range(60):
+        s.step()
+        alone.step()
+        assert int(s.seq_len[0]) == int(alone.seq_len[0]) and int(s.root[0]) == int(alone.root[0])
+    assert (s.seq_len - s.span.first).tolist() == [64, min(64, int(s.seq_len[1]))] and not s._shared
+    assert s.main.read_flags() == 0 and rows_and_counts_agree(s)
+
+
+def test_rows_that_share_pages_beside_rows_that_do_not():
+    """Rows 0 and 1 are copies of one prompt, rows 2 and 3 have their own, in a pool without room for copies of all four: texts, lists of kept slots and sums of sessions of one row."""
+    keep, recent, slack, B = 64, 24, 20, 4
+    weights = make_weights(F32)
+    kw = dict(budget=(keep, recent, slack), sinks=3, prefill_chunk=32, want_logits=True)
+    prompts = torch.stack([text(b, 90) for b in (0, 0, 2, 3)])
+    s = gpu_session(F32, TREE, B, 400, weights, pool_pages=44, **kw)
+    s.prefill(prompts)
+    s.fork([0, 0, 2, 3])
+    singles = [gpu_session(F32, TREE, 1, 400, weights, **kw) for _ in range(B)]
+    for b, one in enumerate(singles):
+        one.prefill(prompts[b:b + 1])
+    u = torch.tensor([0.11, 0.37, 0.62, 0.93], device="cuda:0")
+    cuts = [0] * B
+    for step in range(30):
+        v = (u + 0.29 * step) % 1.0
+        before = s.span.first.tolist()
+        s.step(typical=(0.8, 0.2, 0.4, v))
+        for b, one in enumerate(singles):
+            one.step(typical=(0.8, 0.2, 0.4, v[b:b + 1].contiguous()))
+            assert int(one.seq_len[0]) == int(s.seq_len[b]) and int(one.span.first[0]) == int(s.span.first[b]) and int(one.root[0]) == int(s.root[b])
+            if int(s.span.first[b]) != before[b]:
+                cuts[b] += 1
+                assert torch.equal(s._kept[:, b], one._kept[:, 0])
+            F, L = int(s.span.first[b]), int(s.seq_len[b])
+            x, y = s.span.score[:, b, :, F:L], one.span.score[:, 0, :, F:L]
+            assert ((x - y).abs() <= 1e-4 * y.abs() + 1e-6).all()
+        assert rows_and_counts_agree(s)
+    assert min(cuts) >= 2 and s.main.read_flags() == 0
