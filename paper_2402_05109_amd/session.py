@@ -322,17 +322,18 @@ class Session:
 
     def _keep_accepted(self, c: hb.Hydra, o: _Outputs, B: int, h_last: torch.Tensor, root: torch.Tensor) -> None:
         # (no hydra_score_compact: a prompt's path is the identity, and the root of a step sees no other node, so their sums all begin at 0)
+        if self.budget is not None:
+            self._growth += c.depth + 1               # first: whatever is broken off behind this is not forgotten
         c.kv_compact(B, o.n_acc, o.path, o.next_root, o.last_node, o.hidden, self.kv, self.seq_len, h_last, root, o.kv_index)
         if self.kv8 is not None:
             c.hydra_kv8_seal(B, self.seq_len, self.kv8)
 
-    def _trim(self, grown: int) -> None:
+    def _trim(self) -> None:
         """Rows over the budget are cut, once in a while: a cut leaves at most keep + slack / 2 tokens, and the next one comes before a row can have taken
         the other half."""
         if self.budget is None:
             return
         keep, recent, slack = self.budget
-        self._growth += grown
         if self._growth <= slack - slack // 2 or max(self.host_len, self._other_len) <= keep + slack // 2:
             return
         self.span.span_hint = 0 if self.host_len == 0 else max(self.host_len, self._other_len)
@@ -573,7 +574,7 @@ class Session:
                 pos += n
                 self.host_len += n
                 self._growth_since_copy += n          # a length on its way to the host was read before these
-                self._trim(n)
+                self._trim()
         except BaseException:
             if behind is not None:                    # broken off: back to the text that h_last and root belong to
                 self._back_to(behind)
@@ -643,7 +644,7 @@ class Session:
         self._keep_accepted(c, o, self.B, self.h_last, self.root)
         self.host_len += c.depth + 1          # upper bound; the device holds the exact value
         self._growth_since_copy += c.depth + 1
-        self._trim(c.depth + 1)
+        self._trim()
 
     def step(self, name: str = "main", hook=None, typical=None) -> None:
         """One speculative step of every row.  `hook(outputs)` may edit tree_tokens between

@@ -60,7 +60,7 @@ def test_a_row_that_cannot_be_cut_gives_back_the_pages_reserved_for_it():
         s.step()
     assert s.main.read_flags() == 0
     s._drop_scratch()
-    keep, s._trim = s._trim, lambda grown: None
+    keep, s._trim = s._trim, lambda: None
     s.step()
     s._drop_scratch()
     lens = (s.seq_len - s.span.first).tolist()
@@ -73,7 +73,7 @@ def test_a_row_that_cannot_be_cut_gives_back_the_pages_reserved_for_it():
     s.page_table[2, bad] = s.n_pages + 3
     s.pages.ref[page] -= 1
     assert rows_and_counts_agree(s)
-    keep(1)
+    keep()
     assert s.main.read_flags() == 64 and (s.seq_len - s.span.first).tolist() == [64, 64, lens[2], 64]
     assert rows_and_counts_agree(s)
     assert (s._dst.page_table == -1).all()
@@ -127,3 +127,30 @@ def test_rows_that_share_pages_beside_rows_that_do_not():
             assert ((x - y).abs() <= 1e-4 * y.abs() + 1e-6).all()
         assert rows_and_counts_agree(s)
     assert min(cuts) >= 2 and s.main.read_flags() == 0
+
+
+@pytest.mark.parametrize("pool", [None, 40])
+@pytest.mark.parametrize("behind", [True, False])
+def test_a_chunk_that_is_broken_off_behind_its_compaction_counts(behind, pool):
+    """An interrupt between the compaction of a chunk and the cut (or in front of both): what the row has taken is remembered, and it never holds more than keep + slack."""
+    keep, slack = 64, 40
+    weights = make_weights(F32)
+    s = gpu_session(F32, TREE, 1, 600, weights, budget=(keep, 16, slack), prefill_chunk=32, pool_pages=pool)
+    s.prefill(text(0, 96).reshape(1, 96))
+    assert int(s.seq_len[0] - s.span.first[0]) <= keep + slack // 2
+    compact = s._keep_accepted
+
+    def broken(*args):
+        if behind:
+            compact(*args)
+        raise KeyboardInterrupt
+
+    for n in (17, 15):                                                       # slack - slack / 2 = 20 is reached with the second one
+        s._keep_accepted = broken
+        with pytest.raises(KeyboardInterrupt):
+            s.prefill(text(1, n).reshape(1, n))
+        s._keep_accepted = compact
+    for _ in range(40):
+        s.step()
+        assert int(s.seq_len[0] - s.span.first[0]) <= min(keep + slack, s._most_held())
+    assert s.main.read_flags() == 0

@@ -135,13 +135,13 @@ def test_a_budget_in_16_bits_follows_the_definition(keep, recent, sinks, pool):
         s.ws.fill_(255)
         forward(*args, **kw)
 
-    def follow(grown):
+    def follow():
         for b, d in enumerate(decs):
             d.feed(fed[b][0], fed[b][1])
         check_scores(cfg, s, decs)
         score = to_np(s.span.score)
         state = [(int(s.span.first[b]), int(s.seq_len[b])) for b in range(B)]
-        trim(grown)
+        trim()
         for b, d in enumerate(decs):
             first, n = state[b]
             cut = n - first > keep
