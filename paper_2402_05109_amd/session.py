@@ -47,7 +47,8 @@ class Session:
     What a text of any length costs can be bounded (positions go on, up to max_len): window = W lets a token see the last W positions and the first
     `sinks`; budget = (keep, recent, slack) keeps about `keep` tokens per layer and head, the first `sinks`, the last `recent` and those that drew most
     attention so far; between steps and prompt chunks no row holds more than keep + slack.  A prompt's tokens all count, of a step its root, the one node that is sure to stay.
-    With pool_pages, pages that nobody sees any more go back to the pool."""
+    With pool_pages, pages that nobody sees any more go back to the pool.  A step under a budget that is captured into a graph cuts the rows over keep + slack / 2
+    on every replay; not behind fork(), where a cut waits for the device."""
 
     def __init__(self, shape, parent: Sequence[int], B: int, max_len: int,
                  get_tensor: Callable[[str], torch.Tensor], device="cuda:0", prefill_chunk: int = 64,
@@ -138,6 +139,7 @@ class Session:
                 self._evicted = torch.zeros(B, **i32)
             self.span = hb.KVSpan(self.kv, first=first, n_sinks=sinks, window=window or 0, score=score)
             self._growth = 0                          # tokens that a row can have taken since the last cut
+            self._replays = False                     # whether a graph holds a step: replays make rows longer than host_len knows
             self._shared = False                      # rows may share pages
             if self.pool:
                 self._lo = torch.zeros(B, **i32)
@@ -287,7 +289,8 @@ class Session:
         held = max(self.host_len, self._other_len)
         if self.budget is not None:
             keep, _, slack = self.budget
-            held = min(held, keep + slack // 2 + self._growth)
+            most = keep + slack // 2 + self._growth
+            held = most if self._replays else min(held, most)
         return held
 
     def reset(self) -> None:
@@ -330,18 +333,24 @@ class Session:
 
     def _trim(self) -> None:
         """Rows over the budget are cut, once in a while: a cut leaves at most keep + slack / 2 tokens, and the next one comes before a row can have taken
-        the other half."""
+        the other half.  A graph gets the cut with each step, which then cuts the rows over keep + slack / 2 on every replay."""
         if self.budget is None:
             return
         keep, recent, slack = self.budget
-        if self._growth <= slack - slack // 2 or max(self.host_len, self._other_len) <= keep + slack // 2:
+        captures = torch.cuda.is_current_stream_capturing()
+        if captures and self.pool and self._shared:
+            raise RuntimeError("the cut of rows that may share pages waits for the device: such a step cannot be captured")
+        self._replays |= captures
+        most = max(self.host_len, self._other_len)
+        if not captures and (self._growth <= slack - slack // 2 or (most <= keep + slack // 2 and not self._replays)):
             return
-        self.span.span_hint = 0 if self.host_len == 0 else max(self.host_len, self._other_len)
+        self.span.span_hint = keep + slack + self._growth if self._replays else most
         if self.pool and self._shared:
             self._cut_shared(keep, recent, slack // 2)
         else:
             self.main.hydra_kv_evict(self.B, self.seq_len, self.span, keep, recent, slack // 2, self._kept, self._evicted)
-        self._growth = 0
+        if not captures:                              # (nothing has run: what a row may have taken stays counted)
+            self._growth = 0
 
     def _cut_shared(self, keep: int, recent: int, spare: int) -> None:
         """The cut of rows that may share pages (waits for the device): those that do go to pages of their own, and what they held goes back where no other row has it; the others
