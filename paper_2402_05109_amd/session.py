@@ -46,7 +46,9 @@ class Session:
 
     What a text of any length costs can be bounded (positions go on, up to max_len): window = W lets a token see the last W positions and the first
     `sinks`; budget = (keep, recent, slack) keeps about `keep` tokens per layer and head, the first `sinks`, the last `recent` and those that drew most
-    attention so far; between steps and prompt chunks no row holds more than keep + slack.  A prompt's tokens all count, of a step its root, the one node that is sure to stay.
+    attention so far; between steps and prompt chunks no row holds more than keep + slack.  A prompt's tokens all count, of a step its root, the one
+    node that is sure to stay when the weights are added up: of n tokens that a step accepts n - 1 give none away and begin with none, so what is kept behind generated text depends on
+    the tree and on acceptance and is not what decoding token by token would keep under the same budget (one node a step: it is).
     With pool_pages, pages that nobody sees any more go back to the pool.  A step under a budget that is captured into a graph cuts the rows over keep + slack / 2
     on every replay; not behind fork(), where a cut waits for the device."""
 
